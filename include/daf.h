@@ -380,6 +380,159 @@ daf_status_t daf_decoder_layer(const daf_attn_cfg_t *cfg,
                                void *k_cache, void *v_cache, void *workspace,
                                size_t ws_bytes, hipStream_t stream);
 
+/* ---- Paged 8-bit K/V cache -------------------------------------------------
+ *
+ * The offline document K/V that DAF reuses (Sec. 1), held in 8 bits and in pages
+ * that sequences share: a document set is stored once, each request forks it,
+ * gets its own copy of the pages it writes its recomputed rows into (the hybrid
+ * cache, Sec. 2 item 2), answers its question over it and decodes from it.
+ *
+ * A page holds DAF_PAGE_TOKENS tokens of every layer and K/V head: token t of a
+ * sequence lies in slot t % 64 of the page table[seq][t / 64]. Per layer, page and
+ * head it has e4m3 codes (OCP: 3 mantissa bits, largest 448, no infinities) and one
+ * scale each for K and V, 0 or a power of two >= 2^-100; a value is code * scale.
+ * V is stored transposed, so that a product over tokens reads tokens in order.
+ *
+ * The arrays are DEVICE memory, owned by the caller and 16-byte aligned. A new
+ * cache has refs and len all 0; nothing else needs a value. What the calls below
+ * read on the device is not checked by the host: table entries outside
+ * [0, n_pages) count as pages that are not there (no keys, nothing read or
+ * written), sequences outside [0, n_seqs) as empty ones, and len is read as at
+ * most max_seq_pages * 64. No such value makes a call read or write out of
+ * bounds. Calls that change a cache are ordered by the caller with the calls
+ * that use it (one stream, or events). */
+enum { DAF_PAGE_TOKENS = 64 };
+
+typedef struct {
+  int32_t n_layers, n_pages;     /* >= 1 */
+  int32_t n_kv_heads, head_dim;  /* Hkv >= 1; D: 64 or 128 */
+  int32_t n_seqs, max_seq_pages; /* rows and row length of table; max_seq_pages < 2^25 */
+  void *k;        /* e4m3 [n_layers][n_pages][Hkv][64][D] */
+  void *v;        /* e4m3 [n_layers][n_pages][Hkv][D][64] */
+  float *k_scale; /* [n_layers][n_pages][Hkv] */
+  float *v_scale; /* [n_layers][n_pages][Hkv] */
+  int32_t *table; /* [n_seqs][max_seq_pages]: page ids */
+  int32_t *len;   /* [n_seqs]: tokens held */
+  int32_t *refs;  /* [n_pages]: table entries that name the page; 0 = free */
+} daf_cache_t;
+
+/* Rows of a ragged batch of requests on a cache. cu is HOST memory, the [n + 1]
+ * prefix sums (from 0) of the rows per request, read during the call only. seq
+ * (DEVICE int32 [n]) is each request's sequence; NULL: request b is sequence b.
+ * pos (DEVICE int32 [cu[n]]) is each row's position in its sequence, strictly
+ * increasing within a request; NULL: a request's rows are the last ones of its
+ * sequence (row j of m at position len - m + j). */
+typedef struct {
+  int32_t n;
+  const int32_t *cu;
+  const int32_t *seq;
+  const int32_t *pos;
+} daf_cache_rows_t;
+
+/* Write the rows' K/V (k, v [cu[n]][Hkv][D] of cfg's dtype) into one layer of
+ * the cache: pos = NULL appends (daf_pages_extend has taken the pages and raised
+ * len already), pos = the important tokens' positions makes the hybrid cache
+ * (Sec. 2 item 2; daf_pages_unshare first where pages are shared).
+ *   A page and head's scale becomes the larger of its present one, if a token of
+ * the page stays (one below len, or with pos = NULL below the new rows, that the
+ * call does not write), and the smallest power of two >= 2^-100 under which the
+ * largest new magnitude is at most 448 (none for all zeros). Codes are rounded to
+ * nearest even; the codes that stay are rounded again where the scale grows (a
+ * loss only where they fall below the smallest normal code). Where no token of
+ * the page stays, its other slots become 0. Infinities count as the largest
+ * finite value of the dtype, NaN stays NaN and does not count for the scale.
+ *   Rows whose position is not in [0, len) are left out. The result is undefined
+ * (but in bounds) if positions do not increase, if two requests of the call name
+ * the same page, or where a page is shared: its other owners see the rows too. */
+daf_status_t daf_cache_write(const daf_attn_cfg_t *cfg, const daf_cache_t *cache,
+                             int32_t layer, const daf_cache_rows_t *rows,
+                             const void *k, const void *v, hipStream_t stream);
+
+/* The rows' K/V of one layer as values (k, v [cu[n]][Hkv][D] of cfg's dtype, both
+ * of which hold them exactly), e.g. the k_cached of daf_select_important. k or v
+ * may be NULL (not wanted). Rows whose position is not in [0, len), or whose page
+ * is not there, become 0. */
+daf_status_t daf_cache_read(const daf_attn_cfg_t *cfg, const daf_cache_t *cache,
+                            int32_t layer, const daf_cache_rows_t *rows, void *k,
+                            void *v, hipStream_t stream);
+
+/* Bytes of workspace daf_cache_attn needs (0 on bad input or none needed). */
+size_t daf_cache_attn_workspace_size(const daf_attn_cfg_t *cfg,
+                                     const daf_cache_t *cache,
+                                     const daf_cache_rows_t *rows, int32_t max_len);
+
+/* Attention of the rows over one layer of the cache: question rows (stage 2,
+ * Sec. 2 item 2, on the hybrid cache), rows at given positions, or the single row
+ * per sequence of a decode step.
+ *   q [cu[n]][Hq][D] -> o [cu[n]][Hq][D]; lse: nullable float32 [Hq][cu[n]].
+ * A row sees the keys 0 .. its position of its sequence, as far as len goes (pos =
+ * NULL: causal, aligned to the end; pos need not increase here). A row that sees
+ * no key gets o = 0 and lse = -infinity. Keys that no row of the call sees may
+ * hold anything, NaN included; all others must be finite.
+ *   max_len: a HOST bound on the sequences' len (at most max_seq_pages * 64) that
+ * the launch is planned for; len is read on the device, at most max_len counts.
+ *   Softmax and sums in fp32; the codes, and q in bf16, enter the products
+ * exactly. bf16: probabilities are rounded to bf16 for the value product; the
+ * row's sum and the LSE are those of the unrounded ones. fp32: q and the
+ * probabilities enter as three bf16 terms each (24 bits).
+ *   workspace: at least daf_cache_attn_workspace_size bytes, 16-byte aligned,
+ * contents undefined after the call. */
+daf_status_t daf_cache_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *cache,
+                            int32_t layer, const daf_cache_rows_t *rows,
+                            int32_t max_len, const void *q, void *o, float *lse,
+                            void *workspace, size_t ws_bytes, hipStream_t stream);
+
+/* Page calls. They work on all layers, take sequence and page lists in DEVICE
+ * memory and never wait for the device. Those that take pages take the free ones
+ * (refs 0) of the lowest ids, in the order of the requests and of their pages, and
+ * do all or nothing: *status (DEVICE int32) becomes 0, or the number of pages that
+ * were lacking, or -1 if an argument is invalid (a sequence out of range or named
+ * twice, a length out of range, positions that do not increase), and unless it is 0
+ * nothing else changes.
+ *
+ * Workspace of any of them (fork, unshare, compact); 0 on bad input. 16-byte
+ * aligned, contents undefined after the call. */
+size_t daf_pages_workspace_size(const daf_cache_t *cache);
+
+/* Lengthen n (<= 4096) distinct sequences by n_new[i] >= 0 tokens: pages as needed,
+ * len raised. seq NULL: sequences 0 .. n-1; n_new NULL: one token each. */
+daf_status_t daf_pages_extend(const daf_cache_t *cache, int32_t n,
+                              const int32_t *seq, const int32_t *n_new,
+                              int32_t *status, hipStream_t stream);
+
+/* Make the empty (len 0) sequence dst[i] a copy of src[i], i < n (<= 4096): full
+ * pages are shared (refs + 1), a last page that is not full is copied into a page
+ * of its own. dst are distinct and none of them is a src; a src may be named
+ * several times. */
+daf_status_t daf_pages_fork(const daf_cache_t *cache, int32_t n,
+                            const int32_t *src, const int32_t *dst,
+                            int32_t *status, void *workspace, size_t ws_bytes,
+                            hipStream_t stream);
+
+/* Give the sequences of `rows` (n <= 256, distinct) copies of their own of the
+ * pages that hold a row's position and whose refs is above 1 before the call. */
+daf_status_t daf_pages_unshare(const daf_cache_t *cache,
+                               const daf_cache_rows_t *rows, int32_t *status,
+                               void *workspace, size_t ws_bytes, hipStream_t stream);
+
+/* Empty n sequences: refs - 1 for their pages (free at 0), their table entries
+ * become -1, len 0. A sequence named twice or out of range is no error. seq NULL:
+ * sequences 0 .. n-1. */
+daf_status_t daf_pages_free(const daf_cache_t *cache, int32_t n,
+                            const int32_t *seq, hipStream_t stream);
+
+/* Copy the contents of page src[i] to page dst[i], i < n, in every layer; refs and
+ * tables stay as they are. No page may be a dst twice, or both a src and a dst
+ * (undefined contents); pairs with an id outside [0, n_pages) are left out. */
+daf_status_t daf_pages_copy(const daf_cache_t *cache, int32_t n, const int32_t *src,
+                            const int32_t *dst, hipStream_t stream);
+
+/* Move the *n_live (DEVICE int32, output) pages in use to the ids 0 .. *n_live - 1:
+ * the i-th used page at or past n_live, in order of ids, goes to the i-th free one
+ * below; refs and the tables (entries below len) follow. */
+daf_status_t daf_pages_compact(const daf_cache_t *cache, int32_t *n_live,
+                               void *workspace, size_t ws_bytes, hipStream_t stream);
+
 /* Detail of the last failure on the calling thread ("" if none). */
 const char *daf_last_error(void);
 

@@ -21,6 +21,10 @@ __all__ = [
     "daf_layer_attn_noalloc", "daf_check_indices", "daf_select_important",
     "daf_linear", "daf_linear_swiglu", "daf_rmsnorm", "daf_rope", "daf_silu_mul", "daf_decoder_layer_workspace_size",
     "daf_decoder_layer", "LayerWeights", "DAF_LAYER_DAF", "DAF_LAYER_FULL",
+    "DAF_PAGE_TOKENS", "Cache", "CacheRows",
+    "daf_cache_write", "daf_cache_read", "daf_cache_attn_workspace_size", "daf_cache_attn",
+    "daf_pages_workspace_size", "daf_pages_extend", "daf_pages_fork", "daf_pages_unshare", "daf_pages_free",
+    "daf_pages_copy", "daf_pages_compact",
     "daf_status_string", "daf_last_error", "daf_version", "EXPORTED",
 ]
 
@@ -30,6 +34,7 @@ DAF_BF16, DAF_F32 = 0, 1
 DAF_SRC_TOKENS, DAF_SRC_DOCS = 0, 1
 DAF_FUSE_KV, DAF_FUSE_HIDDEN = 1, 2
 DAF_LAYER_DAF, DAF_LAYER_FULL = 0, 1
+DAF_PAGE_TOKENS = 64
 
 # every symbol include/daf.h declares
 EXPORTED = [
@@ -37,7 +42,11 @@ EXPORTED = [
     "daf_fuse", "daf_layer_workspace_size", "daf_layer_attn", "daf_layer_noalloc_max_bytes",
     "daf_layer_attn_noalloc", "daf_check_indices", "daf_select_important",
     "daf_linear", "daf_linear_swiglu", "daf_rmsnorm", "daf_rope", "daf_silu_mul", "daf_decoder_layer_workspace_size",
-    "daf_decoder_layer", "daf_status_string", "daf_last_error", "daf_version",
+    "daf_decoder_layer",
+    "daf_cache_write", "daf_cache_read", "daf_cache_attn_workspace_size", "daf_cache_attn",
+    "daf_pages_workspace_size", "daf_pages_extend", "daf_pages_fork", "daf_pages_unshare", "daf_pages_free",
+    "daf_pages_copy", "daf_pages_compact",
+    "daf_status_string", "daf_last_error", "daf_version",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -99,6 +108,49 @@ class LayerWeights(ctypes.Structure):
         return w
 
 
+class Cache(ctypes.Structure):
+    """daf_cache_t: a paged 8-bit K/V cache. Build it with ``from_tensors``,
+    which takes the sizes from the tensors and keeps them alive."""
+    _fields_ = [("n_layers", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("n_seqs", ctypes.c_int32), ("max_seq_pages", ctypes.c_int32),
+                ("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("table", _vp), ("len", _vp),
+                ("refs", _vp)]
+    _NAMES = ("k", "v", "k_scale", "v_scale", "table", "len", "refs")
+
+    @classmethod
+    def from_tensors(cls, t: dict) -> "Cache":
+        """k [layers][pages][Hkv][64][D] and v [layers][pages][Hkv][D][64] of one-byte
+        elements, k_scale and v_scale float32 [layers][pages][Hkv], table int32
+        [sequences][pages per sequence], len int32 [sequences], refs int32 [pages]."""
+        layers, pages, heads, tokens, d = t["k"].shape
+        want = {"k": (layers, pages, heads, DAF_PAGE_TOKENS, d), "v": (layers, pages, heads, d, DAF_PAGE_TOKENS),
+                "k_scale": (layers, pages, heads), "v_scale": (layers, pages, heads),
+                "table": (t["len"].shape[0], t["table"].shape[-1]), "refs": (pages,)}
+        size = {"k": 1, "v": 1}
+        for n in cls._NAMES:
+            x = t[n]
+            if n in want and tuple(x.shape) != want[n]:
+                raise ValueError(f"{n} has shape {tuple(x.shape)}, not {want[n]}")
+            if x.element_size() != size.get(n, 4) or not x.is_contiguous():
+                raise ValueError(f"{n} must be contiguous, with elements of {size.get(n, 4)} bytes")
+        c = cls(layers, pages, heads, d, t["len"].shape[0], t["table"].shape[1], *[t[n].data_ptr() for n in cls._NAMES])
+        c._keep = t
+        return c
+
+
+class CacheRows(ctypes.Structure):
+    """daf_cache_rows_t: rows of a ragged batch of requests on a cache. ``cu`` are
+    the host prefix sums of the rows per request; ``seq`` and ``pos`` (device, or
+    None) are kept alive."""
+    _fields_ = [("n", ctypes.c_int32), ("cu", ctypes.POINTER(ctypes.c_int32)), ("seq", _vp), ("pos", _vp)]
+
+    def __init__(self, cu, seq=None, pos=None):
+        self._cu = np.ascontiguousarray(cu, dtype=np.int32)
+        self._keep = (seq, pos)
+        super().__init__(len(self._cu) - 1, self._cu.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)), _ptr(seq),
+                         _ptr(pos))
+
+
 _lib = None
 
 
@@ -111,6 +163,7 @@ def lib() -> ctypes.CDLL:
                                "`python -c 'import __graft_entry__ as g; g.build()'`")
         L = ctypes.CDLL(library_path)
         cfgp, bp = ctypes.POINTER(AttnCfg), ctypes.POINTER(_BatchC)
+        cp, rp = ctypes.POINTER(Cache), ctypes.POINTER(CacheRows)
         i32, i64, u32, sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_size_t
         sig = {
             "daf_gather_important": (i32, [bp, i32, _vp, i64, _vp, _vp, _vp]),
@@ -134,6 +187,17 @@ def lib() -> ctypes.CDLL:
             "daf_decoder_layer_workspace_size": (sz, [cfgp, ctypes.POINTER(LayerWeights), bp, i32]),
             "daf_decoder_layer": (i32, [cfgp, ctypes.POINTER(LayerWeights), bp, i32, _vp, _vp, _vp, _vp, _vp,
                                         _vp, sz, _vp]),
+            "daf_cache_write": (i32, [cfgp, cp, i32, rp, _vp, _vp, _vp]),
+            "daf_cache_read": (i32, [cfgp, cp, i32, rp, _vp, _vp, _vp]),
+            "daf_cache_attn_workspace_size": (sz, [cfgp, cp, rp, i32]),
+            "daf_cache_attn": (i32, [cfgp, cp, i32, rp, i32, _vp, _vp, _vp, _vp, sz, _vp]),
+            "daf_pages_workspace_size": (sz, [cp]),
+            "daf_pages_extend": (i32, [cp, i32, _vp, _vp, _vp, _vp]),
+            "daf_pages_fork": (i32, [cp, i32, _vp, _vp, _vp, _vp, sz, _vp]),
+            "daf_pages_unshare": (i32, [cp, rp, _vp, _vp, sz, _vp]),
+            "daf_pages_free": (i32, [cp, i32, _vp, _vp]),
+            "daf_pages_copy": (i32, [cp, i32, _vp, _vp, _vp]),
+            "daf_pages_compact": (i32, [cp, _vp, _vp, sz, _vp]),
             "daf_status_string": (ctypes.c_char_p, [i32]),
             "daf_last_error": (ctypes.c_char_p, []),
             "daf_version": (i32, []),
@@ -301,6 +365,54 @@ def daf_layer_attn_noalloc(cfg: AttnCfg, batch: Batch, idx, q_imp, k_imp, v_imp,
 
 def daf_check_indices(batch: Batch, idx, d_bad_count, stream=None):
     _check(lib().daf_check_indices(_bp(batch), _ptr(idx), _ptr(d_bad_count), _stream(stream)))
+
+
+# ---- the paged 8-bit K/V cache ------------------------------------------------
+def daf_cache_write(cfg: AttnCfg, cache: Cache, layer: int, rows: CacheRows, k, v, stream=None):
+    _check(lib().daf_cache_write(_cfgp(cfg), cache, layer, rows, _ptr(k), _ptr(v), _stream(stream)))
+
+
+def daf_cache_read(cfg: AttnCfg, cache: Cache, layer: int, rows: CacheRows, k, v, stream=None):
+    _check(lib().daf_cache_read(_cfgp(cfg), cache, layer, rows, _ptr(k), _ptr(v), _stream(stream)))
+
+
+def daf_cache_attn_workspace_size(cfg: AttnCfg, cache: Cache, rows: CacheRows, max_len: int) -> int:
+    return int(lib().daf_cache_attn_workspace_size(_cfgp(cfg), cache, rows, max_len))
+
+
+def daf_cache_attn(cfg: AttnCfg, cache: Cache, layer: int, rows: CacheRows, max_len: int, q, o, lse, workspace,
+                   ws_bytes: int, stream=None):
+    _check(lib().daf_cache_attn(_cfgp(cfg), cache, layer, rows, max_len, _ptr(q), _ptr(o), _ptr(lse),
+                                _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def daf_pages_workspace_size(cache: Cache) -> int:
+    return int(lib().daf_pages_workspace_size(cache))
+
+
+def daf_pages_extend(cache: Cache, n: int, seq, n_new, status, stream=None):
+    _check(lib().daf_pages_extend(cache, n, _ptr(seq), _ptr(n_new), _ptr(status), _stream(stream)))
+
+
+def daf_pages_fork(cache: Cache, n: int, src, dst, status, workspace, ws_bytes: int, stream=None):
+    _check(lib().daf_pages_fork(cache, n, _ptr(src), _ptr(dst), _ptr(status), _ptr(workspace), ws_bytes,
+                                _stream(stream)))
+
+
+def daf_pages_unshare(cache: Cache, rows: CacheRows, status, workspace, ws_bytes: int, stream=None):
+    _check(lib().daf_pages_unshare(cache, rows, _ptr(status), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def daf_pages_free(cache: Cache, n: int, seq=None, stream=None):
+    _check(lib().daf_pages_free(cache, n, _ptr(seq), _stream(stream)))
+
+
+def daf_pages_copy(cache: Cache, n: int, src, dst, stream=None):
+    _check(lib().daf_pages_copy(cache, n, _ptr(src), _ptr(dst), _stream(stream)))
+
+
+def daf_pages_compact(cache: Cache, n_live, workspace, ws_bytes: int, stream=None):
+    _check(lib().daf_pages_compact(cache, _ptr(n_live), _ptr(workspace), ws_bytes, _stream(stream)))
 
 
 def daf_status_string(status: int) -> str:

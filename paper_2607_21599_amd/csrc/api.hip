@@ -9,6 +9,7 @@
 #include <mutex>
 #include <vector>
 
+#include "cache.h"
 #include "daf.h"
 #include "daf_internal.h"
 #include "gemm.h"
@@ -671,6 +672,12 @@ daf_status_t run_gemm(const GemmJob &g, hipStream_t st, float *part = nullptr) {
 }
 
 }  // namespace
+
+// The paged cache's entry points (cache_api.hip) report through the same buffer.
+daf_status_t daf::set_error(daf_status_t st, const char *text) {
+  snprintf(g_err, sizeof(g_err), "%s", text);
+  return st;
+}
 
 extern "C" {
 

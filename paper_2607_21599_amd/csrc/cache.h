@@ -1,0 +1,102 @@
+// Internal declarations of the paged 8-bit K/V cache (daf_cache_*, daf_pages_*).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "daf.h"
+
+namespace daf {
+
+constexpr int kPage = DAF_PAGE_TOKENS;  // tokens of a page
+constexpr int kMaxCacheReqs = 256;      // requests per launch (their prefix sums are a kernel argument)
+constexpr int kMaxPageSeqs = 4096;      // sequences per page call (one workgroup plans it)
+constexpr int kMinScaleExp = -100;      // exponent of the smallest scale
+
+// Error text of the calling thread (api.hip).
+daf_status_t set_error(daf_status_t st, const char *text);
+
+// What the kernels need of a cache; k/v and the scales start at the launch's layer.
+struct CacheView {
+  unsigned char *k, *v;
+  float *k_scale, *v_scale;
+  const int32_t *table, *len;
+  int32_t n_pages, hkv, d, n_seqs, max_seq_pages;
+};
+
+// Tokens of sequence `seq`, as far as its table row reaches; 0 out of range.
+__device__ __forceinline__ int seq_len(const int32_t *len, int n_seqs, int max_seq_pages, int seq) {
+  if ((unsigned)seq >= (unsigned)n_seqs) return 0;
+  return min(max(len[seq], 0), max_seq_pages * kPage);
+}
+
+// Row movement between rows [total][hkv][d] and the cache.
+struct StoreLaunch {
+  CacheView c;
+  const int32_t *seq, *pos;  // nullable, at the launch's first request / row
+  const void *k, *v;         // rows, at the launch's first row (nullable when reading)
+  int32_t n_req;
+  int32_t units;             // units of all requests: see unit0
+  int32_t per_req;           // units of every request where they are equal, else 0
+  int32_t cu[kMaxCacheReqs + 1];     // rows of the launch's requests, from 0
+  int32_t unit0[kMaxCacheReqs + 1];  // first unit of each request
+};
+static_assert(sizeof(StoreLaunch) < 4096, "kernel arguments must fit 4 KiB");
+constexpr int kStoreRows = 8;  // rows at positions: rows per unit
+hipError_t launch_cache_store(bool write, bool bf16, const StoreLaunch &p, hipStream_t st);
+
+// Attention over the cache.
+struct CacheAttnLaunch {
+  CacheView c;
+  const int32_t *seq, *pos;
+  const void *q;
+  void *o;
+  float *lse;       // nullable; [hq][lse_stride] at the launch's first row
+  float *part_o;    // n_splits > 1: [row][hq][n_splits][d], normalised
+  float *part_lse;  // [row][hq][n_splits]
+  int32_t lse_stride;
+  int32_t hq, group;
+  int32_t max_len;
+  int32_t n_splits, split_pages;  // pages per split
+  float scale_log2;               // softmax scale * log2(e)
+  int32_t n_req;
+  int32_t blocks;                 // row blocks of all requests
+  int32_t per_req;                // row blocks of every request where they are equal, else 0
+  int32_t cu[kMaxCacheReqs + 1];
+  int32_t blk0[kMaxCacheReqs + 1];
+};
+static_assert(sizeof(CacheAttnLaunch) < 4096, "kernel arguments must fit 4 KiB");
+constexpr int kCacheAttnRows = 16;  // (row, head) pairs of a row block
+hipError_t launch_cache_attn(bool bf16, const CacheAttnLaunch &p, hipStream_t st);
+
+// Page calls.
+struct PoolView {
+  unsigned char *k, *v;
+  float *k_scale, *v_scale;
+  int32_t *table, *len, *refs;
+  int32_t n_layers, n_pages, hkv, d, n_seqs, max_seq_pages;
+};
+// Workspace of the page calls: a count, then three lists of n_pages.
+struct PageWork {
+  int32_t *count;  // [0]: pairs to copy, [1]: pages in use (compact)
+  int32_t *src, *dst, *aux;
+};
+constexpr size_t kPageWorkHead = 256;
+struct UnshareLaunch {
+  PoolView c;
+  PageWork w;
+  const int32_t *seq, *pos;
+  int32_t *status;
+  int32_t n_req;
+  int32_t cu[kMaxCacheReqs + 1];
+};
+hipError_t launch_pages_extend(const PoolView &c, int n, const int32_t *seq, const int32_t *n_new, int32_t *status,
+                               hipStream_t st);
+hipError_t launch_pages_fork(const PoolView &c, const PageWork &w, int n, const int32_t *src, const int32_t *dst,
+                             int32_t *status, hipStream_t st);
+hipError_t launch_pages_unshare(const UnshareLaunch &p, hipStream_t st);
+hipError_t launch_pages_free(const PoolView &c, int n, const int32_t *seq, hipStream_t st);
+hipError_t launch_pages_copy(const PoolView &c, int n, const int32_t *src, const int32_t *dst, hipStream_t st);
+hipError_t launch_pages_compact(const PoolView &c, const PageWork &w, int32_t *n_live, hipStream_t st);
+
+}  // namespace daf

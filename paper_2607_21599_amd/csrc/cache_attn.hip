@@ -1,0 +1,410 @@
+// Attention over the paged 8-bit K/V cache (daf_cache_attn).
+//
+// Per head h of a row with q, over the keys 0 .. limit of its sequence:
+//   s_t = q . k_t * scale,  o = sum_t exp(s_t - m) v_t / sum_t exp(s_t - m)
+// with one pass over the pages: a running maximum m and sum per row, the output
+// rescaled where m grows (fp32). The G query heads of a K/V head share its pages,
+// so a row block is 16 (row, head) pairs of one K/V head.
+//
+// Data path of a wave, one page (64 keys) of one head at a time:
+//  * K and V go from memory to registers in the layout that the matrix
+//    instructions take, 16 bytes per lane and load; the next page's loads are in
+//    flight while a page is worked on. No LDS.
+//  * e4m3 codes become bf16 exactly, and times their scale (a power of two) by the
+//    same conversion instruction, so no multiplication carries the scales.
+//  * S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_16x16x32_bf16. With the rows of K
+//    taken in the order key(t, m) = 16 (m / 4) + 4 t + m % 4 for block t and row m
+//    of the operand, a lane of group g (lane / 16) ends up with the probabilities
+//    of keys 16 g .. 16 g + 15 of row lane % 16, which is how the second product
+//    wants them, and V^T, stored transposed, is read as 16 consecutive keys.
+//  * fp32: q and the probabilities enter as three bf16 terms each.
+// The four waves of a workgroup take the pages of its split in turn and join their
+// (m, sum, O) through LDS; splits are joined by a second kernel.
+#include <math.h>
+
+#include "cache.h"
+
+namespace daf {
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr int kRows = kCacheAttnRows;
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// eight codes (8 bytes) times a power of two, as bf16
+__device__ __forceinline__ bf16x8 widen(unsigned lo, unsigned hi, float scale) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+#else
+  return bf16x8{};
+#endif
+}
+
+__device__ __forceinline__ f32x4 mfma(const bf16x8 &a, const bf16x8 &b, const f32x4 &c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+#else
+  return c;
+#endif
+}
+
+// x and the same register of the lanes that hold the same row (lane ^ 16, ^ 32)
+__device__ __forceinline__ float row_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float row_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+// TERMS bf16 values whose sum is x: one rounding for bf16, 24 bits for fp32
+template <int TERMS>
+__device__ __forceinline__ void split_terms(const float (&x)[8], bf16x8 (&out)[TERMS]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float r = x[i];
+#pragma unroll
+    for (int j = 0; j < TERMS; ++j) {
+      out[j][i] = (__bf16)r;
+      r -= (float)out[j][i];
+    }
+  }
+}
+
+struct Request {
+  int b, block;      // request of the launch and row block in it
+  int row0, n;       // its rows
+  int L;             // tokens of its sequence
+  const int32_t *pages;
+};
+
+__device__ __forceinline__ Request find_request(const CacheAttnLaunch &p, int blk) {
+  Request r;
+  int b = 0;
+  if (p.per_req) {
+    b = blk / p.per_req;
+    r.block = blk - b * p.per_req;
+  } else {
+    for (int step = kMaxCacheReqs / 2; step; step >>= 1)
+      if (b + step < p.n_req && p.blk0[b + step] <= blk) b += step;
+    r.block = blk - p.blk0[b];
+  }
+  r.b = b;
+  r.row0 = p.cu[b];
+  r.n = p.cu[b + 1] - r.row0;
+  const int seq = p.seq ? p.seq[b] : b;
+  r.L = min(seq_len(p.c.len, p.c.n_seqs, p.c.max_seq_pages, seq), p.max_len);
+  r.pages = p.c.table + (int64_t)((unsigned)seq < (unsigned)p.c.n_seqs ? seq : 0) * p.c.max_seq_pages;
+  return r;
+}
+
+// last key that row j of the request sees
+__device__ __forceinline__ int row_limit(const CacheAttnLaunch &p, const Request &r, int j) {
+  return p.pos ? min(p.pos[r.row0 + j], r.L - 1) : r.L - r.n + j;
+}
+
+template <bool BF16>
+__device__ __forceinline__ void store_out(const CacheAttnLaunch &p, int row, int head, int col, const float (&x)[4], int d) {
+  const size_t at = ((size_t)row * p.hq + head) * d + col;
+  if constexpr (BF16) {
+    u32x2 w;
+    w[0] = __builtin_bit_cast(unsigned, bf16x2{(__bf16)x[0], (__bf16)x[1]});
+    w[1] = __builtin_bit_cast(unsigned, bf16x2{(__bf16)x[2], (__bf16)x[3]});
+    *reinterpret_cast<u32x2 *>((__bf16 *)p.o + at) = w;
+  } else {
+    *reinterpret_cast<f32x4 *>((float *)p.o + at) = f32x4{x[0], x[1], x[2], x[3]};
+  }
+}
+
+// K and V of one page of one head, in operand layout
+template <int D>
+struct Frags {
+  u32x4 k[4][D / 64];  // [key block][64 features]: 16 features of one key per lane
+  u32x4 v[D / 16];     // [16 features]: 16 keys of one feature per lane
+  float ks, vs;
+};
+
+template <bool BF16, int D>
+__global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(const CacheAttnLaunch p) {
+  constexpr int T = BF16 ? 1 : 3, DS = D / 32, DB = D / 16;
+  __shared__ float sh_o[kWaves][kRows][D + 4];
+  __shared__ float sh_m[kWaves][kRows], sh_l[kWaves][kRows];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n16 = lane & 15, quad = lane >> 4;
+  const int blk = blockIdx.x % p.blocks, rest = blockIdx.x / p.blocks;
+  const int h = rest % p.c.hkv, split = rest / p.c.hkv;
+  const Request r = find_request(p, blk);
+  const int pages = (r.L + kPage - 1) / kPage;
+  const int pg0 = split * p.split_pages;
+  if (split > 0 && pg0 >= pages) return;  // no keys here: the join leaves this split out
+  const int total = r.n * p.group;
+  const int idx = r.block * kRows + n16;      // this lane's (row, head) pair
+  const int idc = min(idx, total - 1);        // pairs past the end repeat the last one
+  const int row = idc / p.group, head = h * p.group + idc % p.group;
+  const int limit = row_limit(p, r, row);
+  // Q as the B operand: lane n16, features 64 c + 16 quad + 8 (step % 2) .. + 7 of step 2 c + step % 2
+  bf16x8 qf[T][DS];
+  {
+    const size_t at = ((size_t)(r.row0 + row) * p.hq + head) * D;
+#pragma unroll
+    for (int ds = 0; ds < DS; ++ds) {
+      const int f = (ds >> 1) * 64 + quad * 16 + (ds & 1) * 8;
+      if constexpr (BF16) {
+        qf[0][ds] = *reinterpret_cast<const bf16x8 *>((const __bf16 *)p.q + at + f);
+      } else {
+        const f32x4 a = *reinterpret_cast<const f32x4 *>((const float *)p.q + at + f);
+        const f32x4 c = *reinterpret_cast<const f32x4 *>((const float *)p.q + at + f + 4);
+        const float x[8] = {a[0], a[1], a[2], a[3], c[0], c[1], c[2], c[3]};
+        bf16x8 part[T];
+        split_terms<T>(x, part);
+#pragma unroll
+        for (int j = 0; j < T; ++j) qf[j][ds] = part[j];
+      }
+    }
+  }
+  // range of limits over the block's rows
+  int lim_hi = limit, lim_lo = limit;
+#pragma unroll
+  for (int m = 8; m; m >>= 1) {
+    lim_hi = max(lim_hi, __shfl_xor(lim_hi, m));
+    lim_lo = min(lim_lo, __shfl_xor(lim_lo, m));
+  }
+  lim_hi = __builtin_amdgcn_readfirstlane(lim_hi);
+  lim_lo = __builtin_amdgcn_readfirstlane(lim_lo);
+  const int pg1 = min(min(pg0 + p.split_pages, pages), (lim_hi >> 6) + 1);  // lim_hi < 0: none
+
+  f32x4 o[DB] = {};
+  float m_run = -INFINITY, l_run = 0.f;
+
+  // the page ids of this wave, 64 at a time in the lanes
+  int ids = -1, ids_at = -1;
+  auto page_id = [&](int i) {  // i-th page of this wave, pg0 + wave + 4 i
+    if (ids_at < 0 || i >= ids_at + 64) {
+      ids_at = i;
+      const int pg = pg0 + wave + 4 * (i + lane);
+      ids = pg < pg1 ? r.pages[pg] : -1;
+    }
+    return __builtin_amdgcn_readlane(ids, i - ids_at);
+  };
+  // first page from the i-th on that is there; -1 if none
+  int id_next = -1;
+  auto next_page = [&](int i) {
+    for (; pg0 + wave + 4 * i < pg1; ++i) {
+      id_next = page_id(i);
+      if ((unsigned)id_next < (unsigned)p.c.n_pages) return i;
+    }
+    return -1;
+  };
+  auto load = [&](Frags<D> &f, int id) {
+    const size_t at = (size_t)id * p.c.hkv + h;
+    const unsigned char *kp = p.c.k + at * (kPage * D), *vp = p.c.v + at * (kPage * D);
+    const int krow = (n16 >> 2) * 16 + (n16 & 3);
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c)
+        f.k[t][c] = *reinterpret_cast<const u32x4 *>(kp + (krow + t * 4) * D + c * 64 + quad * 16);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) f.v[db] = *reinterpret_cast<const u32x4 *>(vp + (db * 16 + n16) * kPage + quad * 16);
+    f.ks = p.c.k_scale[at];
+    f.vs = p.c.v_scale[at];
+  };
+  auto work = [&](Frags<D> &f, int pg) {
+    f32x4 s[4] = {};
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int ds = 0; ds < DS; ++ds) {
+        const bf16x8 a = widen(f.k[t][ds >> 1][(ds & 1) * 2], f.k[t][ds >> 1][(ds & 1) * 2 + 1], f.ks);
+#pragma unroll
+        for (int j = T - 1; j >= 0; --j) s[t] = mfma(a, qf[j][ds], s[t]);  // small terms first
+      }
+    const int key0 = pg * kPage + quad * 16;  // s[t][i]: key0 + 4 t + i
+    if (pg * kPage + kPage - 1 > lim_lo) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (key0 + 4 * t + i > limit) s[t][i] = -INFINITY;
+      // keys that no row of the block sees may hold NaN codes: their values become 0
+      if (pg * kPage + kPage - 1 > lim_hi) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int left = lim_hi + 1 - (key0 + 4 * t);
+          const unsigned keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << 8 * left) - 1;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) f.v[db][t] &= keep;
+        }
+      }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[t][i]);
+    const float m_new = fmaxf(m_run, row_max(mx) * p.scale_log2);
+    if (__ballot(m_new > m_run)) {
+      const float alpha = m_new > m_run ? exp2_(m_run - m_new) : 1.f;
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[db] *= alpha;
+      m_run = m_new;
+    }
+    const float ref = m_run == -INFINITY ? 0.f : m_run;  // a row that has seen no key
+    float e[2][8];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        e[t >> 1][(t & 1) * 4 + i] = exp2_(__builtin_fmaf(s[t][i], p.scale_log2, -ref));
+        l_run += e[t >> 1][(t & 1) * 4 + i];
+      }
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      bf16x8 pf[T];
+      split_terms<T>(e[ks], pf);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const bf16x8 a = widen(f.v[db][2 * ks], f.v[db][2 * ks + 1], f.vs);
+#pragma unroll
+        for (int j = T - 1; j >= 0; --j) o[db] = mfma(a, pf[j], o[db]);
+      }
+    }
+  };
+
+  Frags<D> fa, fb;
+  int i = next_page(0);
+  if (i >= 0) load(fa, id_next);
+  while (i >= 0) {
+    int i2 = next_page(i + 1);
+    if (i2 >= 0) load(fb, id_next);
+    work(fa, pg0 + wave + 4 * i);
+    if (i2 < 0) break;
+    i = next_page(i2 + 1);
+    if (i >= 0) load(fa, id_next);
+    work(fb, pg0 + wave + 4 * i2);
+  }
+
+  // join the waves
+  l_run = row_sum(l_run);
+  if (quad == 0) sh_m[wave][n16] = m_run, sh_l[wave][n16] = l_run;
+#pragma unroll
+  for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4 *>(&sh_o[wave][n16][db * 16 + quad * 4]) = o[db];
+  __syncthreads();
+  const int rr = threadIdx.x >> 4, c0 = threadIdx.x & 15;  // 16 lanes per pair
+  const int out = r.block * kRows + rr;
+  if (out >= total) return;
+  const int orow = r.row0 + out / p.group, ohead = h * p.group + out % p.group;
+  float m = sh_m[0][rr], w[kWaves], l = 0.f;
+#pragma unroll
+  for (int k = 1; k < kWaves; ++k) m = fmaxf(m, sh_m[k][rr]);
+#pragma unroll
+  for (int k = 0; k < kWaves; ++k) {
+    w[k] = sh_m[k][rr] == -INFINITY ? 0.f : exp2_(sh_m[k][rr] - m);
+    l += w[k] * sh_l[k][rr];
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const float lse = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+#pragma unroll
+  for (int c = c0 * 4; c < D; c += 64) {
+    float x[4] = {};
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+      const f32x4 v = *reinterpret_cast<const f32x4 *>(&sh_o[k][rr][c]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(w[k], v[e], x[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] *= inv;
+    if (p.n_splits == 1)
+      store_out<BF16>(p, orow, ohead, c, x, D);
+    else
+      *reinterpret_cast<f32x4 *>(p.part_o + (((size_t)orow * p.hq + ohead) * p.n_splits + split) * D + c) =
+          f32x4{x[0], x[1], x[2], x[3]};
+  }
+  if (c0 == 0) {
+    if (p.n_splits > 1) p.part_lse[((size_t)orow * p.hq + ohead) * p.n_splits + split] = lse;
+    else if (p.lse) p.lse[(size_t)ohead * p.lse_stride + orow] = lse;
+  }
+}
+
+// Join the splits of one (row, head): o = sum_s e^(lse_s - lse) o_s. Eight groups of
+// 32 lanes take the splits in turn.
+template <bool BF16, int D>
+__global__ __launch_bounds__(kThreads) void cache_join_kernel(const CacheAttnLaunch p) {
+  constexpr int LP = D / 4, GROUPS = kThreads / LP;  // lanes per partial row
+  __shared__ f32x4 sh_o[GROUPS][LP];
+  __shared__ float sh_m[kWaves], sh_l[kWaves];
+  const int t = threadIdx.x, g = t / LP, c = t % LP;
+  const int row = blockIdx.x / p.hq, head = blockIdx.x % p.hq;
+  int b = 0;
+  for (int step = kMaxCacheReqs / 2; step; step >>= 1)
+    if (b + step < p.n_req && p.cu[b + step] <= row) b += step;
+  const int seq = p.seq ? p.seq[b] : b;
+  const int L = min(seq_len(p.c.len, p.c.n_seqs, p.c.max_seq_pages, seq), p.max_len);
+  const int pages = (L + kPage - 1) / kPage;
+  const int n = max(1, (pages + p.split_pages - 1) / p.split_pages);  // splits that hold keys
+  const float *lses = p.part_lse + (size_t)blockIdx.x * p.n_splits;
+  const float *po = p.part_o + (size_t)blockIdx.x * p.n_splits * D;
+  float m = -INFINITY;
+  for (int s = t; s < n; s += kThreads) m = fmaxf(m, lses[s]);
+#pragma unroll
+  for (int k = 32; k; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+  if ((t & 63) == 0) sh_m[t >> 6] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(sh_m[0], sh_m[1]), fmaxf(sh_m[2], sh_m[3]));
+  const float ref = m == -INFINITY ? 0.f : m;
+  float l = 0.f;
+  for (int s = t; s < n; s += kThreads) l += __expf(lses[s] - ref);
+#pragma unroll
+  for (int k = 32; k; k >>= 1) l += __shfl_xor(l, k);
+  if ((t & 63) == 0) sh_l[t >> 6] = l;
+  f32x4 x = {};
+#pragma unroll 4
+  for (int s = g; s < n; s += GROUPS) x += __expf(lses[s] - ref) * *reinterpret_cast<const f32x4 *>(po + (size_t)s * D + c * 4);
+  sh_o[g][c] = x;
+  __syncthreads();
+  if (g) return;
+#pragma unroll
+  for (int k = 1; k < GROUPS; ++k) x += sh_o[k][c];
+  l = (sh_l[0] + sh_l[1]) + (sh_l[2] + sh_l[3]);
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const float y[4] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
+  store_out<BF16>(p, row, head, c * 4, y, D);
+  if (c == 0 && p.lse) p.lse[(size_t)head * p.lse_stride + row] = l > 0.f ? m + __logf(l) : -INFINITY;
+}
+
+template <bool BF16, int D>
+hipError_t launch(const CacheAttnLaunch &p, hipStream_t st) {
+  const int rows = p.cu[p.n_req];
+  cache_attn_kernel<BF16, D><<<p.blocks * p.c.hkv * p.n_splits, kThreads, 0, st>>>(p);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && p.n_splits > 1) {
+    cache_join_kernel<BF16, D><<<rows * p.hq, kThreads, 0, st>>>(p);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+}  // namespace
+
+hipError_t launch_cache_attn(bool bf16, const CacheAttnLaunch &p, hipStream_t st) {
+  if (p.c.d == 128) return bf16 ? launch<true, 128>(p, st) : launch<false, 128>(p, st);
+  return bf16 ? launch<true, 64>(p, st) : launch<false, 64>(p, st);
+}
+
+}  // namespace daf

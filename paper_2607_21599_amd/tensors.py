@@ -11,7 +11,7 @@ from __future__ import annotations
 import numpy as np
 import torch
 
-from . import (DAF_BF16, DAF_F32, DAF_FUSE_HIDDEN, DAF_FUSE_KV, DAF_SRC_TOKENS, AttnCfg, Batch,
+from . import (DAF_BF16, DAF_F32, DAF_FUSE_HIDDEN, DAF_FUSE_KV, DAF_PAGE_TOKENS, DAF_SRC_TOKENS, AttnCfg, Batch,
                daf_fuse, daf_gather_important, daf_imp_self_attn, daf_layer_attn,
                daf_layer_workspace_size, daf_position_attn, daf_qdoc_attn, daf_qdoc_workspace_size)
 
@@ -126,3 +126,19 @@ class LayerBuffers:
         n = t["q_full"].shape[0]
         daf_position_attn(self.cfg, n, n, t["q_full"], None, t["k_cache"], t["v_cache"], t["o_full"],
                           t["lse_full"], stream)
+
+
+def cache_tensors(n_layers: int, n_pages: int, n_kv_heads: int, head_dim: int, n_seqs: int, max_seq_pages: int,
+                  device="cuda") -> dict:
+    """The tensors of an empty paged 8-bit cache, for ``Cache.from_tensors``. The
+    codes and scales need no values; nothing reads them before they are written."""
+    def empty(*shape, dtype):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+    pool = (n_layers, n_pages, n_kv_heads)
+    return {"k": empty(*pool, DAF_PAGE_TOKENS, head_dim, dtype=torch.float8_e4m3fn),
+            "v": empty(*pool, head_dim, DAF_PAGE_TOKENS, dtype=torch.float8_e4m3fn),
+            "k_scale": empty(*pool, dtype=torch.float32), "v_scale": empty(*pool, dtype=torch.float32),
+            "table": torch.full((n_seqs, max_seq_pages), -1, dtype=torch.int32, device=device),
+            "len": torch.zeros(n_seqs, dtype=torch.int32, device=device),
+            "refs": torch.zeros(n_pages, dtype=torch.int32, device=device)}

@@ -1,0 +1,360 @@
+"""GPU: the paged 8-bit K/V cache against oracle/cache.py (64 bits)."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    assert torch.cuda.is_available(), "GPU tests need a ROCm GPU"
+    import paper_2607_21599_amd as daf
+    daf.lib()
+    yield
+    torch.cuda.synchronize()
+
+
+def _pair(**kw):
+    from cache_pair import Pair
+    return Pair(**kw)
+
+
+def _rows(rng, n, heads, d, size=1.0):
+    x = rng.standard_normal((n, heads, d)) * size
+    x *= np.exp2(rng.integers(-3, 4, (n, 1, 1)))  # rows of other sizes, so that scales differ and grow
+    return torch.from_numpy(x).float()
+
+
+def _cu(n):
+    return [0] + np.cumsum(n).tolist()
+
+
+def _fill(p, rng, seq, lens, layers=1, size=1.0):
+    """Sequences of the given lengths with random K/V in every layer."""
+    assert p.extend(seq, lens) == 0
+    cu = _cu(lens)
+    for la in range(layers):
+        p.write(la, cu, seq, _rows(rng, cu[-1], p.heads, p.d, size), _rows(rng, cu[-1], p.heads, p.d, size))
+
+
+# ---- rows ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,d,heads", [(BF16, 128, 4), (BF16, 64, 1), (F32, 64, 3), (F32, 128, 2)])
+def test_appends_of_every_length(dtype, d, heads):
+    """Runs that start and end anywhere in a page, on ragged sequences at once, with
+    scales that grow while earlier tokens of the page stay."""
+    p = _pair(layers=2, pages=40, heads=heads, d=d, n_seqs=5, max_seq_pages=10, dtype=dtype)
+    rng = np.random.default_rng(d + heads)
+    seq = [3, 0, 4]
+    for step, n in enumerate([(1, 63, 0), (64, 1, 129), (0, 65, 7), (200, 2, 1), (1, 1, 1), (61, 0, 130)]):
+        assert p.extend(seq, n) == 0
+        cu = _cu(n)
+        for la in (1, 0):
+            p.write(la, cu, seq, _rows(rng, cu[-1], heads, d, 2.0 ** step), _rows(rng, cu[-1], heads, d, 0.5 ** step))
+        p.same()
+    lens = [int(p.o.len[s]) for s in seq]
+    for la in (0, 1):
+        p.read(la, _cu(lens), seq)
+    p.read(1, _cu([lens[0] + 70, 1, 0]), seq)  # more rows than tokens: zeros before the first
+    p.read(0, [0, 4], [3], [-3, 0, 64, 10_000])  # positions outside: zeros
+
+
+@pytest.mark.parametrize("dtype,d,heads", [(BF16, 128, 2), (BF16, 64, 3), (F32, 64, 1), (F32, 128, 3)])
+@pytest.mark.parametrize("share", [0.02, 0.15, 1.0])
+def test_rows_at_positions(dtype, d, heads, share):
+    """The hybrid cache: recomputed rows over the stored ones, also whole pages."""
+    p = _pair(pages=24, heads=heads, d=d, n_seqs=3, max_seq_pages=9, dtype=dtype)
+    rng = np.random.default_rng(int(share * 100) + d)
+    seq, lens = [2, 0], [517, 300]
+    _fill(p, rng, seq, lens)
+    for size in (0.1, 1.0, 30.0):
+        pos = [np.sort(rng.choice(n, max(1, int(n * share)), replace=False)) for n in lens]
+        cu = _cu([len(x) for x in pos])
+        pos = np.concatenate(pos)
+        p.write(0, cu, seq, _rows(rng, cu[-1], heads, d, size), _rows(rng, cu[-1], heads, d, size), pos)
+        p.same()
+        p.read(0, cu, seq, pos)
+    p.read(0, _cu(lens), seq)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_values_at_the_borders(dtype):
+    """Zeros, subnormal codes, ties, the largest and smallest scales, infinities, NaN;
+    positions that are left out; a page that loses every token but keeps its place."""
+    p = _pair(pages=6, heads=1, d=64, n_seqs=2, max_seq_pages=3, dtype=dtype)
+    assert p.extend([0, 1], [100, 30]) == 0
+    line = torch.zeros(64)
+    rows = [line.clone() for _ in range(30)]
+    rows[0][:8] = torch.tensor([448.0, 1.0, 0.0078125, 0.001953125, 0.0009765625, 17.0, 19.0, -0.0])
+    rows[1][:4] = torch.tensor([449.0, -449.0, 432.0, 464.0])
+    rows[2][0], rows[3][0] = 2.0 ** -110, -2.0 ** -101
+    p.write(0, [0, 30], [1], torch.stack(rows)[:, None], torch.stack(rows[::-1])[:, None])
+    p.same()
+    top = float(torch.finfo(dtype).max)
+    for value in (top, 2.0 ** -100, float("inf"), -float("inf"), float("nan"), 0.0):
+        x = torch.full((2, 1, 64), value)
+        x[1, 0, ::2] = 1e-3
+        p.write(0, [0, 2], [0], x, -x, [3, 64])
+        p.same()
+    p.read(0, [0, 100], [0])
+    # 64 .. 99 written as a whole: the present scale does not count
+    x = torch.full((36, 1, 64), 0.25)
+    p.write(0, [0, 36], [0], x, x, list(range(64, 100)))
+    p.same()
+    assert float(p.t["k_scale"][0, p.t["table"][0, 1], 0]) == 2.0 ** -10
+    # left out: before the first token and at len and past it
+    p.write(0, [0, 4], [0], torch.ones(4, 1, 64), torch.ones(4, 1, 64), [-1, 5, 100, 130])
+    p.same()
+
+
+def test_rows_of_pages_that_are_not_there():
+    """A table entry outside the pool and a sequence outside the table: nothing is
+    written, zeros are read."""
+    p = _pair(pages=8, heads=2, d=64, n_seqs=2, max_seq_pages=4)
+    rng = np.random.default_rng(1)
+    _fill(p, rng, [0], [200])
+    for bad in (-1, 8, 2 ** 31 - 1, -2 ** 31):
+        p.t["table"][0, 1] = bad
+        p.o.table[0, 1] = bad
+        p.write(0, [0, 150], [0], _rows(rng, 150, 2, 64), _rows(rng, 150, 2, 64))
+        p.same()
+        k, _ = p.read(0, [0, 200], [0])
+        assert not k[64:128].any() and k[128:].any()
+    import paper_2607_21599_amd as daf
+    from cache_pair import dev
+    x = torch.ones(6, 2, 64, dtype=BF16, device="cuda")
+    for seq in ([2, -1], [2 ** 30, -2 ** 31]):
+        rows = daf.CacheRows([0, 3, 6], dev(seq))
+        daf.daf_cache_write(p.cfg, p.c, 0, rows, x, x)
+        k, v = torch.ones_like(x), torch.ones_like(x)
+        daf.daf_cache_read(p.cfg, p.c, 0, rows, k, v)
+        assert not k.any() and not v.any()
+    p.same()
+
+
+def test_read_of_one_tensor_and_without_lists():
+    import paper_2607_21599_amd as daf
+    p = _pair(pages=8, heads=2, d=128, n_seqs=2, max_seq_pages=4, dtype=F32)
+    rng = np.random.default_rng(2)
+    _fill(p, rng, [0, 1], [130, 64])
+    k, v = p.read(0, [0, 130, 194], [0, 1])
+    rows = daf.CacheRows([0, 130, 194])  # request b is sequence b
+    for name, want in (("k", k), ("v", v)):
+        got = torch.zeros_like(want)
+        daf.daf_cache_read(p.cfg, p.c, 0, rows, got if name == "k" else None, got if name == "v" else None)
+        assert torch.equal(got, want)
+
+
+def test_more_requests_than_a_launch_takes():
+    """600 requests of 0 to 3 rows: their prefix sums go in several launches."""
+    n = 600
+    p = _pair(pages=n + 4, heads=1, d=64, n_seqs=n, max_seq_pages=2, hq=3)
+    rng = np.random.default_rng(3)
+    seq = rng.permutation(n).tolist()
+    lens = rng.integers(1, 100, n).tolist()
+    assert p.extend(seq, [min(x, 64) for x in lens]) == 0
+    lens = [min(x, 64) for x in lens]
+    p.write(0, _cu(lens), seq, _rows(rng, sum(lens), 1, 64), _rows(rng, sum(lens), 1, 64))
+    p.same()
+    few = [min(int(x), y) for x, y in zip(rng.integers(0, 4, n), lens)]
+    p.read(0, _cu(few), seq)
+    q = torch.from_numpy(rng.standard_normal((sum(few), 3, 64))).float()
+    p.check_attn(0, _cu(few), seq, q)
+    o, lse = p.check_attn(0, _cu(few), None, q)  # request b is sequence b, past the first launch too
+
+
+# ---- attention ------------------------------------------------------------------------
+SHAPES = [(BF16, 128, 4, 28), (BF16, 64, 1, 4), (BF16, 128, 2, 2), (BF16, 64, 2, 34), (F32, 64, 1, 4), (F32, 128, 2, 14)]
+
+
+@pytest.mark.parametrize("dtype,d,heads,hq", SHAPES)
+def test_single_rows(dtype, d, heads, hq):
+    """A decode step over sequences of no, one and many tokens."""
+    lens = [0, 1, 63, 64, 65, 200, 1030, 129]
+    p = _pair(layers=2, pages=32, heads=heads, d=d, hq=hq, n_seqs=9, max_seq_pages=20, dtype=dtype)
+    rng = np.random.default_rng(hq)
+    seq = [8, 1, 0, 3, 2, 5, 7, 6]
+    _fill(p, rng, seq, lens, layers=2)
+    q = torch.from_numpy(rng.standard_normal((8, hq, d))).float()
+    for max_len in (1030, 1280):
+        o, lse = p.check_attn(1, list(range(9)), seq, q, max_len=max_len)
+        assert not o[0].any() and torch.isneginf(lse[:, 0]).all()
+    p.check_attn(0, [0, 1], [7], q[:1])
+
+
+@pytest.mark.parametrize("dtype,d,heads,hq", SHAPES)
+def test_question_rows(dtype, d, heads, hq):
+    """Ragged questions, causal at the end of their sequences; one is longer than its
+    sequence, so that its first rows see no key."""
+    lens, n = [700, 5, 64, 300, 129], [33, 9, 64, 1, 70]
+    p = _pair(pages=24, heads=heads, d=d, hq=hq, n_seqs=5, max_seq_pages=12, dtype=dtype)
+    rng = np.random.default_rng(hq + 1)
+    seq = [4, 0, 1, 3, 2]
+    _fill(p, rng, seq, lens)
+    q = torch.from_numpy(rng.standard_normal((sum(n), hq, d))).float()
+    o, lse = p.check_attn(0, _cu(n), seq, q)
+    assert torch.isneginf(lse[:, 33:37]).all() and not o[33:37].any() and not torch.isneginf(lse[:, 37]).any()
+
+
+@pytest.mark.parametrize("dtype,d,heads,hq", SHAPES)
+def test_rows_at_given_positions(dtype, d, heads, hq):
+    """Positions in any order, before the first token and past the last one."""
+    p = _pair(pages=24, heads=heads, d=d, hq=hq, n_seqs=2, max_seq_pages=12, dtype=dtype)
+    rng = np.random.default_rng(hq + 2)
+    _fill(p, rng, [0, 1], [650, 90])
+    pos = [-1, 649, 0, 63, 64, 5000, 127, 128, 300, 20, -2 ** 31, 89, 2 ** 31 - 1]
+    q = torch.from_numpy(rng.standard_normal((len(pos), hq, d))).float()
+    p.check_attn(0, [0, 9, 13], [0, 1], q, pos)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_long_sequence_in_splits_and_in_one(dtype):
+    """20000 keys: split over workgroups for one row; and in one piece, past 64 pages per
+    wave, where there are enough rows to fill the device."""
+    p = _pair(pages=340, heads=1, d=64, hq=8, n_seqs=1, max_seq_pages=320, dtype=dtype)
+    rng = np.random.default_rng(5)
+    _fill(p, rng, [0], [20000])
+    q = torch.from_numpy(rng.standard_normal((1040, 8, 64))).float()
+    p.check_attn(0, [0, 1], [0], q[:1])
+    q = q.to(dtype)
+    o, lse = p.attn(0, [0, 1040], [0], q.cuda())
+    some = [0, 1, 500, 1038, 1039]  # those that the plain form is asked for
+    p.within_bounds(o[some], lse[:, some], 0, [0, 5], [0], q[some], [20000 - 1040 + j for j in some])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_large_scores_and_rising_maxima(dtype):
+    """Scores that rise from key to key by far more than an exponent's range."""
+    p = _pair(pages=12, heads=1, d=64, hq=2, n_seqs=1, max_seq_pages=10, dtype=dtype)
+    n = 600
+    assert p.extend([0], [n]) == 0
+    rng = np.random.default_rng(6)
+    k = torch.zeros(n, 1, 64)
+    k[:, 0, 0] = torch.linspace(-3000, 3000, n)
+    k[:, 0, 1] = torch.from_numpy(rng.standard_normal(n)).float()
+    v = torch.from_numpy(rng.standard_normal((n, 1, 64))).float()
+    p.write(0, [0, n], [0], k, v)
+    q = torch.zeros(4, 2, 64)
+    q[:, 0, 0], q[:, 1, 0] = 8.0, -8.0
+    q[2:, :, 0] = 0
+    q[:, :, 1] = 1.0
+    p.check_attn(0, [0, 4], [0], q, [599, 300, 599, 10])
+
+
+def test_what_no_row_sees_may_be_nan():
+    """NaN codes past len, past the largest position of the rows, and in free pages."""
+    p = _pair(pages=12, heads=2, d=128, hq=14, n_seqs=2, max_seq_pages=6)
+    rng = np.random.default_rng(7)
+    p.t["k"].view(torch.uint8).fill_(0x7F)  # NaN everywhere that no row is written
+    p.t["v"].view(torch.uint8).fill_(0xFF)
+    for n in "kv":
+        p.o.code[n][:] = np.nan
+    _fill(p, rng, [0, 1], [200, 65])
+    q = torch.from_numpy(rng.standard_normal((4, 14, 128))).float()
+    for n in ("k", "v"):  # slots past len in the last pages too
+        p.t[n].view(torch.uint8)[0, p.t["table"][0, 3].item(), :, 8:] = 0x7F if n == "k" else 0
+    vp = p.t["v"].view(torch.uint8)[0, p.t["table"][0, 3].item()]
+    vp.zero_()
+    for n in "kv":
+        p.o.code[n][0, p.o.table[0, 3], :, 8:] = 0
+        if n == "v":
+            p.o.code[n][0, p.o.table[0, 3]] = 0
+    vp[:, :, 8:] = 0x7F
+    p.check_attn(0, [0, 3, 4], [0, 1], q)
+    p.check_attn(0, [0, 3, 4], [0, 1], q, [10, 70, 130, 64])
+
+
+def test_pages_that_are_not_there_hold_no_keys():
+    p = _pair(pages=12, heads=2, d=64, hq=6, n_seqs=2, max_seq_pages=10)
+    rng = np.random.default_rng(8)
+    _fill(p, rng, [0, 1], [400, 130])
+    q = torch.from_numpy(rng.standard_normal((5, 6, 64))).float()
+    for gone in ([0], [1, 3], [0, 1, 2, 3, 4, 5], [6], list(range(7))):
+        keep = p.o.table.copy()
+        for i in gone:
+            p.o.table[0, i] = -1 if i % 2 else 2 ** 31 - 1
+        p.t["table"].copy_(torch.from_numpy(p.o.table).int())
+        o, lse = p.check_attn(0, [0, 4, 5], [0, 1], q)
+        if len(gone) == 7:
+            assert not o[:4].any() and torch.isneginf(lse[:, :4]).all()
+        p.o.table[:] = keep
+        p.t["table"].copy_(torch.from_numpy(p.o.table).int())
+    # sequences outside the table have no keys; lengths beyond it count as far as it reaches
+    import paper_2607_21599_amd as daf
+    from cache_pair import dev
+    o, lse = p.attn(0, [0, 2, 5], [2, -7], q.to(BF16).cuda())
+    assert not o.any() and torch.isneginf(lse).all()
+    p.t["len"][0] = 2 ** 31 - 1
+    p.o.len[0] = 640
+    p.check_attn(0, [0, 5], [0], q)
+    p.t["len"][0] = -5
+    o, lse = p.attn(0, [0, 5], [0], q.to(BF16).cuda())
+    assert not o.any() and torch.isneginf(lse).all()
+
+
+def test_no_lse_and_untouched_neighbours():
+    """Without an LSE; rows of the output buffer that belong to nobody stay."""
+    import paper_2607_21599_amd as daf
+    from cache_pair import dev
+    p = _pair(pages=70, heads=2, d=64, hq=6, n_seqs=1, max_seq_pages=64)
+    rng = np.random.default_rng(9)
+    _fill(p, rng, [0], [4000])
+    q = torch.from_numpy(rng.standard_normal((3, 6, 64))).to(BF16).cuda()
+    want, _ = p.attn(0, [0, 3], [0], q)
+    rows = daf.CacheRows([0, 3], dev([0]))
+    size = daf.daf_cache_attn_workspace_size(p.cfg, p.c, rows, 4096)
+    assert size > 0
+    ws = torch.full((size + 64,), 0x55, dtype=torch.uint8, device="cuda")
+    o = torch.full((6, 6, 64), 9.0, dtype=BF16, device="cuda")
+    daf.daf_cache_attn(p.cfg, p.c, 0, rows, 4096, q, o, None, ws, size)
+    assert torch.equal(o[:3], want) and (o[3:] == 9).all() and (ws[size:] == 0x55).all()
+
+
+def test_offsets_past_32_bits():
+    """A pool whose K and V each pass 4 GiB, with the sequences in its last pages."""
+    heads, d, pages = 16, 128, 34000
+    from cache_pair import dev
+    import paper_2607_21599_amd as daf
+    from paper_2607_21599_amd.tensors import cache_tensors
+    t = cache_tensors(1, pages, heads, d, 2, 4)
+    big = daf.Cache.from_tensors(t)
+    assert t["k"].numel() > 2 ** 32
+    t["refs"][:pages - 7] = 1
+    small = _pair(pages=7, heads=heads, d=d, hq=16, n_seqs=2, max_seq_pages=4)
+    rng = np.random.default_rng(10)
+    k, v = _rows(rng, 330, heads, d).to(BF16).cuda(), _rows(rng, 330, heads, d).to(BF16).cuda()
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    rows = daf.CacheRows([0, 200, 330])
+    q = torch.from_numpy(rng.standard_normal((330, 16, d))).to(BF16).cuda()
+    out = []
+    for c, tt in ((big, t), (small.c, small.t)):
+        daf.daf_pages_extend(c, 2, None, dev([200, 130]), st)
+        assert int(st) == 0
+        daf.daf_cache_write(small.cfg, c, 0, rows, k, v)
+        kk, vv, o = torch.zeros_like(k), torch.zeros_like(v), torch.zeros_like(q)
+        daf.daf_cache_read(small.cfg, c, 0, rows, kk, vv)
+        size = daf.daf_cache_attn_workspace_size(small.cfg, c, rows, 256)
+        ws = torch.empty(max(size, 16), dtype=torch.uint8, device="cuda")
+        daf.daf_cache_attn(small.cfg, c, 0, rows, 256, q, o, None, ws, size)
+        # copies up there as well: the second sequence's first page over a page of nobody
+        out.append((kk, vv, o))
+    assert (t["table"][0, :4] - small.t["table"][0, :4] == pages - 7).all()
+    for a, b in zip(*out):
+        assert torch.equal(a, b)
+    t["k"].view(torch.uint8)[:, 5] = 1
+    daf.daf_pages_copy(big, 1, dev([pages - 7]), dev([5]))
+    for n in ("k", "v"):
+        x = t[n].view(torch.uint8)
+        assert torch.equal(x[:, 5], x[:, pages - 7])
+    ws_size = daf.daf_pages_workspace_size(big)
+    ws = torch.empty(ws_size, dtype=torch.uint8, device="cuda")
+    t["refs"][100:200] = 0
+    daf.daf_pages_compact(big, st, ws, ws_size)
+    assert int(st) == pages - 100 and int(t["refs"][:pages - 100].min()) == 1 and not t["refs"][pages - 100:].any()
+    assert int(t["table"].max()) < pages - 100
+    daf.daf_cache_read(small.cfg, big, 0, rows, kk, vv)
+    assert torch.equal(kk, out[0][0]) and torch.equal(vv, out[0][1])
