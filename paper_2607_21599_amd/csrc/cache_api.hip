@@ -176,7 +176,7 @@ daf_status_t store(bool write, const daf_attn_cfg_t *cfg, const daf_cache_t *c, 
       p.c = view(c, layer);
       p.n_req = std::min(kMaxCacheReqs, rows->n - b0);
       p.units = fill(rows, b0, p.n_req, p.cu, p.unit0, &p.per_req, units_of);
-      if (p.units < 0 || (int64_t)p.units * c->n_kv_heads > INT32_MAX)
+      if (p.units < 0 || (int64_t)p.units * c->n_kv_heads > INT32_MAX / 2)
         return fail(DAF_ERR_UNSUPPORTED, "%d rows of %d heads are too many for one call", total, c->n_kv_heads);
       if (pass == 0 || p.units == 0) continue;
       const int64_t row0 = rows->cu[b0];

@@ -6,11 +6,11 @@
 // value for normal codes), and where a later row raises s the codes that stay
 // change only if they leave the normal range.
 //
-// A workgroup owns one page of one head, so that the page's maxima, its scale and
-// the 64-byte lines of the transposed V (64 tokens of one feature) have one
-// writer. K rows go 16 bytes of input per lane; for V a lane takes two features and
-// 16 (D = 64: 8) consecutive slots, so that its transposed bytes are whole 16-byte
-// pieces without a pass through LDS. Both are loaded before the maxima are taken.
+// A workgroup owns K or V of one page of one head, so that the page's maximum, its
+// scale and the 64-byte lines of the transposed V (64 tokens of one feature) have
+// one writer. K goes 8 elements per lane; for V a lane takes two features of 16
+// (D = 64: 8) consecutive slots, so that its transposed codes are whole pieces
+// without a pass through LDS. All rows are loaded before the maximum is taken.
 // Bound by HBM for long runs of rows, by latency for a few.
 #include "cache.h"
 
@@ -19,69 +19,71 @@ namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 
-// Elements of one dtype: E of them as 32-bit words in memory.
+// Rows of one dtype, held as they are in memory until they are converted: N elements
+// in words() 32-bit words.
 template <bool BF16>
-struct Elem;
-template <>
-struct Elem<true> {
-  static constexpr int kBytes = 2;
-  static constexpr float kMax = 3.38953139e38f;  // 0x7f7f
+struct Elem {
+  static constexpr int kBytes = BF16 ? 2 : 4;
+  static constexpr float kMax = BF16 ? 3.38953139e38f : 3.402823466e38f;  // largest finite value
+  static constexpr int words(int n) { return n * kBytes / 4; }
+  // N * kBytes bytes at p, which is aligned to them or to 16
   template <int N>
-  static __device__ __forceinline__ void load(const unsigned char *p, float (&x)[N]) {
-    unsigned w[N / 2];
-    if constexpr (N == 8) {
-      const u32x4 v = *reinterpret_cast<const u32x4 *>(p);
+  static __device__ __forceinline__ void load(const unsigned char *p, unsigned (&w)[words(N)]) {
+    constexpr int W = words(N);
+    if constexpr (W >= 4) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = v[i];
+      for (int i = 0; i < W / 4; ++i) {
+        const u32x4 v = reinterpret_cast<const u32x4 *>(p)[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
+      }
+    } else if constexpr (W == 2) {
+      const u32x2 v = *reinterpret_cast<const u32x2 *>(p);
+      w[0] = v[0], w[1] = v[1];
     } else {
       w[0] = *reinterpret_cast<const unsigned *>(p);
     }
-#pragma unroll
-    for (int i = 0; i < N / 2; ++i) {
-      x[2 * i] = __builtin_bit_cast(float, w[i] << 16);
-      x[2 * i + 1] = __builtin_bit_cast(float, w[i] & 0xffff0000u);
-    }
   }
-  // values that bf16 holds exactly (NaN keeps a set mantissa bit of the upper half)
+  // element i; LIMITED: infinities as the largest finite value, NaN as it is
+  template <bool LIMITED, int W>
+  static __device__ __forceinline__ float get(const unsigned (&w)[W], int i) {
+    const unsigned u = !BF16 ? w[i] : i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16;
+    const float x = __builtin_bit_cast(float, u);
+    return !LIMITED ? x : x > kMax ? kMax : x < -kMax ? -kMax : x;
+  }
+  // the larger of m and the magnitudes in w, as bits, per half in bf16
+  static __device__ __forceinline__ unsigned max_bits(unsigned m, unsigned w) {
+    if constexpr (!BF16) return max(m, w & 0x7fffffffu);
+    return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(u16x2, m),
+                                                                  __builtin_bit_cast(u16x2, w & 0x7fff7fffu)));
+  }
+  // the same as the bits of one fp32 value
+  static __device__ __forceinline__ unsigned whole(unsigned m) {
+    return !BF16 ? m : max(m & 0xffff0000u, m << 16);
+  }
+  // values that the dtype holds exactly (a NaN keeps a set mantissa bit)
   template <int N>
   static __device__ __forceinline__ void store(unsigned char *p, const float (&x)[N]) {
-    unsigned w[N / 2];
+    constexpr int W = words(N);
+    unsigned w[W];
 #pragma unroll
-    for (int i = 0; i < N / 2; ++i)
-      w[i] = (__builtin_bit_cast(unsigned, x[2 * i]) >> 16) | (__builtin_bit_cast(unsigned, x[2 * i + 1]) & 0xffff0000u);
-    if constexpr (N == 8)
-      *reinterpret_cast<u32x4 *>(p) = u32x4{w[0], w[1], w[2], w[3]};
-    else
+    for (int i = 0; i < W; ++i)
+      w[i] = !BF16 ? __builtin_bit_cast(unsigned, x[i])
+                   : __builtin_bit_cast(unsigned, x[2 * i]) >> 16 | (__builtin_bit_cast(unsigned, x[2 * i + 1]) & 0xffff0000u);
+    if constexpr (W >= 4) {
+#pragma unroll
+      for (int i = 0; i < W / 4; ++i)
+        reinterpret_cast<u32x4 *>(p)[i] = u32x4{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
+    } else if constexpr (W == 2) {
+      *reinterpret_cast<u32x2 *>(p) = u32x2{w[0], w[1]};
+    } else {
       *reinterpret_cast<unsigned *>(p) = w[0];
-  }
-};
-template <>
-struct Elem<false> {
-  static constexpr int kBytes = 4;
-  static constexpr float kMax = 3.402823466e38f;
-  template <int N>
-  static __device__ __forceinline__ void load(const unsigned char *p, float (&x)[N]) {
-    if constexpr (N == 8) {
-      const f32x4 a = *reinterpret_cast<const f32x4 *>(p), b = *reinterpret_cast<const f32x4 *>(p + 16);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
-    } else {
-      const f32x2 a = *reinterpret_cast<const f32x2 *>(p);
-      x[0] = a[0], x[1] = a[1];
-    }
-  }
-  template <int N>
-  static __device__ __forceinline__ void store(unsigned char *p, const float (&x)[N]) {
-    if constexpr (N == 8) {
-      *reinterpret_cast<f32x4 *>(p) = f32x4{x[0], x[1], x[2], x[3]};
-      *reinterpret_cast<f32x4 *>(p + 16) = f32x4{x[4], x[5], x[6], x[7]};
-    } else {
-      *reinterpret_cast<f32x2 *>(p) = f32x2{x[0], x[1]};
     }
   }
 };
@@ -107,10 +109,6 @@ __device__ __forceinline__ unsigned rescale(unsigned w, float ratio) {
   return to_codes(x[0] * ratio, x[1] * ratio, x[2] * ratio, x[3] * ratio);
 }
 
-__device__ __forceinline__ float limited(float x, float most) {
-  return x > most ? most : x < -most ? -most : x;  // NaN passes
-}
-
 // The smallest power of two >= 2^kMinScaleExp under which top is at most 448 =
 // 1.75 * 2^8; 0 for 0. From the bits of top, so exact.
 __device__ __forceinline__ float scale_for(float top) {
@@ -124,174 +122,199 @@ __device__ __forceinline__ float inverse(float s) {
   return s == 0.f ? 0.f : __builtin_bit_cast(float, (254u << 23) - __builtin_bit_cast(unsigned, s));
 }
 
-__device__ __forceinline__ float wave_max(float x) {
+__device__ __forceinline__ unsigned wave_max(unsigned x) {
 #pragma unroll
-  for (int m = 32; m; m >>= 1) x = fmaxf(x, __shfl_xor(x, m));
+  for (int m = 32; m; m >>= 1) x = max(x, (unsigned)__shfl_xor((int)x, m));
   return x;
 }
 
 struct Shared {
-  int row[kPage];      // per slot: the request's row that lies there, or -1
-  float top[2][4];     // per wave: largest magnitude of K and V
-  float scale[2];      // present scales
+  int row[kPage];  // per slot: the request's row that lies there, or -1
+  unsigned top[2][4];  // per wave: largest magnitude, its bits; the same of finite ones
+  float scale;     // present scale
 };
 
-// One page of one head: the rows in sh.row (set, and a barrier passed). `held`:
-// tokens of the page that the sequence had before (write).
-template <bool BF16, int D, bool WRITE>
-__device__ __forceinline__ void do_page(const StoreLaunch &p, Shared &sh, int64_t row0, int h, int page, int tokens,
-                                        int held) {
+// A lane's share of K or V of a page. A lane has PASSES pieces of N elements of a
+// row. K: 8 features of every SPP-th slot. V: 2 features of PASSES consecutive
+// slots, so that its codes are whole 16-byte (D = 64: 8-byte) pieces of the
+// transposed page, Q words of four.
+template <int D, bool IS_V>
+struct Share {
+  static constexpr int N = IS_V ? 2 : 8, CH = D / 8, SPP = kThreads / CH;
+  static constexpr int PASSES = IS_V ? 16 * D / 128 : kPage / SPP, LPS = kPage / PASSES;
+  static constexpr int Q = IS_V ? PASSES / 4 : 1;
+};
+
+// Codes of the rows in x (those in `mine`; zeros elsewhere) into the page; kept codes
+// stay, times `ratio` where the scale grew.
+template <bool BF16, int D, bool IS_V, bool LIMITED, typename X, typename Old>
+__device__ __forceinline__ void put(const X &x, Old &old, unsigned char *codes, unsigned mine, bool kept, bool grow,
+                                    float inv, float ratio, int slot0, int d0) {
   using E = Elem<BF16>;
-  constexpr int CH = D / 8, SPP = kThreads / CH, PASSES = kPage / SPP;  // K: 8 elements per lane
-  constexpr int LPR = D / 2, SPT = 16 * D / 128;                        // V: 2 features, SPT slots per lane
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  const size_t rowb = (size_t)p.c.hkv * D * E::kBytes;
-  const bool there = (unsigned)page < (unsigned)p.c.n_pages;
-  const size_t blk = there ? (size_t)page * p.c.hkv + h : 0;
-  unsigned char *kp = p.c.k + blk * (kPage * D), *vp = p.c.v + blk * (kPage * D);
-  const int slot0 = wave * 16 + lane / LPR * SPT, d0 = lane % LPR * 2;
-
-  const int mine = sh.row[lane];
-  const unsigned long long asked = __ballot(mine >= 0);
-  // rows that can be moved: below the sequence's tokens, in a page that is there
-  const unsigned long long have = !there ? 0ull : tokens >= 64 ? ~0ull : (1ull << max(tokens, 0)) - 1;
-  const unsigned long long go = asked & have;
-  const unsigned wave_go = (unsigned)(go >> (16 * wave)) & 0xffffu, wave_asked = (unsigned)(asked >> (16 * wave)) & 0xffffu;
-
-  if constexpr (WRITE) {
-    if (!go) return;  // uniform in the workgroup
-    const bool kept = ((held >= 64 ? ~0ull : (1ull << held) - 1) & ~go) != 0;
-    float kx[PASSES][8], vx[SPT][2];
-    float top_k = 0.f, top_v = 0.f;
+  using S = Share<D, IS_V>;
+  if constexpr (!IS_V) {
 #pragma unroll
-    for (int i = 0; i < PASSES; ++i) {
-      const int slot = i * SPP + t / CH;
-      if ((go >> slot) & 1)
-        E::template load<8>((const unsigned char *)p.k + (row0 + sh.row[slot]) * rowb + (size_t)h * D * E::kBytes +
-                                t % CH * 8 * E::kBytes, kx[i]);
-    }
+    for (int i = 0; i < S::PASSES; ++i) {
+      u32x2 *dst = reinterpret_cast<u32x2 *>(codes + (slot0 + i * S::SPP) * D + d0);
+      if (!kept || ((mine >> i) & 1)) {  // zeros where no row goes
+        float y[8];
 #pragma unroll
-    for (int s = 0; s < SPT; ++s)
-      if ((go >> (slot0 + s)) & 1)
-        E::template load<2>((const unsigned char *)p.v + (row0 + sh.row[slot0 + s]) * rowb +
-                                ((size_t)h * D + d0) * E::kBytes, vx[s]);
-    // the V bytes that stay, where this wave's slots take a new row
-    unsigned old_v[2][SPT / 4];
-    const bool merge = kept && wave_go;
-    auto load_old = [&] {
-#pragma unroll
-      for (int f = 0; f < 2; ++f)
-#pragma unroll
-        for (int j = 0; j < SPT / 4; ++j)
-          old_v[f][j] = reinterpret_cast<const unsigned *>(vp + (d0 + f) * kPage + slot0)[j];
-    };
-    if (merge) load_old();
-#pragma unroll
-    for (int i = 0; i < PASSES; ++i) {
-      const int slot = i * SPP + t / CH;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        kx[i][j] = (go >> slot) & 1 ? limited(kx[i][j], E::kMax) : 0.f;
-        top_k = fmaxf(top_k, fabsf(kx[i][j]));
-      }
-    }
-#pragma unroll
-    for (int s = 0; s < SPT; ++s)
-#pragma unroll
-      for (int f = 0; f < 2; ++f) {
-        vx[s][f] = (go >> (slot0 + s)) & 1 ? limited(vx[s][f], E::kMax) : 0.f;
-        top_v = fmaxf(top_v, fabsf(vx[s][f]));
-      }
-    top_k = wave_max(top_k);
-    top_v = wave_max(top_v);
-    if (lane == 0) sh.top[0][wave] = top_k, sh.top[1][wave] = top_v;
-    if (t == 0) sh.scale[0] = p.c.k_scale[blk], sh.scale[1] = p.c.v_scale[blk];
-    __syncthreads();
-    float s0[2], s1[2], inv[2], ratio[2];
-#pragma unroll
-    for (int f = 0; f < 2; ++f) {
-      const float top = fmaxf(fmaxf(sh.top[f][0], sh.top[f][1]), fmaxf(sh.top[f][2], sh.top[f][3]));
-      s0[f] = kept ? sh.scale[f] : 0.f;
-      s1[f] = fmaxf(s0[f], scale_for(top));
-      inv[f] = inverse(s1[f]);
-      ratio[f] = s0[f] * inv[f];
-    }
-    if (t == 0) p.c.k_scale[blk] = s1[0], p.c.v_scale[blk] = s1[1];
-    const bool grow_k = kept && s1[0] > s0[0], grow_v = kept && s1[1] > s0[1];
-#pragma unroll
-    for (int i = 0; i < PASSES; ++i) {
-      const int slot = i * SPP + t / CH;
-      u32x2 *dst = reinterpret_cast<u32x2 *>(kp + slot * D + t % CH * 8);
-      if (!kept || ((go >> slot) & 1)) {  // zeros where no row goes
-        const float *x = kx[i];
-        *dst = u32x2{to_codes(x[0] * inv[0], x[1] * inv[0], x[2] * inv[0], x[3] * inv[0]),
-                     to_codes(x[4] * inv[0], x[5] * inv[0], x[6] * inv[0], x[7] * inv[0])};
-      } else if (grow_k) {
+        for (int j = 0; j < 8; ++j) y[j] = E::template get<LIMITED>(x[i], j) * inv;
+        *dst = u32x2{to_codes(y[0], y[1], y[2], y[3]), to_codes(y[4], y[5], y[6], y[7])};
+      } else if (grow) {
         const u32x2 w = *dst;
-        *dst = u32x2{rescale(w[0], ratio[0]), rescale(w[1], ratio[0])};
+        *dst = u32x2{rescale(w[0], ratio), rescale(w[1], ratio)};
       }
     }
-    if (kept && !wave_go && !grow_v) return;
-    if (grow_v && !merge) load_old();
+  } else {
+    if (kept && !mine && !grow) return;
+    if (grow && !mine)
+#pragma unroll
+      for (int f = 0; f < 2; ++f) Elem<false>::template load<S::Q>(codes + (d0 + f) * kPage + slot0, old[f]);
 #pragma unroll
     for (int f = 0; f < 2; ++f) {
-      unsigned w[SPT / 4];
+      unsigned w[S::Q];
 #pragma unroll
-      for (int j = 0; j < SPT / 4; ++j) {
-        w[j] = to_codes(vx[4 * j][f] * inv[1], vx[4 * j + 1][f] * inv[1], vx[4 * j + 2][f] * inv[1],
-                        vx[4 * j + 3][f] * inv[1]);
+      for (int j = 0; j < S::Q; ++j) {
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = E::template get<LIMITED>(x[4 * j + e], f) * inv;
+        w[j] = to_codes(y[0], y[1], y[2], y[3]);
         if (kept) {
-          unsigned m = (unsigned)(go >> (slot0 + 4 * j)) & 15u;  // new rows among the four slots, as bytes
+          unsigned m = (mine >> 4 * j) & 15u;  // new rows among the four slots, as bytes
           m = ((m & 1) | (m & 2) << 7 | (m & 4) << 14 | (m & 8) << 21) * 255u;
-          const unsigned stay = grow_v ? rescale(old_v[f][j], ratio[1]) : old_v[f][j];
+          const unsigned stay = grow ? rescale(old[f][j], ratio) : old[f][j];
           w[j] = (w[j] & m) | (stay & ~m);
         }
       }
-      unsigned *dst = reinterpret_cast<unsigned *>(vp + (d0 + f) * kPage + slot0);
-      if constexpr (SPT == 16)
+      unsigned *dst = reinterpret_cast<unsigned *>(codes + (d0 + f) * kPage + slot0);
+      if constexpr (S::PASSES == 16)
         *reinterpret_cast<u32x4 *>(dst) = u32x4{w[0], w[1], w[2], w[3]};
       else
         *reinterpret_cast<u32x2 *>(dst) = u32x2{w[0], w[1]};
     }
+  }
+}
+
+// K (IS_V false) or V of one page of one head: the rows in sh.row (set, and a
+// barrier passed). tokens: of the page, at the call's end; held: before it (write).
+template <bool BF16, int D, bool WRITE, bool IS_V>
+__device__ __forceinline__ void do_page(const StoreLaunch &p, Shared &sh, int64_t row0, int h, int page, int tokens,
+                                        int held) {
+  using E = Elem<BF16>;
+  using S = Share<D, IS_V>;
+  constexpr int N = S::N, CH = S::CH, SPP = S::SPP, PASSES = S::PASSES, LPS = S::LPS, Q = S::Q;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const size_t rowb = (size_t)p.c.hkv * D * E::kBytes;
+  const bool there = (unsigned)page < (unsigned)p.c.n_pages;
+  const size_t blk = there ? (size_t)page * p.c.hkv + h : 0;
+  unsigned char *codes = (IS_V ? p.c.v : p.c.k) + blk * (kPage * D);
+  float *scale = (IS_V ? p.c.v_scale : p.c.k_scale) + blk;
+  // V: when writing, LPS neighbouring lanes hold the 64 tokens of two features (whole
+  // 64-byte lines of codes), when reading, the lanes of D / 2 hold a row
+  const int slot0 = !IS_V ? t / CH : WRITE ? lane % LPS * PASSES : (t / (D / 2)) * PASSES;
+  const int d0 = !IS_V ? t % CH * 8 : WRITE ? (wave * (64 / LPS) + lane / LPS) * 2 : t % (D / 2) * 2;
+  auto slot = [&](int i) { return IS_V ? slot0 + i : slot0 + i * SPP; };
+  const unsigned char *rows = static_cast<const unsigned char *>(IS_V ? p.v : p.k);
+  auto at = [&](int i) { return rows + (row0 + sh.row[slot(i)]) * rowb + ((size_t)h * D + d0) * E::kBytes; };
+
+  const unsigned long long asked = __ballot(sh.row[lane] >= 0);
+  // rows that can be moved: below the sequence's tokens, in a page that is there
+  const unsigned long long can = asked & (tokens >= 64 ? ~0ull : (1ull << max(tokens, 0)) - 1);
+  const unsigned long long go = there ? can : 0ull;
+  auto bits = [&](unsigned long long m) {  // of this lane's slots
+    if constexpr (IS_V) return (unsigned)(m >> slot0) & ((1u << PASSES) - 1);
+    unsigned r = 0;
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) r |= ((unsigned)(m >> slot(i)) & 1) << i;
+    return r;
+  };
+  const unsigned mine = bits(go);
+
+  if constexpr (WRITE) {
+    unsigned x[PASSES][E::words(N)] = {};
+    const unsigned rows_mine = bits(can);  // not `go`: these loads need not wait for the page's id
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i)
+      if ((rows_mine >> i) & 1) E::template load<N>(at(i), x[i]);
+    if (!go) return;  // uniform in the workgroup
+    float present = 0.f;
+    if (t == 0) present = *scale;
+    const bool kept = ((held >= 64 ? ~0ull : (1ull << held) - 1) & ~go) != 0;
+    // V: the codes that stay beside a new one in a piece
+    unsigned old[2][Q] = {};
+    auto load_old = [&] {
+#pragma unroll
+      for (int f = 0; f < 2; ++f) Elem<false>::template load<Q>(codes + (d0 + f) * kPage + slot0, old[f]);
+    };
+    if constexpr (IS_V)
+      if (kept && mine) load_old();
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i)
+#pragma unroll
+      for (int j = 0; j < E::words(N); ++j) top = E::max_bits(top, x[i][j]);
+    top = wave_max(E::whole(top));
+    if (lane == 0) sh.top[0][wave] = top;
+    if (t == 0) sh.scale = present;
+    __syncthreads();
+    top = max(max(sh.top[0][0], sh.top[0][1]), max(sh.top[0][2], sh.top[0][3]));
+    const bool special = top >= 0x7f800000u;  // infinities or NaN among the rows
+    if (special) {
+      float m = 0.f;
+#pragma unroll
+      for (int i = 0; i < PASSES; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) m = fmaxf(m, fabsf(E::template get<true>(x[i], j)));
+      top = wave_max(__builtin_bit_cast(unsigned, m));
+      if (lane == 0) sh.top[1][wave] = top;
+      __syncthreads();
+      top = max(max(sh.top[1][0], sh.top[1][1]), max(sh.top[1][2], sh.top[1][3]));
+    }
+    const float s0 = kept ? sh.scale : 0.f;
+    const float s1 = fmaxf(s0, scale_for(__builtin_bit_cast(float, top)));
+    const float inv = inverse(s1), ratio = s0 * inv;
+    const bool grow = kept && s1 > s0;
+    if (t == 0) *scale = s1;
+    special ? put<BF16, D, IS_V, true>(x, old, codes, mine, kept, grow, inv, ratio, slot0, d0)
+            : put<BF16, D, IS_V, false>(x, old, codes, mine, kept, grow, inv, ratio, slot0, d0);
   } else {
-    if (!asked) return;
-    if (p.k) {
-      const float s = there ? p.c.k_scale[blk] : 0.f;
+    const unsigned out = bits(asked);
+    if (!out) return;
+    const float s = there ? *scale : 0.f;
+    if constexpr (!IS_V) {
+      u32x2 w[PASSES] = {};
+#pragma unroll
+      for (int i = 0; i < PASSES; ++i)
+        if ((mine >> i) & 1) w[i] = *reinterpret_cast<const u32x2 *>(codes + slot(i) * D + d0);
 #pragma unroll
       for (int i = 0; i < PASSES; ++i) {
-        const int slot = i * SPP + t / CH;
-        if (!((asked >> slot) & 1)) continue;
-        float x[8] = {};
-        if ((go >> slot) & 1) {
-          const u32x2 w = *reinterpret_cast<const u32x2 *>(kp + slot * D + t % CH * 8);
-          from_codes(w[0], x);
-          from_codes(w[1], x + 4);
+        if (!((out >> i) & 1)) continue;
+        float x[8];
+        from_codes(w[i][0], x);
+        from_codes(w[i][1], x + 4);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) x[j] *= s;
+        for (int j = 0; j < 8; ++j) x[j] *= s;
+        E::template store<8>(const_cast<unsigned char *>(at(i)), x);
+      }
+    } else {
+      unsigned w[2][Q] = {};
+#pragma unroll
+      for (int f = 0; f < 2; ++f)
+        if (mine) Elem<false>::template load<Q>(codes + (d0 + f) * kPage + slot0, w[f]);
+#pragma unroll
+      for (int j = 0; j < Q; ++j) {
+        float a[4], b[4];
+        from_codes(w[0][j], a);
+        from_codes(w[1][j], b);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = 4 * j + e;
+          const bool ok = (mine >> i) & 1;
+          const float x[2] = {ok ? a[e] * s : 0.f, ok ? b[e] * s : 0.f};
+          if ((out >> i) & 1) E::template store<2>(const_cast<unsigned char *>(at(i)), x);
         }
-        E::template store<8>((unsigned char *)p.k + (row0 + sh.row[slot]) * rowb + (size_t)h * D * E::kBytes +
-                                 t % CH * 8 * E::kBytes, x);
       }
-    }
-    if (p.v && wave_asked) {
-      const float s = there ? p.c.v_scale[blk] : 0.f;
-      float x[SPT][2] = {};
-      if (wave_go) {
-#pragma unroll
-        for (int f = 0; f < 2; ++f)
-#pragma unroll
-          for (int j = 0; j < SPT / 4; ++j) {
-            float y[4];
-            from_codes(reinterpret_cast<const unsigned *>(vp + (d0 + f) * kPage + slot0)[j], y);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[4 * j + e][f] = (go >> (slot0 + 4 * j + e)) & 1 ? y[e] * s : 0.f;
-          }
-      }
-#pragma unroll
-      for (int i = 0; i < SPT; ++i)
-        if ((asked >> (slot0 + i)) & 1)
-          E::template store<2>((unsigned char *)p.v + (row0 + sh.row[slot0 + i]) * rowb +
-                                   ((size_t)h * D + d0) * E::kBytes, x[i]);
     }
   }
 }
@@ -303,7 +326,10 @@ template <bool BF16, int D, bool WRITE>
 __global__ __launch_bounds__(kThreads) void cache_store_kernel(const StoreLaunch p) {
   __shared__ Shared sh;
   const int t = threadIdx.x;
-  const int h = blockIdx.x % p.c.hkv, unit = blockIdx.x / p.c.hkv;
+  const int half = p.units * p.c.hkv;  // workgroups of K, then those of V
+  const bool is_v = (int)blockIdx.x >= half || !p.k;
+  const int job = (int)blockIdx.x >= half ? blockIdx.x - half : blockIdx.x;
+  const int h = job % p.c.hkv, unit = job / p.c.hkv;
   int b = 0;
   if (p.per_req) {
     b = unit / p.per_req;
@@ -330,27 +356,38 @@ __global__ __launch_bounds__(kThreads) void cache_store_kernel(const StoreLaunch
     __syncthreads();
     const int pg = (int)(pg64 < 0 ? -1 : pg64);
     const int held = (int)min(max(first - pg64 * kPage, (int64_t)0), (int64_t)kPage);
-    do_page<BF16, D, WRITE>(p, sh, row0, h, page_of(pg), pg < 0 ? 0 : min(L - pg * kPage, kPage), held);
+    const int tokens = pg < 0 ? 0 : min(L - pg * kPage, kPage);
+    is_v ? do_page<BF16, D, WRITE, true>(p, sh, row0, h, page_of(pg), tokens, held)
+         : do_page<BF16, D, WRITE, false>(p, sh, row0, h, page_of(pg), tokens, held);
     return;
   }
+  // which of the unit's rows are their page's first, from one load per lane
   const int32_t *pos = p.pos + row0;
-  for (int r = u * kStoreRows, end = min(n, r + kStoreRows); r < end; ++r) {
-    const int pg = pos[r] >> 6;
-    if (r > 0 && pos[r - 1] >> 6 == pg) continue;
+  const int r0 = u * kStoreRows, lane = t & 63;
+  const int mine = lane < kStoreRows && r0 + lane < n ? pos[r0 + lane] >> 6 : INT32_MIN;
+  const int before = lane < kStoreRows && r0 + lane > 0 && r0 + lane < n ? pos[r0 + lane - 1] >> 6 : INT32_MAX;
+  unsigned firsts = (unsigned)__ballot(lane < kStoreRows && r0 + lane < n && mine != before);
+  for (; firsts; firsts &= firsts - 1) {
+    const int i = __builtin_ctz(firsts), r = r0 + i;
+    const int pg = __builtin_amdgcn_readlane(mine, i);
     __syncthreads();  // the page before is done with sh
-    if (t < kPage) sh.row[t] = -1;
-    __syncthreads();
-    if (t < kPage && r + t < n && pos[r + t] >> 6 == pg) sh.row[pos[r + t] & 63] = r + t;
+    if (t < kPage) {
+      sh.row[t] = -1;
+      // same wave, in order
+      const int at = r + t < n ? pos[r + t] : 0;
+      if (r + t < n && at >> 6 == pg) sh.row[at & 63] = r + t;
+    }
     __syncthreads();
     const int tokens = pg < 0 || (int64_t)pg * kPage >= L ? 0 : min(L - pg * kPage, kPage);
-    do_page<BF16, D, WRITE>(p, sh, row0, h, page_of(pg), tokens, tokens);
+    is_v ? do_page<BF16, D, WRITE, true>(p, sh, row0, h, page_of(pg), tokens, tokens)
+         : do_page<BF16, D, WRITE, false>(p, sh, row0, h, page_of(pg), tokens, tokens);
   }
 }
 
 }  // namespace
 
 hipError_t launch_cache_store(bool write, bool bf16, const StoreLaunch &p, hipStream_t st) {
-  const int grid = p.units * p.c.hkv;
+  const unsigned grid = (unsigned)p.units * p.c.hkv * (p.k && p.v ? 2 : 1);
   auto go = [&](auto kern) { kern<<<grid, kThreads, 0, st>>>(p); };
   if (p.c.d == 128) {
     if (bf16) write ? go(cache_store_kernel<true, 128, true>) : go(cache_store_kernel<true, 128, false>);
