@@ -52,12 +52,15 @@ struct CacheAttnLaunch {
   const void *q;
   void *o;
   float *lse;       // nullable; [hq][lse_stride] at the launch's first row
-  float *part_o;    // n_splits > 1: [row][hq][n_splits][d], normalised
-  float *part_lse;  // [row][hq][n_splits]
+  // n_splits > 1: normalised partial outputs and their LSE, [row][hq][n_splits] of d
+  // values; wide: [row block][hkv][tile of 16 pairs][n_splits] of d / 16 x 64 lanes x 4
+  // values in the order of the accumulators, and of 16 LSEs
+  float *part_o, *part_lse;
   int32_t lse_stride;
   int32_t hq, group;
   int32_t max_len;
-  int32_t n_splits, split_pages;  // pages per split
+  int32_t wide;                   // the kernel for many rows
+  int32_t n_splits, split_pages;  // pages per split (wide: at most kMaxSplitPages)
   float scale_log2;               // softmax scale * log2(e)
   int32_t n_req;
   int32_t blocks;                 // row blocks of all requests
@@ -66,7 +69,9 @@ struct CacheAttnLaunch {
   int32_t blk0[kMaxCacheReqs + 1];
 };
 static_assert(sizeof(CacheAttnLaunch) < 4096, "kernel arguments must fit 4 KiB");
-constexpr int kCacheAttnRows = 16;  // (row, head) pairs of a row block
+// (row, head) pairs of a row block: few rows, many rows in bf16 and in fp32
+constexpr int kCacheAttnRows = 16, kCacheWideRows = 128, kCacheWideRowsF32 = 64;
+constexpr int kMaxSplitPages = 64;
 hipError_t launch_cache_attn(bool bf16, const CacheAttnLaunch &p, hipStream_t st);
 
 // Page calls.

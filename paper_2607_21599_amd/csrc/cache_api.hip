@@ -197,28 +197,43 @@ daf_status_t store(bool write, const daf_attn_cfg_t *cfg, const daf_cache_t *c, 
 
 // ---- attention ------------------------------------------------------------------
 struct AttnPlan {
+  int wide, block_rows;  // which kernel; (row, head) pairs of its row blocks
   int n_splits, split_pages;
   size_t lse_bytes, total;  // workspace: LSEs, then partial outputs
 };
 
-int64_t row_blocks(const daf_attn_cfg_t *cfg, int64_t n) {
-  return (n * (cfg->n_q_heads / cfg->n_kv_heads) + kCacheAttnRows - 1) / kCacheAttnRows;
+int64_t row_blocks(const daf_attn_cfg_t *cfg, int64_t n, int block_rows) {
+  return (n * (cfg->n_q_heads / cfg->n_kv_heads) + block_rows - 1) / block_rows;
+}
+// (row, head) pairs with a place of their own among the wide kernel's partial results
+size_t wide_pairs(const daf_attn_cfg_t *cfg, int64_t blocks, int block_rows) {
+  return (size_t)blocks * cfg->n_kv_heads * block_rows;
 }
 
-// Pages per split, from the sizes that the host knows: about two workgroups per CU,
-// four waves of a workgroup with a page each at least.
+// Kernel and pages per split, from the sizes that the host knows: about two
+// workgroups per CU.
 AttnPlan plan_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_cache_rows_t *rows, int32_t max_len) {
   AttnPlan a{};
-  int64_t blocks = 0;
-  for (int b = 0; b < rows->n; ++b) blocks += row_blocks(cfg, rows->cu[b + 1] - rows->cu[b]);
+  int64_t most = 0, blocks = 0;
+  for (int b = 0; b < rows->n; ++b) most = std::max<int64_t>(most, rows->cu[b + 1] - rows->cu[b]);
+  a.wide = most * (cfg->n_q_heads / cfg->n_kv_heads) > 2 * kCacheAttnRows;
+  a.block_rows = !a.wide ? kCacheAttnRows : cfg->dtype == DAF_BF16 ? kCacheWideRows : kCacheWideRowsF32;
+  for (int b = 0; b < rows->n; ++b) blocks += row_blocks(cfg, rows->cu[b + 1] - rows->cu[b], a.block_rows);
   const int64_t pages = std::max<int64_t>(1, ((int64_t)max_len + kPage - 1) / kPage);
   const int64_t jobs = std::max<int64_t>(1, blocks * c->n_kv_heads);
-  int64_t splits = std::max<int64_t>(1, std::min((512 + jobs - 1) / jobs, (pages + 3) / 4));
-  if (pages <= 16) splits = 1;
+  int64_t splits;
+  if (a.wide) {
+    splits = std::max<int64_t>(std::max<int64_t>(1, 512 / jobs), (pages + kMaxSplitPages - 1) / kMaxSplitPages);
+    splits = std::min(splits, (pages + 1) / 2);
+  } else {  // a page at least for each of a workgroup's four waves
+    splits = std::max<int64_t>(1, std::min((512 + jobs - 1) / jobs, (pages + 3) / 4));
+    if (pages <= 16) splits = 1;
+  }
   a.split_pages = (int)((pages + splits - 1) / splits);
   a.n_splits = (int)((pages + a.split_pages - 1) / a.split_pages);
   if (a.n_splits > 1) {
-    const size_t pairs = (size_t)rows->cu[rows->n] * cfg->n_q_heads * a.n_splits;
+    const size_t pairs = (a.wide ? wide_pairs(cfg, blocks, a.block_rows) : (size_t)rows->cu[rows->n] * cfg->n_q_heads) *
+                         a.n_splits;
     a.lse_bytes = (pairs * sizeof(float) + 255) / 256 * 256;
     a.total = a.lse_bytes + pairs * cfg->head_dim * sizeof(float);
   }
@@ -257,13 +272,16 @@ daf_status_t attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, int32_t layer
   const bool bf16 = cfg->dtype == DAF_BF16;
   const size_t row_bytes = (size_t)cfg->n_q_heads * cfg->head_dim * (bf16 ? 2 : 4);
   const float scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale : 1.f / sqrtf((float)cfg->head_dim);
-  for (int pass = 0; pass < 2; ++pass)
+  for (int pass = 0; pass < 2; ++pass) {
+    int64_t block0 = 0;
     for (int b0 = 0; b0 < rows->n; b0 += kMaxCacheReqs) {
       CacheAttnLaunch p;
       p.c = view(c, layer);
       p.n_req = std::min(kMaxCacheReqs, rows->n - b0);
-      p.blocks = fill(rows, b0, p.n_req, p.cu, p.blk0, &p.per_req, [&](int64_t n) { return row_blocks(cfg, n); });
-      if (p.blocks < 0 || (int64_t)p.blocks * c->n_kv_heads * a.n_splits > INT32_MAX)
+      p.blocks = fill(rows, b0, p.n_req, p.cu, p.blk0, &p.per_req, 
+                      [&](int64_t n) { return row_blocks(cfg, n, a.block_rows); });
+      if (p.blocks < 0 || ((int64_t)c->n_kv_heads * a.n_splits + 7) * p.blocks > INT32_MAX ||
+          (int64_t)p.blocks * c->n_kv_heads * 8 > INT32_MAX)
         return fail(DAF_ERR_UNSUPPORTED, "%d rows over %d keys are too many for one call", total, max_len);
       if (pass == 0 || p.blocks == 0) continue;
       const int64_t row0 = rows->cu[b0];
@@ -277,19 +295,22 @@ daf_status_t attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, int32_t layer
       p.o = const_cast<char *>(rows_at(o, row0, row_bytes));
       p.lse = lse ? lse + row0 : nullptr;
       p.lse_stride = total;
-      const size_t pair0 = (size_t)row0 * cfg->n_q_heads * a.n_splits;
+      const size_t pair0 = (a.wide ? wide_pairs(cfg, block0, a.block_rows) : (size_t)row0 * cfg->n_q_heads) * a.n_splits;
       p.part_lse = a.total ? static_cast<float *>(workspace) + pair0 : nullptr;
       p.part_o = a.total ? reinterpret_cast<float *>(static_cast<char *>(workspace) + a.lse_bytes) +
                                pair0 * cfg->head_dim : nullptr;
       p.hq = cfg->n_q_heads;
       p.group = cfg->n_q_heads / cfg->n_kv_heads;
       p.max_len = max_len;
+      p.wide = a.wide;
       p.n_splits = a.n_splits;
       p.split_pages = a.split_pages;
       p.scale_log2 = scale * 1.4426950408889634f;
       const hipError_t e = launch_cache_attn(bf16, p, stream);
       if (e != hipSuccess) return launched(e, "cache attention launch");
+      block0 += p.blocks;
     }
+  }
   return ok();
 }
 

@@ -36,6 +36,7 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kRows = kCacheAttnRows;
+constexpr int kXcdCount = 8;  // workgroups go to the XCDs in turn
 constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -81,6 +82,27 @@ __device__ __forceinline__ void split_terms(const float (&x)[8], bf16x8 (&out)[T
     for (int j = 0; j < TERMS; ++j) {
       out[j][i] = (__bf16)r;
       r -= (float)out[j][i];
+    }
+  }
+}
+
+// A row of q as the B operand, in T terms: put(term, step, x). Lane quad holds
+// features 64 c + 16 quad + 8 e .. + 7 of step 2 c + e, e < 2.
+template <bool BF16, int D, typename F>
+__device__ __forceinline__ void load_q(const CacheAttnLaunch &p, size_t at, int quad, F put) {
+#pragma unroll
+  for (int ds = 0; ds < D / 32; ++ds) {
+    const int f = (ds >> 1) * 64 + quad * 16 + (ds & 1) * 8;
+    if constexpr (BF16) {
+      put(0, ds, *reinterpret_cast<const bf16x8 *>((const __bf16 *)p.q + at + f));
+    } else {
+      const f32x4 a = *reinterpret_cast<const f32x4 *>((const float *)p.q + at + f);
+      const f32x4 c = *reinterpret_cast<const f32x4 *>((const float *)p.q + at + f + 4);
+      const float x[8] = {a[0], a[1], a[2], a[3], c[0], c[1], c[2], c[3]};
+      bf16x8 part[3];
+      split_terms<3>(x, part);
+#pragma unroll
+      for (int j = 0; j < 3; ++j) put(j, ds, part[j]);
     }
   }
 }
@@ -156,26 +178,9 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(const CacheAttn
   const int idc = min(idx, total - 1);        // pairs past the end repeat the last one
   const int row = idc / p.group, head = h * p.group + idc % p.group;
   const int limit = row_limit(p, r, row);
-  // Q as the B operand: lane n16, features 64 c + 16 quad + 8 (step % 2) .. + 7 of step 2 c + step % 2
   bf16x8 qf[T][DS];
-  {
-    const size_t at = ((size_t)(r.row0 + row) * p.hq + head) * D;
-#pragma unroll
-    for (int ds = 0; ds < DS; ++ds) {
-      const int f = (ds >> 1) * 64 + quad * 16 + (ds & 1) * 8;
-      if constexpr (BF16) {
-        qf[0][ds] = *reinterpret_cast<const bf16x8 *>((const __bf16 *)p.q + at + f);
-      } else {
-        const f32x4 a = *reinterpret_cast<const f32x4 *>((const float *)p.q + at + f);
-        const f32x4 c = *reinterpret_cast<const f32x4 *>((const float *)p.q + at + f + 4);
-        const float x[8] = {a[0], a[1], a[2], a[3], c[0], c[1], c[2], c[3]};
-        bf16x8 part[T];
-        split_terms<T>(x, part);
-#pragma unroll
-        for (int j = 0; j < T; ++j) qf[j][ds] = part[j];
-      }
-    }
-  }
+  load_q<BF16, D>(p, ((size_t)(r.row0 + row) * p.hq + head) * D, quad,
+                  [&](int j, int ds, const bf16x8 &x) { qf[j][ds] = x; });
   // range of limits over the block's rows
   int lim_hi = limit, lim_lo = limit;
 #pragma unroll
@@ -388,16 +393,316 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(const CacheAttnLau
   if (c == 0 && p.lse) p.lse[(size_t)head * p.lse_stride + row] = l > 0.f ? m + __logf(l) : -INFINITY;
 }
 
+// ---- many rows -------------------------------------------------------------------
+// A row block is 4 waves of 16 MT (row, head) pairs, which share every page through
+// LDS: copies go from memory to LDS in the layout that the waves read (16 bytes per
+// lane of the operand, in lane order: no bank conflicts), kStages - 1 pages ahead.
+constexpr int kStages = 3;
+constexpr float kNoReference = -3e38f;           // before the first key: any visible one's probability is infinite
+constexpr unsigned kRaise = (127 + 8) << 7;      // bf16 bits of the probability that raises the reference: 2^8
+
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0F70);  // vmcnt(N); the other counters at their maxima
+}
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_barrier" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// One 1 KiB copy of `extent` bytes at base: lane i's 16 bytes at voff go to LDS byte
+// lds + 16 i. In asm, so that the compiler does not wait for the copies in flight at
+// each LDS read: wait_vm counts them, the barriers order them.
+__device__ __forceinline__ void copy_to_lds(const u32x4 &rsrc, uint32_t voff, uint32_t lds) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dwordx4 %1, %2, 0 offen lds"
+      :
+      : "s"(lds), "v"(voff), "s"(rsrc)
+      : "memory", "m0");
+#endif
+}
+
+// the larger of three bf16 values that are not negative, per half of a word; their
+// bits order alike as fp16, and a pattern of an fp16 NaN stays one
+__device__ __forceinline__ unsigned max3_pairs(unsigned a, unsigned b, unsigned c) {
+  unsigned r;
+  asm("v_pk_maximum3_f16 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
+template <bool BF16, int D, int MT>
+struct WideState {
+  static constexpr int T = BF16 ? 1 : 3, DS = D / 32, DB = D / 16;
+  bf16x8 q[T][MT][DS];
+  f32x4 o[MT][DB];
+  float m[MT], l[MT];
+  int limit[MT];
+  float scale_log2;
+};
+
+// Half HALF (keys 16 quad + 8 HALF .. + 7 of each lane group) of a page in LDS.
+template <bool BF16, int D, int MT, int HALF, bool MASK>
+__device__ __forceinline__ void wide_half(WideState<BF16, D, MT> &w, const unsigned char *page, int lane, int key0,
+                                          int lim_hi, float ks, float vs) {
+  using W = WideState<BF16, D, MT>;
+  constexpr int T = W::T, DB = W::DB, C = D / 64;
+  f32x4 s[MT][2] = {};
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const u32x4 k = *reinterpret_cast<const u32x4 *>(page + ((2 * HALF + t) * C + c) * 1024 + lane * 16);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const bf16x8 a = widen(k[2 * e], k[2 * e + 1], ks);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int j = T - 1; j >= 0; --j) s[mt][t] = mfma(a, w.q[j][mt][2 * c + e], s[mt][t]);
+      }
+    }
+  if constexpr (MASK) {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (key0 + 8 * HALF + i > w.limit[mt]) s[mt][i >> 2][i & 3] = -INFINITY;
+  }
+  float e[MT][8];
+  bf16x8 pf[MT][T];
+  auto weights = [&] {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[mt][i] = exp2_(__builtin_fmaf(s[mt][i >> 2][i & 3], w.scale_log2, -w.m[mt]));
+      split_terms<T>(e[mt], pf[mt]);
+    }
+  };
+  weights();
+  unsigned top = 0;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const u32x4 a = __builtin_bit_cast(u32x4, pf[mt][0]);
+    top = max3_pairs(top, a[0], a[1]);
+    top = max3_pairs(top, a[2], a[3]);
+  }
+  if (__ballot(top >= kRaise << 16 || (top & 0xffffu) >= kRaise)) {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      float mx = s[mt][0][0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[mt][i >> 2][i & 3]);
+      const float m = fmaxf(w.m[mt], row_max(mx) * w.scale_log2), alpha = exp2_(w.m[mt] - m);
+      w.m[mt] = m;
+      w.l[mt] *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) w.o[mt][db] *= alpha;
+    }
+    weights();
+  }
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+    w.l[mt] += ((e[mt][0] + e[mt][1]) + (e[mt][2] + e[mt][3])) + ((e[mt][4] + e[mt][5]) + (e[mt][6] + e[mt][7]));
+#pragma unroll
+  for (int db = 0; db < DB; ++db) {
+    u32x2 v = *reinterpret_cast<const u32x2 *>(page + kPage * D + db * 1024 + lane * 16 + HALF * 8);
+    if constexpr (MASK) {
+      // keys that no row of the wave sees may hold NaN codes: their values become 0
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int left = lim_hi + 1 - (key0 + 8 * HALF + 4 * t);
+        v[t] &= left >= 4 ? ~0u : left <= 0 ? 0u : (1u << 8 * left) - 1;
+      }
+    }
+    const bf16x8 a = widen(v[0], v[1], vs);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int j = T - 1; j >= 0; --j) w.o[mt][db] = mfma(a, pf[mt][j], w.o[mt][db]);
+  }
+}
+
+template <bool BF16, int D, int MT>
+__global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttnLaunch p) {
+  using W = WideState<BF16, D, MT>;
+  constexpr int DB = W::DB;
+  constexpr int PAGE_BYTES = 2 * kPage * D, IPW = PAGE_BYTES / 1024 / kWaves;  // copies per wave and page
+  __shared__ __align__(16) unsigned char lds[kStages * PAGE_BYTES];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n16 = lane & 15, quad = lane >> 4;
+  // the row blocks of one (head, split) read the same pages: consecutive on one XCD
+  const int groups = p.c.hkv * p.n_splits;
+  const int xcd = blockIdx.x % kXcdCount, slot = blockIdx.x / kXcdCount;
+  const int g = slot / p.blocks * kXcdCount + xcd, blk = slot % p.blocks;
+  if (g >= groups) return;
+  const int h = g % p.c.hkv, split = g / p.c.hkv;
+  const Request r = find_request(p, blk);
+  const int pages = (r.L + kPage - 1) / kPage;
+  const int pg0 = split * p.split_pages;
+  if (split > 0 && pg0 >= pages) return;  // no keys here: the join leaves this split out
+  const int total = r.n * p.group;
+
+  W w;
+  w.scale_log2 = p.scale_log2;
+  int lim_hi = INT32_MIN, lim_lo = INT32_MAX;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int idx = min((r.block * kWaves + wave) * 16 * MT + mt * 16 + n16, total - 1);  // past the end: the last pair
+    const int row = idx / p.group, head = h * p.group + idx % p.group;
+    w.limit[mt] = row_limit(p, r, row);
+    lim_hi = max(lim_hi, w.limit[mt]);
+    lim_lo = min(lim_lo, w.limit[mt]);
+    load_q<BF16, D>(p, ((size_t)(r.row0 + row) * p.hq + head) * D, quad, [&](int j, int ds, const bf16x8 &x) { w.q[j][mt][ds] = x; });
+    w.m[mt] = kNoReference;
+    w.l[mt] = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) w.o[mt][db] = f32x4{};
+  }
+#pragma unroll
+  for (int m = 8; m; m >>= 1) {
+    lim_hi = max(lim_hi, __shfl_xor(lim_hi, m));
+    lim_lo = min(lim_lo, __shfl_xor(lim_lo, m));
+  }
+  lim_hi = __builtin_amdgcn_readfirstlane(lim_hi);
+  lim_lo = __builtin_amdgcn_readfirstlane(lim_lo);
+
+  // this split's pages, one per lane (split_pages <= 64)
+  const int n = __builtin_amdgcn_readfirstlane(min(pg0 + p.split_pages, pages) - pg0);
+  const int id = lane < n ? r.pages[pg0 + lane] : -1;
+  const bool there = (unsigned)id < (unsigned)p.c.n_pages;
+  const size_t at = (size_t)(there ? id : 0) * p.c.hkv + h;
+  const int ids = there ? id : -1;
+  const float kss = p.c.k_scale[at], vss = p.c.v_scale[at];
+  uint32_t voff[IPW];
+#pragma unroll
+  for (int i = 0; i < IPW; ++i) {
+    const int j = (wave & 1) * IPW + i;  // of K (waves 0 and 1) or V
+    voff[i] = wave < 2 ? ((n16 >> 2) * 16 + (n16 & 3) + j / (D / 64) * 4) * D + j % (D / 64) * 64 + quad * 16
+                       : (j * 16 + n16) * kPage + quad * 16;
+  }
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds + wave * IPW * 1024;
+  const unsigned char *pool = wave < 2 ? p.c.k : p.c.v;
+  auto fetch = [&](int i) {
+    const int pid = max(__builtin_amdgcn_readlane(ids, i), 0);  // a page that is not there: any page, its keys are skipped
+    const uint64_t base = (uint64_t)(pool + ((size_t)pid * p.c.hkv + h) * (kPage * D));
+    const u32x4 rsrc = {(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, (uint32_t)(kPage * D), 0x00020000u};
+    const uint32_t to = lds0 + i % kStages * PAGE_BYTES;
+#pragma unroll
+    for (int c = 0; c < IPW; ++c) copy_to_lds(rsrc, voff[c], to + c * 1024);
+  };
+  auto page = [&](int i) {
+    const int first = (pg0 + i) * kPage;
+    if (first > lim_hi || __builtin_amdgcn_readlane(ids, i) < 0) return;
+    const float ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, kss), i));
+    const float vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, vss), i));
+    const unsigned char *src = lds + i % kStages * PAGE_BYTES;
+    const int key0 = first + quad * 16;
+    if (first + kPage - 1 > lim_lo) {
+      wide_half<BF16, D, MT, 0, true>(w, src, lane, key0, lim_hi, ks, vs);
+      wide_half<BF16, D, MT, 1, true>(w, src, lane, key0, lim_hi, ks, vs);
+    } else {
+      wide_half<BF16, D, MT, 0, false>(w, src, lane, key0, lim_hi, ks, vs);
+      wide_half<BF16, D, MT, 1, false>(w, src, lane, key0, lim_hi, ks, vs);
+    }
+  };
+  if (n > 0) {
+    wait_vm<0>();
+    fetch(0);
+    if (n > 1) fetch(1);
+    for (int i = 0; i < n; ++i) {
+      if (i + 1 < n) wait_vm<IPW>();  // page i is here, page i + 1 may be on its way
+      else wait_vm<0>();
+      lds_barrier();  // for every wave, and all are done with page i - 1, whose place page i + 2 takes
+      if (i + 2 < n) fetch(i + 2);
+      page(i);
+    }
+  }
+
+  // results
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const float l = row_sum(w.l[mt]);
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float lse = l > 0.f ? (w.m[mt] + log2f(l)) * kLn2 : -INFINITY;
+    const int tile = (r.block * kWaves + wave) * MT + mt, idx = tile * 16 + n16;
+    if (p.n_splits > 1) {
+      const size_t part = (((size_t)(blk * p.c.hkv + h) * kWaves + wave) * MT + mt) * p.n_splits + split;
+      if (quad == 0) p.part_lse[part * 16 + n16] = lse;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        *reinterpret_cast<f32x4 *>(p.part_o + (part * DB + db) * 256 + lane * 4) = w.o[mt][db] * inv;
+    } else if (idx < total) {
+      const int row = r.row0 + idx / p.group, head = h * p.group + idx % p.group;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const f32x4 x = w.o[mt][db] * inv;
+        const float y[4] = {x[0], x[1], x[2], x[3]};
+        store_out<BF16>(p, row, head, db * 16 + quad * 4, y, D);
+      }
+      if (quad == 0 && p.lse) p.lse[(size_t)head * p.lse_stride + row] = lse;
+    }
+  }
+}
+
+// Join the splits of one tile of 16 pairs; a wave takes DB / 4 blocks of 16 features,
+// a lane the same pair and features as in the kernel above.
+template <bool BF16, int D, int MT>
+__global__ __launch_bounds__(kThreads) void cache_wide_join_kernel(const CacheAttnLaunch p) {
+  constexpr int DB = D / 16, PER = DB / kWaves;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n16 = lane & 15, quad = lane >> 4;
+  const int tile = blockIdx.x % (kWaves * MT), rest = blockIdx.x / (kWaves * MT);
+  const int h = rest % p.c.hkv, blk = rest / p.c.hkv;
+  const Request r = find_request(p, blk);
+  const int idx = (r.block * kWaves * MT + tile) * 16 + n16, total = r.n * p.group;
+  if ((r.block * kWaves * MT + tile) * 16 >= total) return;
+  const int pages = (r.L + kPage - 1) / kPage;
+  const int n = max(1, (pages + p.split_pages - 1) / p.split_pages);  // splits that hold keys
+  const size_t part = (size_t)blockIdx.x * p.n_splits;
+  const float *lse = p.part_lse + part * 16 + n16;
+  float m = -INFINITY;
+#pragma unroll 8
+  for (int s = 0; s < n; ++s) m = fmaxf(m, lse[s * 16]);
+  const float ref = m == -INFINITY ? 0.f : m;
+  f32x4 x[PER] = {};
+  float l = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < n; ++s) {
+    const float wt = __expf(lse[s * 16] - ref);
+    l += wt;
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+      x[k] += wt * *reinterpret_cast<const f32x4 *>(p.part_o + ((part + s) * DB + wave * PER + k) * 256 + lane * 4);
+  }
+  if (idx >= total) return;
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const int row = r.row0 + idx / p.group, head = h * p.group + idx % p.group;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const float y[4] = {x[k][0] * inv, x[k][1] * inv, x[k][2] * inv, x[k][3] * inv};
+    store_out<BF16>(p, row, head, (wave * PER + k) * 16 + quad * 4, y, D);
+  }
+  if (wave == 0 && quad == 0 && p.lse) p.lse[(size_t)head * p.lse_stride + row] = l > 0.f ? m + __logf(l) : -INFINITY;
+}
+
 template <bool BF16, int D>
 hipError_t launch(const CacheAttnLaunch &p, hipStream_t st) {
-  const int rows = p.cu[p.n_req];
-  cache_attn_kernel<BF16, D><<<p.blocks * p.c.hkv * p.n_splits, kThreads, 0, st>>>(p);
-  hipError_t e = hipGetLastError();
-  if (e == hipSuccess && p.n_splits > 1) {
-    cache_join_kernel<BF16, D><<<rows * p.hq, kThreads, 0, st>>>(p);
-    e = hipGetLastError();
+  constexpr int MT = BF16 ? kCacheWideRows / 64 : kCacheWideRowsF32 / 64;
+  const int jobs = p.blocks * p.c.hkv;
+  if (p.wide) {
+    const int groups = p.c.hkv * p.n_splits;
+    cache_wide_kernel<BF16, D, MT><<<(groups + kXcdCount - 1) / kXcdCount * kXcdCount * p.blocks, kThreads, 0, st>>>(p);
+  } else {
+    cache_attn_kernel<BF16, D><<<jobs * p.n_splits, kThreads, 0, st>>>(p);
   }
-  return e;
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.n_splits == 1) return e;
+  if (p.wide) cache_wide_join_kernel<BF16, D, MT><<<jobs * kWaves * MT, kThreads, 0, st>>>(p);
+  else cache_join_kernel<BF16, D><<<p.cu[p.n_req] * p.hq, kThreads, 0, st>>>(p);
+  return hipGetLastError();
 }
 
 }  // namespace
