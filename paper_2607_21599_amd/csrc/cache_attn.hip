@@ -22,6 +22,8 @@
 // (m, sum, O) through LDS; splits are joined by a second kernel.
 #include <math.h>
 
+#include <type_traits>
+
 #include "cache.h"
 
 namespace daf {
@@ -30,6 +32,7 @@ namespace {
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
@@ -396,10 +399,22 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(const CacheAttnLau
 // ---- many rows -------------------------------------------------------------------
 // A row block is 4 waves of 16 MT (row, head) pairs, which share every page through
 // LDS: copies go from memory to LDS in the layout that the waves read (16 bytes per
-// lane of the operand, in lane order: no bank conflicts), kStages - 1 pages ahead.
-constexpr int kStages = 3;
-constexpr float kNoReference = -3e38f;           // before the first key: any visible one's probability is infinite
-constexpr unsigned kRaise = (127 + 8) << 7;      // bf16 bits of the probability that raises the reference: 2^8
+// lane of the operand, in lane order: no bank conflicts for K), two pages ahead.
+//
+// Half pages (32 keys) go through three stages, each of another half: the scores of
+// half h + 1, the weights of half h and the value product of half h - 1 make one
+// block of straight code, in which every matrix instruction has 3 to 4 vector
+// instructions of the other stages beside it (one wave's matrix and vector
+// instructions overlap when they are mixed: 1 and 3 take 9.4 ns on a SIMD with two
+// waves, against 7.8 and 4.8 alone; 4 and 16 in turn take 40 of 31 and 26).
+//
+// The reference m of a row is an integer (base-2 units), so that raising it scales O,
+// the sum and the weights in flight by a power of two, exactly. It is raised, to the
+// ceiling of the row's maximum, before a half whose scores would give a weight above
+// 2^8, so a weight is at most that.
+constexpr int kStages = 4;
+constexpr float kNoReference = -3e38f;  // before the first visible key
+constexpr float kSlack = 8.f;
 
 template <int N>
 __device__ __forceinline__ void wait_vm() {
@@ -411,126 +426,217 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// One 1 KiB copy of `extent` bytes at base: lane i's 16 bytes at voff go to LDS byte
+// One 1 KiB copy: lane i's 16 bytes at byte voff + soff of the buffer go to LDS byte
 // lds + 16 i. In asm, so that the compiler does not wait for the copies in flight at
 // each LDS read: wait_vm counts them, the barriers order them.
-__device__ __forceinline__ void copy_to_lds(const u32x4 &rsrc, uint32_t voff, uint32_t lds) {
+__device__ __forceinline__ void copy_to_lds(const u32x4 &rsrc, uint32_t voff, uint32_t soff, uint32_t lds) {
 #if defined(__HIP_DEVICE_COMPILE__)
   asm volatile(
       "s_mov_b32 m0, %0\n\t"
       "s_nop 0\n\t"
-      "buffer_load_dwordx4 %1, %2, 0 offen lds"
+      "buffer_load_dwordx4 %1, %2, %3 offen lds"
       :
-      : "s"(lds), "v"(voff), "s"(rsrc)
+      : "s"(lds), "v"(voff), "s"(rsrc), "s"(soff)
       : "memory", "m0");
 #endif
 }
 
-// the larger of three bf16 values that are not negative, per half of a word; their
-// bits order alike as fp16, and a pattern of an fp16 NaN stays one
-__device__ __forceinline__ unsigned max3_pairs(unsigned a, unsigned b, unsigned c) {
-  unsigned r;
-  asm("v_pk_maximum3_f16 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
+// 16 keys x 16 rows over 128 e4m3 features times 2^(exponent - 127) of each side
+__device__ __forceinline__ f32x4 mfma8(const i32x8 &a, const i32x8 &b, const f32x4 &c, int ea, int eb) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, ea, 0, eb);
+#else
+  return c;
+#endif
 }
 
-template <bool BF16, int D, int MT>
-struct WideState {
-  static constexpr int T = BF16 ? 1 : 3, DS = D / 32, DB = D / 16;
-  bf16x8 q[T][MT][DS];
-  f32x4 o[MT][DB];
-  float m[MT], l[MT];
-  int limit[MT];
-  float scale_log2;
-};
-
-// Half HALF (keys 16 quad + 8 HALF .. + 7 of each lane group) of a page in LDS.
-template <bool BF16, int D, int MT, int HALF, bool MASK>
-__device__ __forceinline__ void wide_half(WideState<BF16, D, MT> &w, const unsigned char *page, int lane, int key0,
-                                          int lim_hi, float ks, float vs) {
-  using W = WideState<BF16, D, MT>;
-  constexpr int T = W::T, DB = W::DB, C = D / 64;
-  f32x4 s[MT][2] = {};
+// A bf16 row of q as two e4m3 terms: high + low, times the row's power of two. e4m3
+// has 4 significant bits and bf16 8, so the sum is q exactly, except that a feature
+// below 2^-10 of the row's largest may be off by 2^-17 of that. K then enters the
+// scores as it is stored, without a conversion, at the matrix cores' double rate for
+// 8 bits. D = 64: one operand of 128, quads 0 and 1 the high terms, 2 and 3 the low.
+template <int D>
+struct Split8 {
+  static constexpr int NT = D / 64;  // operands
+  i32x8 q[NT];
+  int exponent;  // of the row's scale, biased
+  // x: this lane's 32 features (D = 128: all that it holds; D = 64: of its half of the row)
+  __device__ __forceinline__ void set(const float (&x)[32], int quad) {
+    float top = 0.f;
 #pragma unroll
-  for (int t = 0; t < 2; ++t)
+    for (int i = 0; i < 32; ++i) top = fmaxf(top, fabsf(x[i]));
+    top = row_max(top);
+    const unsigned u = __builtin_bit_cast(unsigned, top);
+    // smallest e with top <= 448 * 2^e, kept where both 2^e and its inverse are normal
+    const int e = min(max((int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), -120), 120);
+    exponent = e + 127;
+    const float inv = __builtin_bit_cast(float, (unsigned)(127 - e) << 23);
+#if defined(__HIP_DEVICE_COMPILE__)
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const u32x4 k = *reinterpret_cast<const u32x4 *>(page + ((2 * HALF + t) * C + c) * 1024 + lane * 16);
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const bf16x8 a = widen(k[2 * e], k[2 * e + 1], ks);
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-          for (int j = T - 1; j >= 0; --j) s[mt][t] = mfma(a, w.q[j][mt][2 * c + e], s[mt][t]);
+    for (int w = 0; w < 8; ++w) {
+      const float y[4] = {x[4 * w] * inv, x[4 * w + 1] * inv, x[4 * w + 2] * inv, x[4 * w + 3] * inv};
+      int hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+      hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], hi, true);
+      const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
+      int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0] - a[0], y[1] - a[1], 0, false);
+      lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2] - b[0], y[3] - b[1], lo, true);
+      if constexpr (NT == 2) {
+        q[0][w] = hi;
+        q[1][w] = lo;
+      } else {
+        q[0][w] = quad < 2 ? hi : lo;
       }
     }
-  if constexpr (MASK) {
+#endif
+  }
+};
+
+template <bool BF16, int D, int MT>
+struct Wide {
+  static constexpr int T = BF16 ? 1 : 3, DS = D / 32, DB = D / 16;
+  static constexpr int C = BF16 ? 2 : D / 64;              // 16-byte pieces of a key that a lane reads
+  static constexpr int UNITS = BF16 ? 2 : 4 * (D / 64);    // steps of the scores of a half
+  static constexpr int MFMAS = (BF16 ? 2 * (D / 64) : UNITS * T) * MT + DB * MT * T;  // of a block
+  static constexpr int PAGE_BYTES = 2 * kPage * D;
+  using Scores = f32x4[MT][2];   // a lane's 8 keys of a half, per row
+  using Weights = bf16x8[MT][T];
+  bf16x8 q[BF16 ? 1 : T][MT][DS];  // fp32
+  Split8<D> q8[MT];                // bf16
+  f32x4 o[MT][DB];
+  float m[MT], l[MT], top[MT];   // reference, sum, largest score that needs no raise
+  int limit[MT];
+  float scale_log2;
+  int lane, lim_hi;
+
+  // K of half HALF of a page in LDS: of 16 keys, a lane's pieces
+  template <int HALF>
+  __device__ __forceinline__ void read_k(const unsigned char *page, u32x4 (&k)[2][C]) const {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const unsigned char *at = BF16 && D == 64
+                                      ? page + (2 * HALF + t) * 1024 + ((2 * ((lane >> 4) & 1) + c) * 16 + (lane & 15)) * 16
+                                      : page + ((2 * HALF + t) * C + c) * 1024 + lane * 16;
+        k[t][c] = *reinterpret_cast<const u32x4 *>(at);
+      }
+  }
+  template <int HALF>
+  __device__ __forceinline__ void read_v(const unsigned char *page, u32x2 (&v)[DB]) const {
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+      v[db] = *reinterpret_cast<const u32x2 *>(page + kPage * D + db * 1024 + lane * 16 + HALF * 8);
+  }
+  // step u of the scores, u < UNITS
+  __device__ __forceinline__ void score_unit(int u, const u32x4 (&k)[2][C], float ks, Scores &s) const {
+    if constexpr (BF16) {
+      i32x8 a;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) a[i] = (int)k[u][i >> 2][i & 3];
+      const int ea = (int)(__builtin_bit_cast(unsigned, ks) >> 23);
+#pragma unroll
+      for (int j = Split8<D>::NT - 1; j >= 0; --j)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+          s[mt][u] = mfma8(a, q8[mt].q[j], j == Split8<D>::NT - 1 ? f32x4{} : s[mt][u], ea, q8[mt].exponent);
+    } else {
+      const int t = u & 1, e = (u >> 1) & 1, c = u >> 2;
+      const bf16x8 a = widen(k[t][c][2 * e], k[t][c][2 * e + 1], ks);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int j = T - 1; j >= 0; --j)
+          s[mt][t] = mfma(a, q[j][mt][2 * c + e], c + e == 0 && j == T - 1 ? f32x4{} : s[mt][t]);
+    }
+  }
+  __device__ __forceinline__ void value_unit(int db, const u32x2 (&v)[DB], float vs, const Weights &pf) {
+    const bf16x8 a = widen(v[db][0], v[db][1], vs);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int j = T - 1; j >= 0; --j) o[mt][db] = mfma(a, pf[mt][j], o[mt][db]);
+  }
+  // keys (key, key + 1, ...: a lane's 8) past a row's limit get no weight, and the
+  // values of those that no row of the wave sees, which may be NaN codes, become 0
+  __device__ __forceinline__ void mask_scores(Scores &s, int key) const {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (key0 + 8 * HALF + i > w.limit[mt]) s[mt][i >> 2][i & 3] = -INFINITY;
+        if (key + i > limit[mt]) s[mt][i >> 2][i & 3] = -INFINITY;
   }
-  float e[MT][8];
-  bf16x8 pf[MT][T];
-  auto weights = [&] {
+  __device__ __forceinline__ void mask_values(u32x2 (&v)[DB], int key) const {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int left = lim_hi + 1 - key - 4 * t;
+      const unsigned keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << 8 * left) - 1;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) v[db][t] &= keep;
+    }
+  }
+  // raises the references that the scores s need raised; pf are the weights in flight
+  __device__ __forceinline__ void raise(const Scores &s, Weights &pf) {
+    bool need = false;
+    float mx[MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
+      mx[mt] = s[mt][0][0];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) e[mt][i] = exp2_(__builtin_fmaf(s[mt][i >> 2][i & 3], w.scale_log2, -w.m[mt]));
-      split_terms<T>(e[mt], pf[mt]);
+      for (int i = 1; i < 8; ++i) mx[mt] = fmaxf(mx[mt], s[mt][i >> 2][i & 3]);
+      need |= mx[mt] > top[mt];
     }
-  };
-  weights();
-  unsigned top = 0;
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    const u32x4 a = __builtin_bit_cast(u32x4, pf[mt][0]);
-    top = max3_pairs(top, a[0], a[1]);
-    top = max3_pairs(top, a[2], a[3]);
-  }
-  if (__ballot(top >= kRaise << 16 || (top & 0xffffu) >= kRaise)) {
+    if (__builtin_expect(__ballot(need) == 0, 1)) return;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      float mx = s[mt][0][0];
+      const float to = fmaxf(m[mt], ceilf(row_max(mx[mt]) * scale_log2));
+      const float alpha = exp2_(m[mt] - to);  // a power of two; 0 for the first keys
+      m[mt] = to;
+      top[mt] = (to + kSlack) / scale_log2;
+      l[mt] *= alpha;
 #pragma unroll
-      for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[mt][i >> 2][i & 3]);
-      const float m = fmaxf(w.m[mt], row_max(mx) * w.scale_log2), alpha = exp2_(w.m[mt] - m);
-      w.m[mt] = m;
-      w.l[mt] *= alpha;
+      for (int db = 0; db < DB; ++db) o[mt][db] *= alpha;
 #pragma unroll
-      for (int db = 0; db < DB; ++db) w.o[mt][db] *= alpha;
+      for (int j = 0; j < T; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) pf[mt][j][i] = (__bf16)((float)pf[mt][j][i] * alpha);
     }
-    weights();
   }
+  // The block: weights of scores s into pf (l grows), scores of K k into s, value
+  // product of the weights that pf held.
+  __device__ __forceinline__ void block(Scores &s, Weights &pf, const u32x4 (&k)[2][C], float ks, const u32x2 (&v)[DB],
+                                        float vs) {
+    Scores next;
+    float e[MT][8];
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
-    w.l[mt] += ((e[mt][0] + e[mt][1]) + (e[mt][2] + e[mt][3])) + ((e[mt][4] + e[mt][5]) + (e[mt][6] + e[mt][7]));
+    for (int step = 0; step < 8; ++step) {
 #pragma unroll
-  for (int db = 0; db < DB; ++db) {
-    u32x2 v = *reinterpret_cast<const u32x2 *>(page + kPage * D + db * 1024 + lane * 16 + HALF * 8);
-    if constexpr (MASK) {
-      // keys that no row of the wave sees may hold NaN codes: their values become 0
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int left = lim_hi + 1 - (key0 + 8 * HALF + 4 * t);
-        v[t] &= left >= 4 ? ~0u : left <= 0 ? 0u : (1u << 8 * left) - 1;
+      for (int mt = 0; mt < MT; ++mt) {
+        e[mt][step] = exp2_(__builtin_fmaf(s[mt][step >> 2][step & 3], scale_log2, -m[mt]));
+        l[mt] += e[mt][step];
       }
+      if (step * UNITS % 8 == 0) score_unit(step * UNITS / 8, k, ks, next);
+      if (step * DB % 8 == 0) value_unit(step * DB / 8, v, vs, pf);
     }
-    const bf16x8 a = widen(v[0], v[1], vs);
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int mt = 0; mt < MT; ++mt) {
+      split_terms<T>(e[mt], pf[mt]);
+      s[mt][0] = next[mt][0];
+      s[mt][1] = next[mt][1];
+    }
+    // a matrix instruction, then four others, and so on
 #pragma unroll
-      for (int j = T - 1; j >= 0; --j) w.o[mt][db] = mfma(a, pf[mt][j], w.o[mt][db]);
+    for (int i = 0; i < MFMAS; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x402, 4, 0);
+    }
   }
-}
+};
 
 template <bool BF16, int D, int MT>
 __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttnLaunch p) {
-  using W = WideState<BF16, D, MT>;
-  constexpr int DB = W::DB;
-  constexpr int PAGE_BYTES = 2 * kPage * D, IPW = PAGE_BYTES / 1024 / kWaves;  // copies per wave and page
+  using W = Wide<BF16, D, MT>;
+  constexpr int DB = W::DB, C = W::C;
+  constexpr int PAGE_BYTES = W::PAGE_BYTES, IPW = PAGE_BYTES / 1024 / kWaves;  // copies per wave and page
   __shared__ __align__(16) unsigned char lds[kStages * PAGE_BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n16 = lane & 15, quad = lane >> 4;
@@ -548,6 +654,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
 
   W w;
   w.scale_log2 = p.scale_log2;
+  w.lane = lane;
   int lim_hi = INT32_MIN, lim_lo = INT32_MAX;
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
@@ -556,8 +663,22 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
     w.limit[mt] = row_limit(p, r, row);
     lim_hi = max(lim_hi, w.limit[mt]);
     lim_lo = min(lim_lo, w.limit[mt]);
-    load_q<BF16, D>(p, ((size_t)(r.row0 + row) * p.hq + head) * D, quad, [&](int j, int ds, const bf16x8 &x) { w.q[j][mt][ds] = x; });
+    const size_t q_at = ((size_t)(r.row0 + row) * p.hq + head) * D;
+    if constexpr (BF16) {
+      float x[32];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int f = D == 128 ? c / 2 * 64 + quad * 16 + c % 2 * 8 : (quad & 1) * 32 + c * 8;
+        const bf16x8 y = *reinterpret_cast<const bf16x8 *>((const __bf16 *)p.q + q_at + f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[8 * c + i] = (float)y[i];
+      }
+      w.q8[mt].set(x, quad);
+    } else {
+      load_q<BF16, D>(p, q_at, quad, [&](int j, int ds, const bf16x8 &x) { w.q[j][mt][ds] = x; });
+    }
     w.m[mt] = kNoReference;
+    w.top[mt] = kNoReference / p.scale_log2;
     w.l[mt] = 0.f;
 #pragma unroll
     for (int db = 0; db < DB; ++db) w.o[mt][db] = f32x4{};
@@ -567,59 +688,102 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
     lim_hi = max(lim_hi, __shfl_xor(lim_hi, m));
     lim_lo = min(lim_lo, __shfl_xor(lim_lo, m));
   }
-  lim_hi = __builtin_amdgcn_readfirstlane(lim_hi);
+  w.lim_hi = __builtin_amdgcn_readfirstlane(lim_hi);
   lim_lo = __builtin_amdgcn_readfirstlane(lim_lo);
 
-  // this split's pages, one per lane (split_pages <= 64)
-  const int n = __builtin_amdgcn_readfirstlane(min(pg0 + p.split_pages, pages) - pg0);
-  const int id = lane < n ? r.pages[pg0 + lane] : -1;
+  // this split's pages that are there, one per lane (split_pages <= 64): lane i takes
+  // the i-th of them
+  const int in_split = min(pg0 + p.split_pages, pages) - pg0;
+  int id = lane < in_split ? r.pages[pg0 + lane] : -1;
   const bool there = (unsigned)id < (unsigned)p.c.n_pages;
-  const size_t at = (size_t)(there ? id : 0) * p.c.hkv + h;
-  const int ids = there ? id : -1;
-  const float kss = p.c.k_scale[at], vss = p.c.v_scale[at];
-  uint32_t voff[IPW];
-#pragma unroll
-  for (int i = 0; i < IPW; ++i) {
-    const int j = (wave & 1) * IPW + i;  // of K (waves 0 and 1) or V
-    voff[i] = wave < 2 ? ((n16 >> 2) * 16 + (n16 & 3) + j / (D / 64) * 4) * D + j % (D / 64) * 64 + quad * 16
-                       : (j * 16 + n16) * kPage + quad * 16;
+  const unsigned long long mask = __ballot(there);
+  const int n = __builtin_popcountll(mask);
+  int from = 0;  // lane of the lane-th set bit
+  {
+    unsigned long long left = mask;
+    for (int i = 0; i < n; ++i, left &= left - 1)
+      if (lane == i) from = __builtin_ctzll(left);
   }
+  id = __shfl(id, from);
+  const int firsts = (pg0 + from) * kPage;  // first key of the page
+  const size_t at = (size_t)(lane < n ? id : 0) * p.c.hkv + h;
+  const float kss = p.c.k_scale[at], vss = p.c.v_scale[at];
+  auto of_page = [](float x, int i) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), i));
+  };
+  // copies of this wave: half of the K (waves 0 and 1) or V (2 and 3) of a page
+  const uint32_t voff = wave < 2 ? ((n16 >> 2) * 16 + (n16 & 3)) * D + quad * 16 : n16 * kPage + quad * 16;
+  auto soff = [&](int i) {
+    const int j = (wave & 1) * IPW + i;
+    return wave < 2 ? j / (D / 64) * 4 * D + j % (D / 64) * 64 : j * 16 * kPage;
+  };
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds + wave * IPW * 1024;
   const unsigned char *pool = wave < 2 ? p.c.k : p.c.v;
   auto fetch = [&](int i) {
-    const int pid = max(__builtin_amdgcn_readlane(ids, i), 0);  // a page that is not there: any page, its keys are skipped
+    const int pid = __builtin_amdgcn_readlane(id, i);
     const uint64_t base = (uint64_t)(pool + ((size_t)pid * p.c.hkv + h) * (kPage * D));
     const u32x4 rsrc = {(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, (uint32_t)(kPage * D), 0x00020000u};
     const uint32_t to = lds0 + i % kStages * PAGE_BYTES;
 #pragma unroll
-    for (int c = 0; c < IPW; ++c) copy_to_lds(rsrc, voff[c], to + c * 1024);
+    for (int c = 0; c < IPW; ++c) copy_to_lds(rsrc, voff, soff(c), to + c * 1024);
   };
-  auto page = [&](int i) {
-    const int first = (pg0 + i) * kPage;
-    if (first > lim_hi || __builtin_amdgcn_readlane(ids, i) < 0) return;
-    const float ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, kss), i));
-    const float vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, vss), i));
-    const unsigned char *src = lds + i % kStages * PAGE_BYTES;
-    const int key0 = first + quad * 16;
-    if (first + kPage - 1 > lim_lo) {
-      wide_half<BF16, D, MT, 0, true>(w, src, lane, key0, lim_hi, ks, vs);
-      wide_half<BF16, D, MT, 1, true>(w, src, lane, key0, lim_hi, ks, vs);
-    } else {
-      wide_half<BF16, D, MT, 0, false>(w, src, lane, key0, lim_hi, ks, vs);
-      wide_half<BF16, D, MT, 1, false>(w, src, lane, key0, lim_hi, ks, vs);
+  auto stage = [&](int i) { return lds + i % kStages * PAGE_BYTES; };
+
+  typename W::Scores s;
+  typename W::Weights pf = {};
+  // Page i: its scores of half 0 are in s, the weights of the page before's half 1 in pf.
+  auto step = [&](int i, auto masked) {
+    constexpr bool MASK = decltype(masked)::value;
+    const int key = __builtin_amdgcn_readlane(firsts, i) + quad * 16;
+    const int before = __builtin_amdgcn_readlane(firsts, max(i - 1, 0)) + quad * 16;
+    const float ks = of_page(kss, i), vs = of_page(vss, i);
+    const float ks_next = of_page(kss, min(i + 1, n - 1)), vs_before = of_page(vss, max(i - 1, 0));
+    // page i + 1 is here for every wave, and all are done with page i - 2, whose place
+    // the copies of page i + 2 take
+    wait_vm<0>();
+    lds_barrier();
+    if (i + 2 < n) fetch(i + 2);
+    u32x4 k[2][C];
+    u32x2 v[DB];
+    w.template read_k<1>(stage(i), k);
+    w.template read_v<1>(stage(i + kStages - 1), v);  // page i - 1 (zeros for the first)
+    if constexpr (MASK) {
+      w.mask_scores(s, key);
+      w.mask_values(v, before + 8);
     }
+    w.raise(s, pf);
+    w.block(s, pf, k, ks, v, vs_before);
+    w.template read_k<0>(stage(i + 1), k);
+    w.template read_v<0>(stage(i), v);
+    if constexpr (MASK) {
+      w.mask_scores(s, key + 8);
+      w.mask_values(v, key);
+    }
+    w.raise(s, pf);
+    w.block(s, pf, k, ks_next, v, vs);  // past the last page: scores that nobody uses
   };
   if (n > 0) {
-    wait_vm<0>();
+    // no page before the first: zeros in its place
+    *reinterpret_cast<u32x4 *>(stage(kStages - 1) + kPage * D + threadIdx.x * 16) = u32x4{};
+    if constexpr (D == 128) *reinterpret_cast<u32x4 *>(stage(kStages - 1) + kPage * D + (256 + threadIdx.x) * 16) = u32x4{};
     fetch(0);
     if (n > 1) fetch(1);
-    for (int i = 0; i < n; ++i) {
-      if (i + 1 < n) wait_vm<IPW>();  // page i is here, page i + 1 may be on its way
-      else wait_vm<0>();
-      lds_barrier();  // for every wave, and all are done with page i - 1, whose place page i + 2 takes
-      if (i + 2 < n) fetch(i + 2);
-      page(i);
-    }
+    wait_vm<0>();
+    __syncthreads();
+    u32x4 k[2][C];
+    w.template read_k<0>(stage(0), k);
+#pragma unroll
+    for (int u = 0; u < W::UNITS; ++u) w.score_unit(u, k, of_page(kss, 0), s);
+    // pages that every row of the wave sees whole, then the others
+    const int whole = __builtin_popcountll(__ballot(lane < n && firsts + kPage - 1 <= lim_lo));
+    int i = 0;
+    for (; i < whole; ++i) step(i, std::false_type{});
+    for (; i < n; ++i) step(i, std::true_type{});
+    u32x2 v[DB];
+    w.template read_v<1>(stage(n - 1), v);
+    w.mask_values(v, __builtin_amdgcn_readlane(firsts, n - 1) + quad * 16 + 8);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) w.value_unit(db, v, of_page(vss, n - 1), pf);
   }
 
   // results
