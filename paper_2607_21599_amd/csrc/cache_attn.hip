@@ -412,9 +412,16 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(const CacheAttnLau
 // the sum and the weights in flight by a power of two, exactly. It is raised, to the
 // ceiling of the row's maximum, before a half whose scores would give a weight above
 // 2^8, so a weight is at most that.
-constexpr int kStages = 4;
+constexpr int kStages = 3;
 constexpr float kNoReference = -3e38f;  // before the first visible key
 constexpr float kSlack = 8.f;
+
+// one instruction: fmaxf on results of matrix instructions brings a second one each
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 
 template <int N>
 __device__ __forceinline__ void wait_vm() {
@@ -521,11 +528,10 @@ struct Wide {
         k[t][c] = *reinterpret_cast<const u32x4 *>(at);
       }
   }
-  template <int HALF>
-  __device__ __forceinline__ void read_v(const unsigned char *page, u32x2 (&v)[DB]) const {
+  // V of a page: of 16 features, a lane's 16 keys (the first 8 are half 0)
+  __device__ __forceinline__ void read_v(const unsigned char *page, u32x4 (&v)[DB]) const {
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
-      v[db] = *reinterpret_cast<const u32x2 *>(page + kPage * D + db * 1024 + lane * 16 + HALF * 8);
+    for (int db = 0; db < DB; ++db) v[db] = *reinterpret_cast<const u32x4 *>(page + kPage * D + db * 1024 + lane * 16);
   }
   // step u of the scores, u < UNITS
   __device__ __forceinline__ void score_unit(int u, const u32x4 (&k)[2][C], float ks, Scores &s) const {
@@ -549,8 +555,9 @@ struct Wide {
           s[mt][t] = mfma(a, q[j][mt][2 * c + e], c + e == 0 && j == T - 1 ? f32x4{} : s[mt][t]);
     }
   }
-  __device__ __forceinline__ void value_unit(int db, const u32x2 (&v)[DB], float vs, const Weights &pf) {
-    const bf16x8 a = widen(v[db][0], v[db][1], vs);
+  template <int HALF>
+  __device__ __forceinline__ void value_unit(int db, const u32x4 (&v)[DB], float vs, const Weights &pf) {
+    const bf16x8 a = widen(v[db][2 * HALF], v[db][2 * HALF + 1], vs);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -565,9 +572,9 @@ struct Wide {
       for (int i = 0; i < 8; ++i)
         if (key + i > limit[mt]) s[mt][i >> 2][i & 3] = -INFINITY;
   }
-  __device__ __forceinline__ void mask_values(u32x2 (&v)[DB], int key) const {
+  __device__ __forceinline__ void mask_values(u32x4 (&v)[DB], int key) const {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < 4; ++t) {
       const int left = lim_hi + 1 - key - 4 * t;
       const unsigned keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << 8 * left) - 1;
 #pragma unroll
@@ -580,9 +587,10 @@ struct Wide {
     float mx[MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      mx[mt] = s[mt][0][0];
-#pragma unroll
-      for (int i = 1; i < 8; ++i) mx[mt] = fmaxf(mx[mt], s[mt][i >> 2][i & 3]);
+      mx[mt] = max3(s[mt][0][0], s[mt][0][1], s[mt][0][2]);
+      mx[mt] = max3(mx[mt], s[mt][0][3], s[mt][1][0]);
+      mx[mt] = max3(mx[mt], s[mt][1][1], s[mt][1][2]);
+      mx[mt] = max3(mx[mt], s[mt][1][3], s[mt][1][3]);
       need |= mx[mt] > top[mt];
     }
     if (__builtin_expect(__ballot(need) == 0, 1)) return;
@@ -603,7 +611,8 @@ struct Wide {
   }
   // The block: weights of scores s into pf (l grows), scores of K k into s, value
   // product of the weights that pf held.
-  __device__ __forceinline__ void block(Scores &s, Weights &pf, const u32x4 (&k)[2][C], float ks, const u32x2 (&v)[DB],
+  template <int HALF>  // of v's page
+  __device__ __forceinline__ void block(Scores &s, Weights &pf, const u32x4 (&k)[2][C], float ks, const u32x4 (&v)[DB],
                                         float vs) {
     Scores next;
     float e[MT][8];
@@ -615,7 +624,7 @@ struct Wide {
         l[mt] += e[mt][step];
       }
       if (step * UNITS % 8 == 0) score_unit(step * UNITS / 8, k, ks, next);
-      if (step * DB % 8 == 0) value_unit(step * DB / 8, v, vs, pf);
+      if (step * DB % 8 == 0) value_unit<HALF>(step * DB / 8, v, vs, pf);
     }
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -731,41 +740,33 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
 
   typename W::Scores s;
   typename W::Weights pf = {};
+  u32x4 v[DB] = {};
   // Page i: its scores of half 0 are in s, the weights of the page before's half 1 in pf.
   auto step = [&](int i, auto masked) {
     constexpr bool MASK = decltype(masked)::value;
     const int key = __builtin_amdgcn_readlane(firsts, i) + quad * 16;
-    const int before = __builtin_amdgcn_readlane(firsts, max(i - 1, 0)) + quad * 16;
     const float ks = of_page(kss, i), vs = of_page(vss, i);
     const float ks_next = of_page(kss, min(i + 1, n - 1)), vs_before = of_page(vss, max(i - 1, 0));
-    // page i + 1 is here for every wave, and all are done with page i - 2, whose place
+    // page i + 1 is here for every wave, and all are done with page i - 1, whose place
     // the copies of page i + 2 take
     wait_vm<0>();
     lds_barrier();
     if (i + 2 < n) fetch(i + 2);
     u32x4 k[2][C];
-    u32x2 v[DB];
     w.template read_k<1>(stage(i), k);
-    w.template read_v<1>(stage(i + kStages - 1), v);  // page i - 1 (zeros for the first)
-    if constexpr (MASK) {
-      w.mask_scores(s, key);
-      w.mask_values(v, before + 8);
-    }
+    if constexpr (MASK) w.mask_scores(s, key);
     w.raise(s, pf);
-    w.block(s, pf, k, ks, v, vs_before);
+    w.template block<1>(s, pf, k, ks, v, vs_before);  // v: of page i - 1 (zeros for the first)
     w.template read_k<0>(stage(i + 1), k);
-    w.template read_v<0>(stage(i), v);
+    w.read_v(stage(i), v);
     if constexpr (MASK) {
       w.mask_scores(s, key + 8);
       w.mask_values(v, key);
     }
     w.raise(s, pf);
-    w.block(s, pf, k, ks_next, v, vs);  // past the last page: scores that nobody uses
+    w.template block<0>(s, pf, k, ks_next, v, vs);  // past the last page: scores that nobody uses
   };
   if (n > 0) {
-    // no page before the first: zeros in its place
-    *reinterpret_cast<u32x4 *>(stage(kStages - 1) + kPage * D + threadIdx.x * 16) = u32x4{};
-    if constexpr (D == 128) *reinterpret_cast<u32x4 *>(stage(kStages - 1) + kPage * D + (256 + threadIdx.x) * 16) = u32x4{};
     fetch(0);
     if (n > 1) fetch(1);
     wait_vm<0>();
@@ -779,11 +780,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
     int i = 0;
     for (; i < whole; ++i) step(i, std::false_type{});
     for (; i < n; ++i) step(i, std::true_type{});
-    u32x2 v[DB];
-    w.template read_v<1>(stage(n - 1), v);
-    w.mask_values(v, __builtin_amdgcn_readlane(firsts, n - 1) + quad * 16 + 8);
 #pragma unroll
-    for (int db = 0; db < DB; ++db) w.value_unit(db, v, of_page(vss, n - 1), pf);
+    for (int db = 0; db < DB; ++db) w.template value_unit<1>(db, v, of_page(vss, n - 1), pf);
   }
 
   // results
