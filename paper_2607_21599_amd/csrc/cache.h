@@ -59,7 +59,7 @@ struct CacheAttnLaunch {
   int32_t lse_stride;
   int32_t hq, group;
   int32_t max_len;
-  int32_t wide;                   // the kernel for many rows
+  int32_t wide, part_bf16;        // the kernel for many rows; its partial outputs in bf16
   int32_t n_splits, split_pages;  // pages per split (wide: at most kMaxSplitPages)
   float scale_log2;               // softmax scale * log2(e)
   int32_t n_req;

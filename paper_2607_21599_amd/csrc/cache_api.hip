@@ -199,6 +199,7 @@ daf_status_t store(bool write, const daf_attn_cfg_t *cfg, const daf_cache_t *c, 
 struct AttnPlan {
   int wide, block_rows;  // which kernel; (row, head) pairs of its row blocks
   int n_splits, split_pages;
+  int part_bf16;
   size_t lse_bytes, total;  // workspace: LSEs, then partial outputs
 };
 
@@ -235,7 +236,11 @@ AttnPlan plan_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_ca
     const size_t pairs = (a.wide ? wide_pairs(cfg, blocks, a.block_rows) : (size_t)rows->cu[rows->n] * cfg->n_q_heads) *
                          a.n_splits;
     a.lse_bytes = (pairs * sizeof(float) + 255) / 256 * 256;
-    a.total = a.lse_bytes + pairs * cfg->head_dim * sizeof(float);
+    // Partial outputs of the wide kernel in bf16 halve what it writes and the join
+    // reads. Their roundings (2^-8 each, of independent signs) average: from 8 splits on
+    // they add less than 1 / 16 to the squared error of the probabilities' and output's.
+    a.part_bf16 = a.wide && cfg->dtype == DAF_BF16 && a.n_splits >= 8;
+    a.total = a.lse_bytes + pairs * cfg->head_dim * (a.part_bf16 ? 2 : sizeof(float));
   }
   return a;
 }
@@ -280,7 +285,7 @@ daf_status_t attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, int32_t layer
       p.n_req = std::min(kMaxCacheReqs, rows->n - b0);
       p.blocks = fill(rows, b0, p.n_req, p.cu, p.blk0, &p.per_req, 
                       [&](int64_t n) { return row_blocks(cfg, n, a.block_rows); });
-      if (p.blocks < 0 || ((int64_t)c->n_kv_heads * a.n_splits + 7) * p.blocks > INT32_MAX ||
+      if (p.blocks < 0 || (int64_t)p.blocks * c->n_kv_heads * a.n_splits > INT32_MAX - 8 ||
           (int64_t)p.blocks * c->n_kv_heads * 8 > INT32_MAX)
         return fail(DAF_ERR_UNSUPPORTED, "%d rows over %d keys are too many for one call", total, max_len);
       if (pass == 0 || p.blocks == 0) continue;
@@ -297,8 +302,10 @@ daf_status_t attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, int32_t layer
       p.lse_stride = total;
       const size_t pair0 = (a.wide ? wide_pairs(cfg, block0, a.block_rows) : (size_t)row0 * cfg->n_q_heads) * a.n_splits;
       p.part_lse = a.total ? static_cast<float *>(workspace) + pair0 : nullptr;
-      p.part_o = a.total ? reinterpret_cast<float *>(static_cast<char *>(workspace) + a.lse_bytes) +
-                               pair0 * cfg->head_dim : nullptr;
+      p.part_o = a.total ? reinterpret_cast<float *>(static_cast<char *>(workspace) + a.lse_bytes +
+                                                     pair0 * cfg->head_dim * (a.part_bf16 ? 2 : sizeof(float)))
+                         : nullptr;
+      p.part_bf16 = a.part_bf16;
       p.hq = cfg->n_q_heads;
       p.group = cfg->n_q_heads / cfg->n_kv_heads;
       p.max_len = max_len;

@@ -142,14 +142,16 @@ __device__ __forceinline__ int row_limit(const CacheAttnLaunch &p, const Request
   return p.pos ? min(p.pos[r.row0 + j], r.L - 1) : r.L - r.n + j;
 }
 
+__device__ __forceinline__ u32x2 pack4(const f32x4 &x) {
+  return u32x2{__builtin_bit_cast(unsigned, bf16x2{(__bf16)x[0], (__bf16)x[1]}),
+               __builtin_bit_cast(unsigned, bf16x2{(__bf16)x[2], (__bf16)x[3]})};
+}
+
 template <bool BF16>
 __device__ __forceinline__ void store_out(const CacheAttnLaunch &p, int row, int head, int col, const float (&x)[4], int d) {
   const size_t at = ((size_t)row * p.hq + head) * d + col;
   if constexpr (BF16) {
-    u32x2 w;
-    w[0] = __builtin_bit_cast(unsigned, bf16x2{(__bf16)x[0], (__bf16)x[1]});
-    w[1] = __builtin_bit_cast(unsigned, bf16x2{(__bf16)x[2], (__bf16)x[3]});
-    *reinterpret_cast<u32x2 *>((__bf16 *)p.o + at) = w;
+    *reinterpret_cast<u32x2 *>((__bf16 *)p.o + at) = pack4(f32x4{x[0], x[1], x[2], x[3]});
   } else {
     *reinterpret_cast<f32x4 *>((float *)p.o + at) = f32x4{x[0], x[1], x[2], x[3]};
   }
@@ -382,7 +384,7 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(const CacheAttnLau
   for (int k = 32; k; k >>= 1) l += __shfl_xor(l, k);
   if ((t & 63) == 0) sh_l[t >> 6] = l;
   f32x4 x = {};
-#pragma unroll 4
+#pragma unroll 8
   for (int s = g; s < n; s += GROUPS) x += __expf(lses[s] - ref) * *reinterpret_cast<const f32x4 *>(po + (size_t)s * D + c * 4);
   sh_o[g][c] = x;
   __syncthreads();
@@ -649,15 +651,18 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
   __shared__ __align__(16) unsigned char lds[kStages * PAGE_BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n16 = lane & 15, quad = lane >> 4;
-  // the row blocks of one (head, split) read the same pages: consecutive on one XCD
-  const int groups = p.c.hkv * p.n_splits;
-  const int xcd = blockIdx.x % kXcdCount, slot = blockIdx.x / kXcdCount;
-  const int g = slot / p.blocks * kXcdCount + xcd, blk = slot % p.blocks;
-  if (g >= groups) return;
+  // the row blocks of one (head, split) read the same pages: neighbours, on one XCD but
+  // for the few at the ends of its equal share
+  const int per_xcd = gridDim.x / kXcdCount;
+  const int wg = blockIdx.x % kXcdCount * per_xcd + blockIdx.x / kXcdCount;
+  if (wg >= p.c.hkv * p.n_splits * p.blocks) return;
+  const int g = wg / p.blocks, blk = wg % p.blocks;
   const int h = g % p.c.hkv, split = g / p.c.hkv;
   const Request r = find_request(p, blk);
-  const int pages = (r.L + kPage - 1) / kPage;
   const int pg0 = split * p.split_pages;
+  // the page ids do not wait for the length
+  int id = lane < p.split_pages && pg0 + lane < p.c.max_seq_pages ? r.pages[pg0 + lane] : -1;
+  const int pages = (r.L + kPage - 1) / kPage;
   if (split > 0 && pg0 >= pages) return;  // no keys here: the join leaves this split out
   const int total = r.n * p.group;
 
@@ -700,21 +705,17 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
   w.lim_hi = __builtin_amdgcn_readfirstlane(lim_hi);
   lim_lo = __builtin_amdgcn_readfirstlane(lim_lo);
 
-  // this split's pages that are there, one per lane (split_pages <= 64): lane i takes
-  // the i-th of them
-  const int in_split = min(pg0 + p.split_pages, pages) - pg0;
-  int id = lane < in_split ? r.pages[pg0 + lane] : -1;
-  const bool there = (unsigned)id < (unsigned)p.c.n_pages;
-  const unsigned long long mask = __ballot(there);
+  // this split's pages that are there, one per lane (split_pages <= 64), in order
+  const unsigned long long mask =
+      __ballot(lane < p.split_pages && pg0 + lane < pages && (unsigned)id < (unsigned)p.c.n_pages);
   const int n = __builtin_popcountll(mask);
-  int from = 0;  // lane of the lane-th set bit
-  {
-    unsigned long long left = mask;
-    for (int i = 0; i < n; ++i, left &= left - 1)
-      if (lane == i) from = __builtin_ctzll(left);
+  int firsts = (pg0 + lane) * kPage;  // first key of the page
+  if (mask & (mask + 1)) {            // pages are missing in between: close the gaps
+    const int to = (mask >> lane) & 1 ? __builtin_popcountll(mask & ((1ull << lane) - 1)) * 4 : 252;
+    const int a = __builtin_amdgcn_ds_permute(to, id), f = __builtin_amdgcn_ds_permute(to, firsts);
+    id = a;
+    firsts = f;
   }
-  id = __shfl(id, from);
-  const int firsts = (pg0 + from) * kPage;  // first key of the page
   const size_t at = (size_t)(lane < n ? id : 0) * p.c.hkv + h;
   const float kss = p.c.k_scale[at], vss = p.c.v_scale[at];
   auto of_page = [](float x, int i) {
@@ -795,8 +796,14 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
       const size_t part = (((size_t)(blk * p.c.hkv + h) * kWaves + wave) * MT + mt) * p.n_splits + split;
       if (quad == 0) p.part_lse[part * 16 + n16] = lse;
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
-        *reinterpret_cast<f32x4 *>(p.part_o + (part * DB + db) * 256 + lane * 4) = w.o[mt][db] * inv;
+      for (int db = 0; db < DB; ++db) {
+        const f32x4 x = w.o[mt][db] * inv;
+        const size_t to = (part * DB + db) * 256 + lane * 4;
+        if (BF16 && p.part_bf16)
+          *reinterpret_cast<u32x2 *>(reinterpret_cast<__bf16 *>(p.part_o) + to) = pack4(x);
+        else
+          *reinterpret_cast<f32x4 *>(p.part_o + to) = x;
+      }
     } else if (idx < total) {
       const int row = r.row0 + idx / p.group, head = h * p.group + idx % p.group;
 #pragma unroll
@@ -810,11 +817,14 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
   }
 }
 
-// Join the splits of one tile of 16 pairs; a wave takes DB / 4 blocks of 16 features,
-// a lane the same pair and features as in the kernel above.
+// Join the splits of one tile of 16 pairs. The waves take the splits in turn, with
+// everything of a split in flight at once, and join their sums through LDS; a lane has
+// the same pair and features as in the kernel above.
 template <bool BF16, int D, int MT>
 __global__ __launch_bounds__(kThreads) void cache_wide_join_kernel(const CacheAttnLaunch p) {
   constexpr int DB = D / 16, PER = DB / kWaves;
+  __shared__ f32x4 sh_x[kWaves][DB][64];
+  __shared__ float sh_m[kWaves][16], sh_l[kWaves][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n16 = lane & 15, quad = lane >> 4;
   const int tile = blockIdx.x % (kWaves * MT), rest = blockIdx.x / (kWaves * MT);
   const int h = rest % p.c.hkv, blk = rest / p.c.hkv;
@@ -824,28 +834,55 @@ __global__ __launch_bounds__(kThreads) void cache_wide_join_kernel(const CacheAt
   const int pages = (r.L + kPage - 1) / kPage;
   const int n = max(1, (pages + p.split_pages - 1) / p.split_pages);  // splits that hold keys
   const size_t part = (size_t)blockIdx.x * p.n_splits;
-  const float *lse = p.part_lse + part * 16 + n16;
-  float m = -INFINITY;
-#pragma unroll 8
-  for (int s = 0; s < n; ++s) m = fmaxf(m, lse[s * 16]);
-  const float ref = m == -INFINITY ? 0.f : m;
-  f32x4 x[PER] = {};
-  float l = 0.f;
-#pragma unroll 4
-  for (int s = 0; s < n; ++s) {
-    const float wt = __expf(lse[s * 16] - ref);
-    l += wt;
+  f32x4 x[DB] = {};
+  float m = -INFINITY, l = 0.f;
+  for (int s = wave; s < n; s += kWaves) {
+    const float lse = p.part_lse[(part + s) * 16 + n16];
+    f32x4 y[DB];
+    if (BF16 && p.part_bf16) {
 #pragma unroll
-    for (int k = 0; k < PER; ++k)
-      x[k] += wt * *reinterpret_cast<const f32x4 *>(p.part_o + ((part + s) * DB + wave * PER + k) * 256 + lane * 4);
+      for (int db = 0; db < DB; ++db) {
+        const u32x2 w = *reinterpret_cast<const u32x2 *>(reinterpret_cast<const __bf16 *>(p.part_o) +
+                                                        ((part + s) * DB + db) * 256 + lane * 4);
+        y[db] = f32x4{__builtin_bit_cast(float, w[0] << 16), __builtin_bit_cast(float, w[0] & 0xffff0000u),
+                      __builtin_bit_cast(float, w[1] << 16), __builtin_bit_cast(float, w[1] & 0xffff0000u)};
+      }
+    } else {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        y[db] = *reinterpret_cast<const f32x4 *>(p.part_o + ((part + s) * DB + db) * 256 + lane * 4);
+    }
+    if (lse == -INFINITY) continue;  // of a row that sees no key there
+    const float to = fmaxf(m, lse), a = __expf(m - to), wt = __expf(lse - to);
+    m = to;
+    l = l * a + wt;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) x[db] = x[db] * a + y[db] * wt;
   }
+#pragma unroll
+  for (int db = 0; db < DB; ++db) sh_x[wave][db][lane] = x[db];
+  if (quad == 0) sh_m[wave][n16] = m, sh_l[wave][n16] = l;
+  __syncthreads();
   if (idx >= total) return;
+  m = fmaxf(fmaxf(sh_m[0][n16], sh_m[1][n16]), fmaxf(sh_m[2][n16], sh_m[3][n16]));
+  float w[kWaves];
+  l = 0.f;
+#pragma unroll
+  for (int k = 0; k < kWaves; ++k) {
+    w[k] = sh_m[k][n16] == -INFINITY ? 0.f : __expf(sh_m[k][n16] - m);
+    l += w[k] * sh_l[k][n16];
+  }
   const float inv = l > 0.f ? 1.f / l : 0.f;
   const int row = r.row0 + idx / p.group, head = h * p.group + idx % p.group;
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
-    const float y[4] = {x[k][0] * inv, x[k][1] * inv, x[k][2] * inv, x[k][3] * inv};
-    store_out<BF16>(p, row, head, (wave * PER + k) * 16 + quad * 4, y, D);
+    const int db = wave * PER + k;
+    f32x4 v = sh_x[0][db][lane] * w[0];
+#pragma unroll
+    for (int j = 1; j < kWaves; ++j) v += sh_x[j][db][lane] * w[j];
+    v *= inv;
+    const float y[4] = {v[0], v[1], v[2], v[3]};
+    store_out<BF16>(p, row, head, db * 16 + quad * 4, y, D);
   }
   if (wave == 0 && quad == 0 && p.lse) p.lse[(size_t)head * p.lse_stride + row] = l > 0.f ? m + __logf(l) : -INFINITY;
 }
@@ -855,8 +892,8 @@ hipError_t launch(const CacheAttnLaunch &p, hipStream_t st) {
   constexpr int MT = BF16 ? kCacheWideRows / 64 : kCacheWideRowsF32 / 64;
   const int jobs = p.blocks * p.c.hkv;
   if (p.wide) {
-    const int groups = p.c.hkv * p.n_splits;
-    cache_wide_kernel<BF16, D, MT><<<(groups + kXcdCount - 1) / kXcdCount * kXcdCount * p.blocks, kThreads, 0, st>>>(p);
+    const int wgs = (jobs * p.n_splits + kXcdCount - 1) / kXcdCount * kXcdCount;
+    cache_wide_kernel<BF16, D, MT><<<wgs, kThreads, 0, st>>>(p);
   } else {
     cache_attn_kernel<BF16, D><<<jobs * p.n_splits, kThreads, 0, st>>>(p);
   }
