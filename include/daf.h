@@ -471,12 +471,11 @@ size_t daf_cache_attn_workspace_size(const daf_attn_cfg_t *cfg,
  * hold anything, NaN included; all others must be finite.
  *   max_len: a HOST bound on the sequences' len (at most max_seq_pages * 64) that
  * the launch is planned for; len is read on the device, at most max_len counts.
- *   Softmax and sums in fp32; the codes enter the products exactly. bf16: so does
- * q, but features below 2^-10 of a row's largest may be off by 2^-17 of that one
- * (q as two 8-bit terms, where a request has more than a few rows); probabilities
- * are rounded to bf16 for the value product; the row's sum and the LSE are those of
- * the unrounded ones. fp32: q and the probabilities enter as three bf16 terms each
- * (24 bits). Sums hold probabilities of at most 2^8, so |V| must stay below 2^100.
+ *   Softmax and sums in fp32; the codes, and q in bf16, enter the products
+ * exactly. bf16: probabilities are rounded to bf16 for the value product; the
+ * row's sum and the LSE are those of the unrounded ones. fp32: q and the
+ * probabilities enter as three bf16 terms each (24 bits). Sums hold probabilities
+ * of at most 2^8, so |V| must stay below 2^100.
  *   workspace: at least daf_cache_attn_workspace_size bytes, 16-byte aligned,
  * contents undefined after the call. */
 daf_status_t daf_cache_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *cache,

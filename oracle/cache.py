@@ -96,12 +96,11 @@ class CacheOracle:
 
     def attn(self, layer, cu, seq, pos, q, scale):
         """o [rows][Hq][D], lse [Hq][rows], and what bounds of the rounding errors take:
-        sum of weights * |v|, and of the visible keys the largest sum |q| |k| * scale and
-        the largest max |q| * sum |k| * scale."""
+        sum of weights * |v| and the largest sum |q| |k| * scale of a visible key."""
         rows, hq, d = q.shape
         heads = self.code["k"].shape[2]
         o, mean = np.zeros((rows, hq, d)), np.zeros((rows, hq, d))
-        lse, size, wide = np.full((hq, rows), -np.inf), np.zeros((hq, rows)), np.zeros((hq, rows))
+        lse, size = np.full((hq, rows), -np.inf), np.zeros((hq, rows))
         for b, s, at in self.positions(cu, seq, pos):
             L = int(self.len[s])
             pages = [self.page(s, i) for i in range(-(-L // PAGE))]
@@ -125,8 +124,7 @@ class CacheOracle:
                         mean[r, hh] = w @ np.abs(vv[see]) / w.sum()
                         lse[hh, r] = m + math.log(w.sum())
                         size[hh, r] = (np.abs(kk[see]) @ np.abs(q[r, hh])).max() * scale
-                        wide[hh, r] = np.abs(kk[see]).sum(1).max() * np.abs(q[r, hh]).max() * scale
-        return o, lse, mean, size, wide
+        return o, lse, mean, size
 
     # -- pages ---------------------------------------------------------------------
     def free_ids(self):

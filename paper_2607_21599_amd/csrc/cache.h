@@ -52,15 +52,17 @@ struct CacheAttnLaunch {
   const void *q;
   void *o;
   float *lse;       // nullable; [hq][lse_stride] at the launch's first row
-  // n_splits > 1: normalised partial outputs and their LSE, [row][hq][n_splits] of d
-  // values; wide: [row block][hkv][tile of 16 pairs][n_splits] of d / 16 x 64 lanes x 4
-  // values in the order of the accumulators, and of 16 LSEs
+  // n_splits > 1: normalised partial outputs and their LSE. Few rows: [hkv][n_splits]
+  // [2][16 pairs] of d values; wide: [row block][hkv][tile of 16 pairs][n_splits] of
+  // d / 16 x 64 lanes x 4 values in the order of the accumulators, and of 16 LSEs
   float *part_o, *part_lse;
+  int32_t *line;    // few rows: the requests' first pages in the line, their pages, a piece's
   int32_t lse_stride;
   int32_t hq, group;
   int32_t max_len;
-  int32_t wide, part_bf16;        // the kernel for many rows; its partial outputs in bf16
-  int32_t n_splits, split_pages;  // pages per split (wide: at most kMaxSplitPages)
+  int32_t wide;                   // the kernel for many rows
+  int32_t n_splits;               // wide: splits of a row block; else workgroups per head
+  int32_t split_pages;            // wide: pages per split, at most kMaxSplitPages
   float scale_log2;               // softmax scale * log2(e)
   int32_t n_req;
   int32_t blocks;                 // row blocks of all requests
@@ -72,6 +74,8 @@ static_assert(sizeof(CacheAttnLaunch) < 4096, "kernel arguments must fit 4 KiB")
 // (row, head) pairs of a row block: few rows, many rows in bf16 and in fp32
 constexpr int kCacheAttnRows = 16, kCacheWideRows = 128, kCacheWideRowsF32 = 64;
 constexpr int kMaxSplitPages = 64;
+constexpr size_t kLineBytes = (2 * kMaxCacheReqs + 64) * sizeof(int32_t);
+constexpr int kMinPiece = 8;  // few rows: pages per workgroup, two for each wave
 hipError_t launch_cache_attn(bool bf16, const CacheAttnLaunch &p, hipStream_t st);
 
 // Page calls.

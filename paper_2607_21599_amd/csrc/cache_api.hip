@@ -199,8 +199,7 @@ daf_status_t store(bool write, const daf_attn_cfg_t *cfg, const daf_cache_t *c, 
 struct AttnPlan {
   int wide, block_rows;  // which kernel; (row, head) pairs of its row blocks
   int n_splits, split_pages;
-  int part_bf16;
-  size_t lse_bytes, total;  // workspace: LSEs, then partial outputs
+  size_t lse_bytes, total;  // workspace: LSEs (and few rows' line), then partial outputs
 };
 
 int64_t row_blocks(const daf_attn_cfg_t *cfg, int64_t n, int block_rows) {
@@ -222,25 +221,25 @@ AttnPlan plan_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_ca
   for (int b = 0; b < rows->n; ++b) blocks += row_blocks(cfg, rows->cu[b + 1] - rows->cu[b], a.block_rows);
   const int64_t pages = std::max<int64_t>(1, ((int64_t)max_len + kPage - 1) / kPage);
   const int64_t jobs = std::max<int64_t>(1, blocks * c->n_kv_heads);
-  int64_t splits;
   if (a.wide) {
-    splits = std::max<int64_t>(std::max<int64_t>(1, 512 / jobs), (pages + kMaxSplitPages - 1) / kMaxSplitPages);
+    int64_t splits = std::max<int64_t>(std::max<int64_t>(1, 512 / jobs), (pages + kMaxSplitPages - 1) / kMaxSplitPages);
     splits = std::min(splits, (pages + 1) / 2);
-  } else {  // a page at least for each of a workgroup's four waves
-    splits = std::max<int64_t>(1, std::min((512 + jobs - 1) / jobs, (pages + 3) / 4));
-    if (pages <= 16) splits = 1;
+    a.split_pages = (int)((pages + splits - 1) / splits);
+    a.n_splits = (int)((pages + a.split_pages - 1) / a.split_pages);
+  } else {
+    // Workgroups per head on the line of all row blocks' pages. Up to 16 pages, four for
+    // each wave, are a workgroup's own: a join would take longer.
+    a.n_splits = 1;
+    if (pages > 16) {
+      const int64_t line = std::min<int64_t>(blocks, INT32_MAX) * pages;
+      a.n_splits = (int)std::max<int64_t>(2, std::min<int64_t>(512 / c->n_kv_heads, (line + kMinPiece - 1) / kMinPiece));
+    }
   }
-  a.split_pages = (int)((pages + splits - 1) / splits);
-  a.n_splits = (int)((pages + a.split_pages - 1) / a.split_pages);
   if (a.n_splits > 1) {
-    const size_t pairs = (a.wide ? wide_pairs(cfg, blocks, a.block_rows) : (size_t)rows->cu[rows->n] * cfg->n_q_heads) *
-                         a.n_splits;
-    a.lse_bytes = (pairs * sizeof(float) + 255) / 256 * 256;
-    // Partial outputs of the wide kernel in bf16 halve what it writes and the join
-    // reads. Their roundings (2^-8 each, of independent signs) average: from 8 splits on
-    // they add less than 1 / 16 to the squared error of the probabilities' and output's.
-    a.part_bf16 = a.wide && cfg->dtype == DAF_BF16 && a.n_splits >= 8;
-    a.total = a.lse_bytes + pairs * cfg->head_dim * (a.part_bf16 ? 2 : sizeof(float));
+    const size_t pairs = a.wide ? wide_pairs(cfg, blocks, a.block_rows) * a.n_splits
+                                : (size_t)a.n_splits * c->n_kv_heads * 2 * kCacheAttnRows;
+    a.lse_bytes = (pairs * sizeof(float) + 255) / 256 * 256 + (a.wide ? 0 : kLineBytes);
+    a.total = a.lse_bytes + pairs * cfg->head_dim * sizeof(float);
   }
   return a;
 }
@@ -285,8 +284,10 @@ daf_status_t attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, int32_t layer
       p.n_req = std::min(kMaxCacheReqs, rows->n - b0);
       p.blocks = fill(rows, b0, p.n_req, p.cu, p.blk0, &p.per_req, 
                       [&](int64_t n) { return row_blocks(cfg, n, a.block_rows); });
-      if (p.blocks < 0 || (int64_t)p.blocks * c->n_kv_heads * a.n_splits > INT32_MAX - 8 ||
-          (int64_t)p.blocks * c->n_kv_heads * 8 > INT32_MAX)
+      const int64_t pages = ((int64_t)max_len + kPage - 1) / kPage;
+      // grids, and few rows' line of pages with a piece of it more
+      if (p.blocks < 0 || (int64_t)p.blocks * c->n_kv_heads * (a.wide ? std::max(a.n_splits, 8) : 1) > INT32_MAX - 8 ||
+          (!a.wide && (int64_t)p.blocks * std::max<int64_t>(pages, 1) > INT32_MAX / 2))
         return fail(DAF_ERR_UNSUPPORTED, "%d rows over %d keys are too many for one call", total, max_len);
       if (pass == 0 || p.blocks == 0) continue;
       const int64_t row0 = rows->cu[b0];
@@ -300,12 +301,13 @@ daf_status_t attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, int32_t layer
       p.o = const_cast<char *>(rows_at(o, row0, row_bytes));
       p.lse = lse ? lse + row0 : nullptr;
       p.lse_stride = total;
-      const size_t pair0 = (a.wide ? wide_pairs(cfg, block0, a.block_rows) : (size_t)row0 * cfg->n_q_heads) * a.n_splits;
+      // few rows: each launch's join is done with the places before the next one's kernel
+      const size_t pair0 = a.wide ? wide_pairs(cfg, block0, a.block_rows) * a.n_splits : 0;
       p.part_lse = a.total ? static_cast<float *>(workspace) + pair0 : nullptr;
-      p.part_o = a.total ? reinterpret_cast<float *>(static_cast<char *>(workspace) + a.lse_bytes +
-                                                     pair0 * cfg->head_dim * (a.part_bf16 ? 2 : sizeof(float)))
-                         : nullptr;
-      p.part_bf16 = a.part_bf16;
+      p.part_o = a.total ? reinterpret_cast<float *>(static_cast<char *>(workspace) + a.lse_bytes) +
+                               pair0 * cfg->head_dim : nullptr;
+      p.line = a.total && !a.wide ? reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + a.lse_bytes - kLineBytes)
+                                  : nullptr;
       p.hq = cfg->n_q_heads;
       p.group = cfg->n_q_heads / cfg->n_kv_heads;
       p.max_len = max_len;

@@ -18,8 +18,9 @@
 //    of keys 16 g .. 16 g + 15 of row lane % 16, which is how the second product
 //    wants them, and V^T, stored transposed, is read as 16 consecutive keys.
 //  * fp32: q and the probabilities enter as three bf16 terms each.
-// The four waves of a workgroup take the pages of its split in turn and join their
-// (m, sum, O) through LDS; splits are joined by a second kernel.
+// Few rows: the four waves of a workgroup take its pages in turn and join their (m,
+// sum, O) through LDS; bound by the pages' bytes. Many rows: below. What workgroups
+// share of a row block is joined by a second kernel.
 #include <math.h>
 
 #include <type_traits>
@@ -32,7 +33,6 @@ namespace {
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
@@ -110,12 +110,28 @@ __device__ __forceinline__ void load_q(const CacheAttnLaunch &p, size_t at, int 
   }
 }
 
+// one instruction: fmaxf on results of matrix instructions brings a second one each
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
 struct Request {
   int b, block;      // request of the launch and row block in it
   int row0, n;       // its rows
   int L;             // tokens of its sequence
   const int32_t *pages;
 };
+
+// The b < n with prefix[b] <= at < prefix[b + 1]: every lane looks at one of each 64
+// (a binary search would wait for a load per step).
+__device__ __forceinline__ int find_in(const int32_t *prefix, int n, int at) {
+  const int lane = threadIdx.x & 63;
+  int b = 0;
+  for (int i = 0; i < n; i += 64) b += __builtin_popcountll(__ballot(i + lane < n && prefix[i + lane + 1] <= at));
+  return b;
+}
 
 __device__ __forceinline__ Request find_request(const CacheAttnLaunch &p, int blk) {
   Request r;
@@ -124,8 +140,7 @@ __device__ __forceinline__ Request find_request(const CacheAttnLaunch &p, int bl
     b = blk / p.per_req;
     r.block = blk - b * p.per_req;
   } else {
-    for (int step = kMaxCacheReqs / 2; step; step >>= 1)
-      if (b + step < p.n_req && p.blk0[b + step] <= blk) b += step;
+    b = find_in(p.blk0, p.n_req, blk);
     r.block = blk - p.blk0[b];
   }
   r.b = b;
@@ -165,27 +180,37 @@ struct Frags {
   float ks, vs;
 };
 
+// ---- few rows --------------------------------------------------------------------
+template <int D>
+struct FewShared {
+  float o[kWaves][kRows][D + 4];
+  float m[kWaves][kRows], l[kWaves][kRows];
+};
+
+// Row block r.block of a request over the pages pg0 .. pg_end - 1 of its sequence, by
+// the whole workgroup. Results go to the output, or with `slot` >= 0 to that place
+// among the partial ones.
 template <bool BF16, int D>
-__global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(const CacheAttnLaunch p) {
+__device__ __forceinline__ void few_rows(const CacheAttnLaunch &p, FewShared<D> &sh, const Request &r, int h, int pg0,
+                                         int pg_end, int slot) {
   constexpr int T = BF16 ? 1 : 3, DS = D / 32, DB = D / 16;
-  __shared__ float sh_o[kWaves][kRows][D + 4];
-  __shared__ float sh_m[kWaves][kRows], sh_l[kWaves][kRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n16 = lane & 15, quad = lane >> 4;
-  const int blk = blockIdx.x % p.blocks, rest = blockIdx.x / p.blocks;
-  const int h = rest % p.c.hkv, split = rest / p.c.hkv;
-  const Request r = find_request(p, blk);
-  const int pages = (r.L + kPage - 1) / kPage;
-  const int pg0 = split * p.split_pages;
-  if (split > 0 && pg0 >= pages) return;  // no keys here: the join leaves this split out
+  // the ids of this wave's pages (pg0 + wave + 4 i), 64 at a time in the lanes; they do
+  // not wait for the length
+  auto load_ids = [&](int i) {
+    const int64_t pg = (int64_t)pg0 + wave + 4 * (i + lane);
+    return pg < p.c.max_seq_pages ? r.pages[pg] : -1;
+  };
+  int ids = load_ids(0), ids_at = 0;
   const int total = r.n * p.group;
   const int idx = r.block * kRows + n16;      // this lane's (row, head) pair
   const int idc = min(idx, total - 1);        // pairs past the end repeat the last one
   const int row = idc / p.group, head = h * p.group + idc % p.group;
-  const int limit = row_limit(p, r, row);
   bf16x8 qf[T][DS];
   load_q<BF16, D>(p, ((size_t)(r.row0 + row) * p.hq + head) * D, quad,
                   [&](int j, int ds, const bf16x8 &x) { qf[j][ds] = x; });
+  const int limit = row_limit(p, r, row);
   // range of limits over the block's rows
   int lim_hi = limit, lim_lo = limit;
 #pragma unroll
@@ -195,18 +220,15 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(const CacheAttn
   }
   lim_hi = __builtin_amdgcn_readfirstlane(lim_hi);
   lim_lo = __builtin_amdgcn_readfirstlane(lim_lo);
-  const int pg1 = min(min(pg0 + p.split_pages, pages), (lim_hi >> 6) + 1);  // lim_hi < 0: none
+  const int pg1 = min(min(pg_end, (r.L + kPage - 1) / kPage), (lim_hi >> 6) + 1);  // lim_hi < 0: none
 
   f32x4 o[DB] = {};
   float m_run = -INFINITY, l_run = 0.f;
 
-  // the page ids of this wave, 64 at a time in the lanes
-  int ids = -1, ids_at = -1;
-  auto page_id = [&](int i) {  // i-th page of this wave, pg0 + wave + 4 i
-    if (ids_at < 0 || i >= ids_at + 64) {
+  auto page_id = [&](int i) {  // i-th page of this wave
+    if (i >= ids_at + 64) {
       ids_at = i;
-      const int pg = pg0 + wave + 4 * (i + lane);
-      ids = pg < pg1 ? r.pages[pg] : -1;
+      ids = load_ids(i);
     }
     return __builtin_amdgcn_readlane(ids, i - ids_at);
   };
@@ -261,11 +283,14 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(const CacheAttn
         }
       }
     }
-    float mx = s[0][0];
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[t][i]);
+    float mx = max3(s[0][0], s[0][1], s[0][2]);
+    mx = max3(mx, s[0][3], s[1][0]);
+    mx = max3(mx, s[1][1], s[1][2]);
+    mx = max3(mx, s[1][3], s[2][0]);
+    mx = max3(mx, s[2][1], s[2][2]);
+    mx = max3(mx, s[2][3], s[3][0]);
+    mx = max3(mx, s[3][1], s[3][2]);
+    mx = fmaxf(mx, s[3][3]);
     const float m_new = fmaxf(m_run, row_max(mx) * p.scale_log2);
     if (__ballot(m_new > m_run)) {
       const float alpha = m_new > m_run ? exp2_(m_run - m_new) : 1.f;
@@ -311,21 +336,21 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(const CacheAttn
 
   // join the waves
   l_run = row_sum(l_run);
-  if (quad == 0) sh_m[wave][n16] = m_run, sh_l[wave][n16] = l_run;
+  if (quad == 0) sh.m[wave][n16] = m_run, sh.l[wave][n16] = l_run;
 #pragma unroll
-  for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4 *>(&sh_o[wave][n16][db * 16 + quad * 4]) = o[db];
+  for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4 *>(&sh.o[wave][n16][db * 16 + quad * 4]) = o[db];
   __syncthreads();
   const int rr = threadIdx.x >> 4, c0 = threadIdx.x & 15;  // 16 lanes per pair
   const int out = r.block * kRows + rr;
   if (out >= total) return;
   const int orow = r.row0 + out / p.group, ohead = h * p.group + out % p.group;
-  float m = sh_m[0][rr], w[kWaves], l = 0.f;
+  float m = sh.m[0][rr], w[kWaves], l = 0.f;
 #pragma unroll
-  for (int k = 1; k < kWaves; ++k) m = fmaxf(m, sh_m[k][rr]);
+  for (int k = 1; k < kWaves; ++k) m = fmaxf(m, sh.m[k][rr]);
 #pragma unroll
   for (int k = 0; k < kWaves; ++k) {
-    w[k] = sh_m[k][rr] == -INFINITY ? 0.f : exp2_(sh_m[k][rr] - m);
-    l += w[k] * sh_l[k][rr];
+    w[k] = sh.m[k][rr] == -INFINITY ? 0.f : exp2_(sh.m[k][rr] - m);
+    l += w[k] * sh.l[k][rr];
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
   const float lse = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
@@ -334,64 +359,181 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(const CacheAttn
     float x[4] = {};
 #pragma unroll
     for (int k = 0; k < kWaves; ++k) {
-      const f32x4 v = *reinterpret_cast<const f32x4 *>(&sh_o[k][rr][c]);
+      const f32x4 v = *reinterpret_cast<const f32x4 *>(&sh.o[k][rr][c]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(w[k], v[e], x[e]);
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] *= inv;
-    if (p.n_splits == 1)
+    if (slot < 0)
       store_out<BF16>(p, orow, ohead, c, x, D);
     else
-      *reinterpret_cast<f32x4 *>(p.part_o + (((size_t)orow * p.hq + ohead) * p.n_splits + split) * D + c) =
-          f32x4{x[0], x[1], x[2], x[3]};
+      *reinterpret_cast<f32x4 *>(p.part_o + ((size_t)slot * kRows + rr) * D + c) = f32x4{x[0], x[1], x[2], x[3]};
   }
   if (c0 == 0) {
-    if (p.n_splits > 1) p.part_lse[((size_t)orow * p.hq + ohead) * p.n_splits + split] = lse;
+    if (slot >= 0) p.part_lse[slot * kRows + rr] = lse;
     else if (p.lse) p.lse[(size_t)ohead * p.lse_stride + orow] = lse;
   }
 }
 
-// Join the splits of one (row, head): o = sum_s e^(lse_s - lse) o_s. Eight groups of
-// 32 lanes take the splits in turn.
+// Short sequences: a workgroup per row block and head.
 template <bool BF16, int D>
-__global__ __launch_bounds__(kThreads) void cache_join_kernel(const CacheAttnLaunch p) {
-  constexpr int LP = D / 4, GROUPS = kThreads / LP;  // lanes per partial row
+__global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(const CacheAttnLaunch p) {
+  __shared__ FewShared<D> sh;
+  const Request r = find_request(p, blockIdx.x % p.blocks);
+  few_rows<BF16, D>(p, sh, r, blockIdx.x / p.blocks, 0, INT32_MAX, -1);
+}
+
+// Long ones: the row blocks' pages, one block after the other, make one line per head,
+// of which every workgroup takes an equal piece, whatever the lengths are on the device
+// (a batch is planned for the longest that it may have, and a captured one grows). A
+// workgroup's first and last row block may be shared with its neighbours: their
+// partial results have two places per workgroup, 0 for a block that did not begin
+// in it and 1 for one that does not end in it.
+//
+// The line lies in the lanes of every wave: lane i has requests 4 i .. 4 i + 3.
+struct Line {
+  int first;               // of the lane's requests' pages in the line
+  int units[4], L[4], seq[4];
+  int end, piece;          // pages of the line, and of a workgroup
+};
+static_assert(kMaxCacheReqs == 4 * 64, "four requests per lane");
+
+__device__ __forceinline__ int line_pages(int L) { return max(1, (L + kPage - 1) / kPage); }
+
+__device__ __forceinline__ Line build_line(const CacheAttnLaunch &p) {
+  Line s;
+  const int lane = threadIdx.x & 63;
+  int sum = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int b = 4 * lane + j;
+    s.seq[j] = b >= p.n_req ? -1 : p.seq ? p.seq[b] : b;
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) s.L[j] = min(seq_len(p.c.len, p.c.n_seqs, p.c.max_seq_pages, s.seq[j]), p.max_len);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int b = 4 * lane + j;
+    s.units[j] = b < p.n_req ? (p.blk0[b + 1] - p.blk0[b]) * line_pages(s.L[j]) : 0;
+    sum += s.units[j];
+  }
+  int upto = sum;
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) {
+    const int y = __shfl_up(upto, k);
+    if (lane >= k) upto += y;
+  }
+  s.first = upto - sum;
+  s.end = __builtin_amdgcn_readlane(upto, 63);
+  s.piece = max(kMinPiece, (s.end + p.n_splits - 1) / p.n_splits);
+  return s;
+}
+
+template <bool BF16, int D>
+__global__ __launch_bounds__(kThreads, 2) void cache_line_kernel(const CacheAttnLaunch p) {
+  __shared__ FewShared<D> sh;
+  const int lane = threadIdx.x & 63;
+  const int h = blockIdx.x % p.c.hkv, k = blockIdx.x / p.c.hkv;
+  const Line line = build_line(p);
+  if (blockIdx.x == 0 && threadIdx.x < 64) {  // for the join
+    int first = line.first;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      p.line[4 * lane + j] = first;
+      p.line[kMaxCacheReqs + 4 * lane + j] = line_pages(line.L[j]);
+      first += line.units[j];
+    }
+    if (lane == 0) p.line[2 * kMaxCacheReqs] = line.piece;
+  }
+  int at = k * line.piece;  // the host keeps n_splits * piece within 32 bits
+  const int to = min(at + line.piece, line.end);
+  while (at < to) {
+    // the lane, then the request of the page `at`
+    const int last = __builtin_popcountll(__ballot(line.first <= at)) - 1;
+    int first = __builtin_amdgcn_readlane(line.first, last), j = 0, L = __builtin_amdgcn_readlane(line.L[0], last),
+        seq = __builtin_amdgcn_readlane(line.seq[0], last);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      const int next = first + __builtin_amdgcn_readlane(line.units[i], last);
+      if (j == i && at >= next) {
+        first = next;
+        j = i + 1;
+        L = __builtin_amdgcn_readlane(line.L[i + 1], last);
+        seq = __builtin_amdgcn_readlane(line.seq[i + 1], last);
+      }
+    }
+    Request r;
+    r.b = 4 * last + j;
+    r.L = L;
+    const int pages = line_pages(L), rest = at - first;
+    r.block = rest / pages;
+    r.row0 = p.cu[r.b];
+    r.n = p.cu[r.b + 1] - r.row0;
+    r.pages = p.c.table + (int64_t)((unsigned)seq < (unsigned)p.c.n_seqs ? seq : 0) * p.c.max_seq_pages;
+    const int pg0 = rest - r.block * pages, pg_end = min(pages, pg0 + to - at);
+    const int slot = pg0 == 0 && pg_end == pages ? -1 : (h * p.n_splits + k) * 2 + (pg0 == 0);
+    few_rows<BF16, D>(p, sh, r, h, pg0, pg_end, slot);
+    at += pg_end - pg0;
+    __syncthreads();  // sh is free
+  }
+}
+
+// Join the pieces of one (row, head): o = sum_s e^(lse_s - lse) o_s. Groups of D / 4
+// lanes take the pieces in turn, four in flight, and join their sums through LDS.
+template <bool BF16, int D>
+__global__ __launch_bounds__(kThreads) void cache_line_join_kernel(const CacheAttnLaunch p) {
+  constexpr int LP = D / 4, GROUPS = kThreads / LP;
   __shared__ f32x4 sh_o[GROUPS][LP];
-  __shared__ float sh_m[kWaves], sh_l[kWaves];
+  __shared__ float sh_m[GROUPS], sh_l[GROUPS];
   const int t = threadIdx.x, g = t / LP, c = t % LP;
   const int row = blockIdx.x / p.hq, head = blockIdx.x % p.hq;
-  int b = 0;
-  for (int step = kMaxCacheReqs / 2; step; step >>= 1)
-    if (b + step < p.n_req && p.cu[b + step] <= row) b += step;
-  const int seq = p.seq ? p.seq[b] : b;
-  const int L = min(seq_len(p.c.len, p.c.n_seqs, p.c.max_seq_pages, seq), p.max_len);
-  const int pages = (L + kPage - 1) / kPage;
-  const int n = max(1, (pages + p.split_pages - 1) / p.split_pages);  // splits that hold keys
-  const float *lses = p.part_lse + (size_t)blockIdx.x * p.n_splits;
-  const float *po = p.part_o + (size_t)blockIdx.x * p.n_splits * D;
-  float m = -INFINITY;
-  for (int s = t; s < n; s += kThreads) m = fmaxf(m, lses[s]);
-#pragma unroll
-  for (int k = 32; k; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
-  if ((t & 63) == 0) sh_m[t >> 6] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(sh_m[0], sh_m[1]), fmaxf(sh_m[2], sh_m[3]));
-  const float ref = m == -INFINITY ? 0.f : m;
-  float l = 0.f;
-  for (int s = t; s < n; s += kThreads) l += __expf(lses[s] - ref);
-#pragma unroll
-  for (int k = 32; k; k >>= 1) l += __shfl_xor(l, k);
-  if ((t & 63) == 0) sh_l[t >> 6] = l;
+  const int piece = p.line[2 * kMaxCacheReqs];
+  const int b = find_in(p.cu, p.n_req, row);
+  const int h = head / p.group, pair = (row - p.cu[b]) * p.group + head % p.group;
+  const int pages = p.line[kMaxCacheReqs + b], from = p.line[b] + pair / kRows * pages;
+  const int k0 = from / piece, k1 = (from + pages - 1) / piece;
+  if (k0 == k1) return;  // in one piece: written already
+  const int n = k1 - k0 + 1;
+  // piece s of the n: the first one's place is its workgroup's second
+  auto at = [&](int s) { return (size_t)((h * p.n_splits + k0 + s) * 2 + (s == 0)) * kRows + pair % kRows; };
+  float m = -INFINITY, l = 0.f;
   f32x4 x = {};
-#pragma unroll 8
-  for (int s = g; s < n; s += GROUPS) x += __expf(lses[s] - ref) * *reinterpret_cast<const f32x4 *>(po + (size_t)s * D + c * 4);
+  for (int s0 = g; s0 < n; s0 += 4 * GROUPS) {
+    float lse[4];
+    f32x4 y[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int s = s0 + j * GROUPS;
+      lse[j] = s < n ? p.part_lse[at(s)] : -INFINITY;
+      y[j] = s < n ? *reinterpret_cast<const f32x4 *>(p.part_o + at(s) * D + c * 4) : f32x4{};
+    }
+    const float to = fmaxf(m, fmaxf(fmaxf(lse[0], lse[1]), fmaxf(lse[2], lse[3])));
+    if (to == -INFINITY) continue;  // a row that sees no key there
+    const float a = __expf(m - to);
+    m = to;
+    l *= a;
+    x *= a;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float w = __expf(lse[j] - to);
+      l += w;
+      x += w * y[j];
+    }
+  }
   sh_o[g][c] = x;
+  if (c == 0) sh_m[g] = m, sh_l[g] = l;
   __syncthreads();
   if (g) return;
-#pragma unroll
-  for (int k = 1; k < GROUPS; ++k) x += sh_o[k][c];
-  l = (sh_l[0] + sh_l[1]) + (sh_l[2] + sh_l[3]);
+  for (int k = 1; k < GROUPS; ++k) m = fmaxf(m, sh_m[k]);
+  const float ref = m == -INFINITY ? 0.f : m;
+  l = 0.f;
+  x = f32x4{};
+  for (int k = 0; k < GROUPS; ++k) {
+    const float w = __expf(sh_m[k] - ref);
+    l += w * sh_l[k];
+    x += w * sh_o[k][c];
+  }
   const float inv = l > 0.f ? 1.f / l : 0.f;
   const float y[4] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
   store_out<BF16>(p, row, head, c * 4, y, D);
@@ -418,13 +560,6 @@ constexpr int kStages = 3;
 constexpr float kNoReference = -3e38f;  // before the first visible key
 constexpr float kSlack = 8.f;
 
-// one instruction: fmaxf on results of matrix instructions brings a second one each
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
-}
-
 template <int N>
 __device__ __forceinline__ void wait_vm() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0F70);  // vmcnt(N); the other counters at their maxima
@@ -450,67 +585,16 @@ __device__ __forceinline__ void copy_to_lds(const u32x4 &rsrc, uint32_t voff, ui
 #endif
 }
 
-// 16 keys x 16 rows over 128 e4m3 features times 2^(exponent - 127) of each side
-__device__ __forceinline__ f32x4 mfma8(const i32x8 &a, const i32x8 &b, const f32x4 &c, int ea, int eb) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, ea, 0, eb);
-#else
-  return c;
-#endif
-}
-
-// A bf16 row of q as two e4m3 terms: high + low, times the row's power of two. e4m3
-// has 4 significant bits and bf16 8, so the sum is q exactly, except that a feature
-// below 2^-10 of the row's largest may be off by 2^-17 of that. K then enters the
-// scores as it is stored, without a conversion, at the matrix cores' double rate for
-// 8 bits. D = 64: one operand of 128, quads 0 and 1 the high terms, 2 and 3 the low.
-template <int D>
-struct Split8 {
-  static constexpr int NT = D / 64;  // operands
-  i32x8 q[NT];
-  int exponent;  // of the row's scale, biased
-  // x: this lane's 32 features (D = 128: all that it holds; D = 64: of its half of the row)
-  __device__ __forceinline__ void set(const float (&x)[32], int quad) {
-    float top = 0.f;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) top = fmaxf(top, fabsf(x[i]));
-    top = row_max(top);
-    const unsigned u = __builtin_bit_cast(unsigned, top);
-    // smallest e with top <= 448 * 2^e, kept where both 2^e and its inverse are normal
-    const int e = min(max((int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), -120), 120);
-    exponent = e + 127;
-    const float inv = __builtin_bit_cast(float, (unsigned)(127 - e) << 23);
-#if defined(__HIP_DEVICE_COMPILE__)
-#pragma unroll
-    for (int w = 0; w < 8; ++w) {
-      const float y[4] = {x[4 * w] * inv, x[4 * w + 1] * inv, x[4 * w + 2] * inv, x[4 * w + 3] * inv};
-      int hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-      hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], hi, true);
-      const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
-      int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0] - a[0], y[1] - a[1], 0, false);
-      lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2] - b[0], y[3] - b[1], lo, true);
-      if constexpr (NT == 2) {
-        q[0][w] = hi;
-        q[1][w] = lo;
-      } else {
-        q[0][w] = quad < 2 ? hi : lo;
-      }
-    }
-#endif
-  }
-};
-
 template <bool BF16, int D, int MT>
 struct Wide {
   static constexpr int T = BF16 ? 1 : 3, DS = D / 32, DB = D / 16;
-  static constexpr int C = BF16 ? 2 : D / 64;              // 16-byte pieces of a key that a lane reads
-  static constexpr int UNITS = BF16 ? 2 : 4 * (D / 64);    // steps of the scores of a half
-  static constexpr int MFMAS = (BF16 ? 2 * (D / 64) : UNITS * T) * MT + DB * MT * T;  // of a block
+  static constexpr int C = D / 64;                         // 16-byte pieces of a key that a lane reads
+  static constexpr int UNITS = 4 * C;                      // steps of the scores of a half
+  static constexpr int MFMAS = (UNITS + DB) * MT * T;      // of a block
   static constexpr int PAGE_BYTES = 2 * kPage * D;
   using Scores = f32x4[MT][2];   // a lane's 8 keys of a half, per row
   using Weights = bf16x8[MT][T];
-  bf16x8 q[BF16 ? 1 : T][MT][DS];  // fp32
-  Split8<D> q8[MT];                // bf16
+  bf16x8 q[T][MT][DS];
   f32x4 o[MT][DB];
   float m[MT], l[MT], top[MT];   // reference, sum, largest score that needs no raise
   int limit[MT];
@@ -523,12 +607,8 @@ struct Wide {
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const unsigned char *at = BF16 && D == 64
-                                      ? page + (2 * HALF + t) * 1024 + ((2 * ((lane >> 4) & 1) + c) * 16 + (lane & 15)) * 16
-                                      : page + ((2 * HALF + t) * C + c) * 1024 + lane * 16;
-        k[t][c] = *reinterpret_cast<const u32x4 *>(at);
-      }
+      for (int c = 0; c < C; ++c)
+        k[t][c] = *reinterpret_cast<const u32x4 *>(page + ((2 * HALF + t) * C + c) * 1024 + lane * 16);
   }
   // V of a page: of 16 features, a lane's 16 keys (the first 8 are half 0)
   __device__ __forceinline__ void read_v(const unsigned char *page, u32x4 (&v)[DB]) const {
@@ -537,25 +617,13 @@ struct Wide {
   }
   // step u of the scores, u < UNITS
   __device__ __forceinline__ void score_unit(int u, const u32x4 (&k)[2][C], float ks, Scores &s) const {
-    if constexpr (BF16) {
-      i32x8 a;
+    const int t = u & 1, e = (u >> 1) & 1, c = u >> 2;
+    const bf16x8 a = widen(k[t][c][2 * e], k[t][c][2 * e + 1], ks);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) a[i] = (int)k[u][i >> 2][i & 3];
-      const int ea = (int)(__builtin_bit_cast(unsigned, ks) >> 23);
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int j = Split8<D>::NT - 1; j >= 0; --j)
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-          s[mt][u] = mfma8(a, q8[mt].q[j], j == Split8<D>::NT - 1 ? f32x4{} : s[mt][u], ea, q8[mt].exponent);
-    } else {
-      const int t = u & 1, e = (u >> 1) & 1, c = u >> 2;
-      const bf16x8 a = widen(k[t][c][2 * e], k[t][c][2 * e + 1], ks);
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int j = T - 1; j >= 0; --j)
-          s[mt][t] = mfma(a, q[j][mt][2 * c + e], c + e == 0 && j == T - 1 ? f32x4{} : s[mt][t]);
-    }
+      for (int j = T - 1; j >= 0; --j)
+        s[mt][t] = mfma(a, q[j][mt][2 * c + e], c + e == 0 && j == T - 1 ? f32x4{} : s[mt][t]);
   }
   template <int HALF>
   __device__ __forceinline__ void value_unit(int db, const u32x4 (&v)[DB], float vs, const Weights &pf) {
@@ -678,19 +746,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
     lim_hi = max(lim_hi, w.limit[mt]);
     lim_lo = min(lim_lo, w.limit[mt]);
     const size_t q_at = ((size_t)(r.row0 + row) * p.hq + head) * D;
-    if constexpr (BF16) {
-      float x[32];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int f = D == 128 ? c / 2 * 64 + quad * 16 + c % 2 * 8 : (quad & 1) * 32 + c * 8;
-        const bf16x8 y = *reinterpret_cast<const bf16x8 *>((const __bf16 *)p.q + q_at + f);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[8 * c + i] = (float)y[i];
-      }
-      w.q8[mt].set(x, quad);
-    } else {
-      load_q<BF16, D>(p, q_at, quad, [&](int j, int ds, const bf16x8 &x) { w.q[j][mt][ds] = x; });
-    }
+    load_q<BF16, D>(p, q_at, quad, [&](int j, int ds, const bf16x8 &x) { w.q[j][mt][ds] = x; });
     w.m[mt] = kNoReference;
     w.top[mt] = kNoReference / p.scale_log2;
     w.l[mt] = 0.f;
@@ -796,14 +852,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
       const size_t part = (((size_t)(blk * p.c.hkv + h) * kWaves + wave) * MT + mt) * p.n_splits + split;
       if (quad == 0) p.part_lse[part * 16 + n16] = lse;
 #pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        const f32x4 x = w.o[mt][db] * inv;
-        const size_t to = (part * DB + db) * 256 + lane * 4;
-        if (BF16 && p.part_bf16)
-          *reinterpret_cast<u32x2 *>(reinterpret_cast<__bf16 *>(p.part_o) + to) = pack4(x);
-        else
-          *reinterpret_cast<f32x4 *>(p.part_o + to) = x;
-      }
+      for (int db = 0; db < DB; ++db)
+        *reinterpret_cast<f32x4 *>(p.part_o + (part * DB + db) * 256 + lane * 4) = w.o[mt][db] * inv;
     } else if (idx < total) {
       const int row = r.row0 + idx / p.group, head = h * p.group + idx % p.group;
 #pragma unroll
@@ -839,19 +889,9 @@ __global__ __launch_bounds__(kThreads) void cache_wide_join_kernel(const CacheAt
   for (int s = wave; s < n; s += kWaves) {
     const float lse = p.part_lse[(part + s) * 16 + n16];
     f32x4 y[DB];
-    if (BF16 && p.part_bf16) {
 #pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        const u32x2 w = *reinterpret_cast<const u32x2 *>(reinterpret_cast<const __bf16 *>(p.part_o) +
-                                                        ((part + s) * DB + db) * 256 + lane * 4);
-        y[db] = f32x4{__builtin_bit_cast(float, w[0] << 16), __builtin_bit_cast(float, w[0] & 0xffff0000u),
-                      __builtin_bit_cast(float, w[1] << 16), __builtin_bit_cast(float, w[1] & 0xffff0000u)};
-      }
-    } else {
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-        y[db] = *reinterpret_cast<const f32x4 *>(p.part_o + ((part + s) * DB + db) * 256 + lane * 4);
-    }
+    for (int db = 0; db < DB; ++db)
+      y[db] = *reinterpret_cast<const f32x4 *>(p.part_o + ((part + s) * DB + db) * 256 + lane * 4);
     if (lse == -INFINITY) continue;  // of a row that sees no key there
     const float to = fmaxf(m, lse), a = __expf(m - to), wt = __expf(lse - to);
     m = to;
@@ -890,17 +930,19 @@ __global__ __launch_bounds__(kThreads) void cache_wide_join_kernel(const CacheAt
 template <bool BF16, int D>
 hipError_t launch(const CacheAttnLaunch &p, hipStream_t st) {
   constexpr int MT = BF16 ? kCacheWideRows / 64 : kCacheWideRowsF32 / 64;
-  const int jobs = p.blocks * p.c.hkv;
+  const int jobs = p.blocks * p.c.hkv, pairs = p.cu[p.n_req] * p.hq;
   if (p.wide) {
     const int wgs = (jobs * p.n_splits + kXcdCount - 1) / kXcdCount * kXcdCount;
     cache_wide_kernel<BF16, D, MT><<<wgs, kThreads, 0, st>>>(p);
+  } else if (p.n_splits > 1) {
+    cache_line_kernel<BF16, D><<<p.n_splits * p.c.hkv, kThreads, 0, st>>>(p);
   } else {
-    cache_attn_kernel<BF16, D><<<jobs * p.n_splits, kThreads, 0, st>>>(p);
+    cache_attn_kernel<BF16, D><<<jobs, kThreads, 0, st>>>(p);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.n_splits == 1) return e;
   if (p.wide) cache_wide_join_kernel<BF16, D, MT><<<jobs * kWaves * MT, kThreads, 0, st>>>(p);
-  else cache_join_kernel<BF16, D><<<p.cu[p.n_req] * p.hq, kThreads, 0, st>>>(p);
+  else cache_line_join_kernel<BF16, D><<<pairs, kThreads, 0, st>>>(p);
   return hipGetLastError();
 }
 

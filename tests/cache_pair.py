@@ -111,11 +111,7 @@ class Pair:
         A score of d terms is off by at most (d + 8) 2^-24 of sum |q||k| scale (fp32
         sums and products) plus 2^-22 of itself (the exponent's argument); a weight by
         twice that (numerator, denominator) plus one part per key of the sums, each
-        2^-24. bf16 q is taken as two e4m3 terms of 4 significant bits under a power of
-        two that brings the row's largest value above 224: their sum is the 8 bits of
-        bf16, except where the second falls among the subnormal codes, whose half step
-        2^-10 is below 2^-17 of 224, so a score may be off by 2^-17 of max |q| sum |k|
-        scale more. bf16 adds half a step (2^-8) for the weight's rounding and one for the
+        2^-24. bf16 adds half a step (2^-8) for the weight's rounding and one for the
         output's, fp32 2^-24 for the output and 2^-23 for the three-term weight.
         """
         q = q.to(self.dtype)
@@ -126,11 +122,9 @@ class Pair:
     def within_bounds(self, o, lse, layer, cu, seq, q, pos):
         """check_attn's comparison of given results, of rows of q that are in the dtype."""
         d, hq = self.d, self.hq
-        want, want_lse, mean, size, wide = self.o.attn(layer, cu, seq, pos, f64(q), 1 / d ** 0.5)
+        want, want_lse, mean, size = self.o.attn(layer, cu, seq, pos, f64(q), 1 / d ** 0.5)
         keys = max([int(self.o.len[s]) for s in seq] + [1])
         e = 2.0 ** -24 * ((d + 8) * size + 4 * size + keys + 64)  # [hq][rows]
-        if self.dtype == torch.bfloat16:
-            e = e + 2.0 ** -17 * wide
         tol = 2 * e.T[..., None] * mean
         half = 2.0 ** -8 if self.dtype == torch.bfloat16 else 2.0 ** -23
         tol = (tol + half * mean) * (1 + half) + half * np.abs(want) + 1e-30
