@@ -85,10 +85,11 @@ struct PoolView {
   int32_t *table, *len, *refs;
   int32_t n_layers, n_pages, hkv, d, n_seqs, max_seq_pages;
 };
-// Workspace of the page calls: a count, then three lists of n_pages.
+// Workspace of the page calls: counts, then four lists of n_pages.
 struct PageWork {
-  int32_t *count;  // [0]: pairs to copy, [1]: pages in use (compact)
-  int32_t *src, *dst, *aux;
+  int32_t *count;           // [0]: pairs to copy, [1]: whether shared pages follow (fork)
+  int32_t *src, *dst;       // the pairs
+  int32_t *aux, *seq;       // compact: each page's new id; unshare: the table entries
 };
 constexpr size_t kPageWorkHead = 256;
 struct UnshareLaunch {

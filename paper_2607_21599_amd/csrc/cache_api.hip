@@ -325,7 +325,7 @@ daf_status_t attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, int32_t layer
 
 // ---- page calls -------------------------------------------------------------------
 size_t page_list_bytes(const daf_cache_t *c) { return ((size_t)c->n_pages * sizeof(int32_t) + 255) / 256 * 256; }
-size_t page_ws_bytes(const daf_cache_t *c) { return kPageWorkHead + 3 * page_list_bytes(c); }
+size_t page_ws_bytes(const daf_cache_t *c) { return kPageWorkHead + 4 * page_list_bytes(c); }
 
 daf_status_t page_work(const daf_cache_t *c, void *ws, size_t ws_bytes, PageWork &w) {
   if (!ws || ws_bytes < page_ws_bytes(c))
@@ -337,6 +337,7 @@ daf_status_t page_work(const daf_cache_t *c, void *ws, size_t ws_bytes, PageWork
   w.src = reinterpret_cast<int32_t *>(p + kPageWorkHead);
   w.dst = reinterpret_cast<int32_t *>(p + kPageWorkHead + list);
   w.aux = reinterpret_cast<int32_t *>(p + kPageWorkHead + 2 * list);
+  w.seq = reinterpret_cast<int32_t *>(p + kPageWorkHead + 3 * list);
   return DAF_OK;
 }
 

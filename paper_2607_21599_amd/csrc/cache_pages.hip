@@ -21,39 +21,38 @@ constexpr int kHash = 2 * kMaxPageSeqs;   // slots of the set of sequences
 constexpr int kCopyThreads = 256;
 constexpr int kPiece = 4 * kCopyThreads * 16;  // bytes a workgroup moves at a time
 
-// Exclusive prefix sums over the workgroup's threads, in 64 bits (a sum may pass 32
-// on its way to being refused); *total gets the sum. sh: 17 words.
-__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t *sh, int64_t *total) {
+// Exclusive prefix sums over the workgroup's threads; *total gets the sum. sh: one
+// word per wave. (64 bits where a sum may pass 32 on its way to being refused.)
+template <typename T>
+__device__ __forceinline__ T block_scan(T x, T *sh, T *total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int64_t s = x;
+  T s = x;
 #pragma unroll
   for (int k = 1; k < 64; k <<= 1) {
-    const int64_t y = __shfl_up(s, k);
+    const T y = __shfl_up(s, k);
     if (lane >= k) s += y;
   }
   __syncthreads();  // sh may still be read from the scan before
   if (lane == 63) sh[wave] = s;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    int64_t sum = 0;
-    for (int w = 0; w < kPlan / 64; ++w) {
-      const int64_t y = sh[w];
-      sh[w] = sum;
-      sum += y;
-    }
-    sh[kPlan / 64] = sum;
+  // every wave adds up the waves' sums
+  T w = lane < kPlan / 64 ? sh[lane] : 0;
+#pragma unroll
+  for (int k = 1; k < kPlan / 64; k <<= 1) {
+    const T y = __shfl_up(w, k);
+    if (lane >= k) w += y;
   }
-  __syncthreads();
-  *total = sh[kPlan / 64];
-  return sh[wave] + s - x;
+  *total = __shfl(w, kPlan / 64 - 1);
+  const T before = __shfl(w, max(wave - 1, 0));
+  return (wave ? before : 0) + s - x;
 }
 
-// A set of sequence numbers: open addressing over kHash slots, at most half full.
+// A set of sequence numbers: open addressing over slots of which at most half are taken.
 __device__ __forceinline__ unsigned hash_of(int key) { return (unsigned)key * 2654435761u >> 19; }
 static_assert(kHash == 1 << 13, "hash_of gives 13 bits");
-// false if the key was there already
-__device__ __forceinline__ bool set_add(int *set, int key) {
-  for (unsigned i = hash_of(key);; i = (i + 1) & (kHash - 1)) {
+// false if the key was there already; slots: a power of two of at most kHash
+__device__ __forceinline__ bool set_add(int *set, int key, int slots = kHash) {
+  for (unsigned i = hash_of(key) & (slots - 1);; i = (i + 1) & (slots - 1)) {
     const int old = atomicCAS(&set[i], -1, key);
     if (old == -1) return true;
     if (old == key) return false;
@@ -66,35 +65,51 @@ __device__ __forceinline__ bool set_has(const int *set, int key) {
   }
 }
 
-// Walks the free pages in order of their ids, 4 per thread and step, until `want`
-// of them were seen: f(rank, id) for each. Returns how many there were (<= want).
-template <typename F>
-__device__ __forceinline__ int64_t walk_free(const int32_t *refs, int n_pages, int64_t want, int64_t *sh, F f) {
-  int64_t seen = 0;
-  for (int64_t base = 0; base < n_pages && seen < want; base += kPlan * 4) {
-    const int64_t at = base + threadIdx.x * 4;
-    int r[4];
-    if (at + 4 <= n_pages) {
-      const i32x4 v = *reinterpret_cast<const i32x4 *>(refs + at);
+// refs of the 16 pages from `at` on (a multiple of 4) as bits: used ones
+__device__ __forceinline__ unsigned used_bits(const int32_t *refs, int n_pages, int64_t at) {
+  unsigned bits = 0;
+  i32x4 v[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) r[k] = v[k];
+  for (int q = 0; q < 4; ++q) {
+    const int64_t i = at + 4 * q;
+    v[q] = i32x4{};
+    if (i + 4 <= n_pages) {
+      v[q] = *reinterpret_cast<const i32x4 *>(refs + i);
     } else {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) r[k] = at + k < n_pages ? refs[at + k] : 1;
+      for (int k = 0; k < 4; ++k) v[q][k] = i + k < n_pages ? refs[i + k] : 0;
     }
-    int64_t mine = 0, total;
+  }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) mine += r[k] <= 0;
-    int64_t rank = seen + block_scan(mine, sh, &total);
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (r[k] <= 0) {
-        if (rank < want) f((int)rank, (int)(at + k));
-        ++rank;
-      }
+  for (int i = 0; i < 16; ++i) bits |= (unsigned)(v[i >> 2][i & 3] > 0) << i;
+  return bits;
+}
+
+// Walks the free pages in order of their ids, 16 per thread and step, until `want` of
+// them were seen: f(rank, id) for each. Returns how many there were (<= want).
+template <typename F>
+__device__ __forceinline__ int64_t walk_free(const int32_t *refs, int n_pages, int64_t want, int *sh, F f) {
+  int64_t seen = 0;
+  for (int64_t base = 0; base < n_pages && seen < want; base += kPlan * 16) {
+    const int64_t at = base + threadIdx.x * 16;
+    const int here = (int)min(max((int64_t)n_pages - at, (int64_t)0), (int64_t)16);
+    unsigned free_ = ~used_bits(refs, n_pages, at) & ((1u << here) - 1);
+    int total;
+    int64_t rank = seen + block_scan(__builtin_popcount(free_), sh, &total);
+    for (; free_ && rank < want; free_ &= free_ - 1, ++rank) f((int)rank, (int)at + __builtin_ctz(free_));
     seen += total;
   }
   return seen < want ? seen : want;
+}
+
+// The same into a list of kShort in LDS, which is complete if `want` is not more.
+constexpr int kShort = kMaxPageSeqs;
+__device__ __forceinline__ int64_t list_free(const PoolView &c, int64_t want, int *sh, int *list) {
+  const int64_t found = walk_free(c.refs, c.n_pages, want, sh, [&](int rank, int id) {
+    if (rank < kShort) list[rank] = id;
+  });
+  __syncthreads();
+  return found;
 }
 
 __device__ __forceinline__ int pages_of(int tokens) { return (tokens + kPage - 1) / kPage; }
@@ -103,28 +118,31 @@ __device__ __forceinline__ bool in_range(int x, int n) { return (unsigned)x < (u
 __global__ __launch_bounds__(kPlan) void pages_extend_kernel(const PoolView c, int n, const int32_t *seq,
                                                              const int32_t *n_new, int32_t *status) {
   __shared__ int set[kHash];
-  __shared__ int off[kMaxPageSeqs];
-  __shared__ int64_t sh[kPlan / 64 + 1];
+  __shared__ int off[kMaxPageSeqs], list[kShort];
+  __shared__ int64_t sh64[kPlan / 64];
+  __shared__ int sh[kPlan / 64];
   __shared__ int bad;
   const int t = threadIdx.x;
-  for (int i = t; i < kHash; i += kPlan) set[i] = -1;
+  if (n > 1)  // one sequence has no double
+    for (int i = t; i < kHash; i += kPlan) set[i] = -1;
   if (t == 0) bad = 0;
-  __syncthreads();
-  int have[kPer], add[kPer], need[kPer];
-  int64_t mine = 0;
+  int s[kPer], have[kPer], add[kPer], need[kPer];
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const int i = t * kPer + k;
-    have[k] = add[k] = need[k] = 0;
-    if (i >= n) continue;
-    const int s = seq ? seq[i] : i;
-    add[k] = n_new ? n_new[i] : 1;
-    if (!in_range(s, c.n_seqs) || add[k] < 0 || !set_add(set, s)) {
-      bad = 1;
-      continue;
-    }
-    have[k] = seq_len(c.len, c.n_seqs, c.max_seq_pages, s);
-    if ((int64_t)have[k] + add[k] > (int64_t)c.max_seq_pages * kPage) {
+    s[k] = i >= n ? -1 : seq ? seq[i] : i;
+    add[k] = i >= n ? 0 : n_new ? n_new[i] : 1;
+  }
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) have[k] = seq_len(c.len, c.n_seqs, c.max_seq_pages, s[k]);
+  __syncthreads();
+  int64_t mine = 0;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    need[k] = 0;
+    if (t * kPer + k >= n) continue;
+    if (!in_range(s[k], c.n_seqs) || add[k] < 0 || (n > 1 && !set_add(set, s[k])) ||
+        (int64_t)have[k] + add[k] > (int64_t)c.max_seq_pages * kPage) {
       bad = 1;
       continue;
     }
@@ -132,12 +150,12 @@ __global__ __launch_bounds__(kPlan) void pages_extend_kernel(const PoolView c, i
     mine += need[k];
   }
   int64_t want;
-  int64_t at = block_scan(mine, sh, &want);  // a barrier: `bad` is final
+  int64_t at = block_scan(mine, sh64, &want);  // its barriers make `bad` final
   if (bad) {
     if (t == 0) *status = -1;
     return;
   }
-  int64_t found = walk_free(c.refs, c.n_pages, want, sh, [](int, int) {});
+  const int64_t found = list_free(c, want, sh, list);
   if (found < want) {
     if (t == 0) *status = (int)min(want - found, (int64_t)INT32_MAX);
     return;
@@ -148,160 +166,175 @@ __global__ __launch_bounds__(kPlan) void pages_extend_kernel(const PoolView c, i
     at += need[k];
   }
   __syncthreads();
-  walk_free(c.refs, c.n_pages, want, sh, [&](int rank, int id) {
+  auto give = [&](int rank, int id) {
     int i = 0;  // the last request whose pages start at or below the rank
     for (int step = kMaxPageSeqs / 2; step; step >>= 1)
       if (off[i + step] <= rank) i += step;
-    const int s = seq ? seq[i] : i;
-    const int first = pages_of(seq_len(c.len, c.n_seqs, c.max_seq_pages, s));
-    c.table[(int64_t)s * c.max_seq_pages + first + rank - off[i]] = id;
+    const int to = seq ? seq[i] : i;
+    const int first = pages_of(seq_len(c.len, c.n_seqs, c.max_seq_pages, to));
+    c.table[(int64_t)to * c.max_seq_pages + first + rank - off[i]] = id;
     c.refs[id] = 1;
-  });
+  };
+  if (want <= kShort) {
+    for (int r = t; r < want; r += kPlan) give(r, list[r]);
+  } else {
+    walk_free(c.refs, c.n_pages, want, sh, give);
+  }
   __syncthreads();  // lengths are read above
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const int i = t * kPer + k;
-    if (i < n) c.len[seq ? seq[i] : i] = have[k] + add[k];
-  }
+  for (int k = 0; k < kPer; ++k)
+    if (t * kPer + k < n) c.len[s[k]] = have[k] + add[k];
   if (t == 0) *status = 0;
 }
 
 __global__ __launch_bounds__(kPlan) void pages_fork_kernel(const PoolView c, const PageWork w, int n,
                                                            const int32_t *src, const int32_t *dst, int32_t *status) {
   __shared__ int set[kHash];
-  __shared__ int64_t sh[kPlan / 64 + 1];
+  __shared__ int list[kShort];
+  __shared__ int sh[kPlan / 64];
   __shared__ int bad;
   const int t = threadIdx.x;
   for (int i = t; i < kHash; i += kPlan) set[i] = -1;
   if (t == 0) bad = 0, w.count[0] = 0, w.count[1] = 0;
-  __syncthreads();
-  int s[kPer], d[kPer], L[kPer];
-  int64_t mine = 0;
+  int s[kPer], d[kPer], L[kPer], held[kPer], last[kPer], mine = 0;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const int i = t * kPer + k;
-    s[k] = d[k] = -1;
-    L[k] = 0;
-    if (i >= n) continue;
-    s[k] = src[i];
-    d[k] = dst[i];
-    if (!in_range(s[k], c.n_seqs) || !in_range(d[k], c.n_seqs) || c.len[d[k]] > 0 || !set_add(set, d[k])) {
-      bad = 1;
-      continue;
-    }
+    s[k] = i < n ? src[i] : -1;
+    d[k] = i < n ? dst[i] : -1;
+  }
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    held[k] = in_range(d[k], c.n_seqs) ? c.len[d[k]] : 0;
     L[k] = seq_len(c.len, c.n_seqs, c.max_seq_pages, s[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < kPer; ++k)  // the last page, where it is not full
+    last[k] = L[k] % kPage ? c.table[(int64_t)s[k] * c.max_seq_pages + L[k] / kPage] : -1;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    if (t * kPer + k >= n) continue;
+    if (!in_range(s[k], c.n_seqs) || !in_range(d[k], c.n_seqs) || held[k] > 0 || !set_add(set, d[k])) bad = 1;
     mine += L[k] % kPage > 0;
   }
-  int64_t want;
-  int64_t rank = block_scan(mine, sh, &want);
+  int want;
+  int rank = block_scan(mine, sh, &want);
 #pragma unroll
   for (int k = 0; k < kPer; ++k)
-    if (s[k] >= 0 && set_has(set, s[k])) bad = 1;
+    if (in_range(s[k], c.n_seqs) && !bad && set_has(set, s[k])) bad = 1;
   __syncthreads();
   if (bad) {
     if (t == 0) *status = -1;
     return;
   }
-  const int64_t found = walk_free(c.refs, c.n_pages, want, sh, [](int, int) {});
+  const int found = (int)list_free(c, want, sh, list);
   if (found < want) {
-    if (t == 0) *status = (int)(want - found);
+    if (t == 0) *status = want - found;
     return;
   }
-  walk_free(c.refs, c.n_pages, want, sh, [&](int r, int id) {
-    w.dst[r] = id;
-    c.refs[id] = 1;
-  });
-  __syncthreads();
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
-    if (d[k] < 0) continue;
+    if (t * kPer + k >= n) continue;
     if (L[k] % kPage) {
-      const int full = L[k] / kPage;
-      w.src[rank] = c.table[(int64_t)s[k] * c.max_seq_pages + full];
-      c.table[(int64_t)d[k] * c.max_seq_pages + full] = w.dst[rank];
+      const int id = list[rank];
+      w.src[rank] = last[k];
+      w.dst[rank] = id;
+      c.table[(int64_t)d[k] * c.max_seq_pages + L[k] / kPage] = id;
+      c.refs[id] = 1;
       ++rank;
     }
     c.len[d[k]] = L[k];
   }
   if (t == 0) {
-    w.count[0] = (int)want;
+    w.count[0] = want;
     w.count[1] = 1;  // shared pages may follow
     *status = 0;
   }
 }
 
-// Rows of the launch in tiles of kPlan; a row that is its page's first in its
+constexpr int kRowsPer = 8;
+// Rows of the launch, kRowsPer per thread and step; a row that is its page's first in its
 // request stands for the page. The pages that are shared are listed in order.
 __global__ __launch_bounds__(kPlan) void pages_unshare_kernel(const UnshareLaunch p) {
-  __shared__ int set[kHash];
-  __shared__ int64_t sh[kPlan / 64 + 1];
+  __shared__ int set[2 * kMaxCacheReqs];
+  __shared__ int seqs[kMaxCacheReqs], lens[kMaxCacheReqs], cu[kMaxCacheReqs + 1];
+  __shared__ int sh[kPlan / 64];
   __shared__ int bad;
   const PoolView &c = p.c;
   const int t = threadIdx.x;
-  for (int i = t; i < kHash; i += kPlan) set[i] = -1;
+  if (t < 2 * kMaxCacheReqs) set[t] = -1;
   if (t == 0) bad = 0, p.w.count[0] = 0, p.w.count[1] = 0;
+  if (t <= p.n_req) cu[t] = p.cu[t];
   __syncthreads();
   if (t < p.n_req) {
     const int s = p.seq ? p.seq[t] : t;
-    if (!in_range(s, c.n_seqs) || !set_add(set, s)) bad = 1;
+    seqs[t] = s;
+    lens[t] = seq_len(c.len, c.n_seqs, c.max_seq_pages, s);
+    if (!in_range(s, c.n_seqs) || !set_add(set, s, 2 * kMaxCacheReqs)) bad = 1;
   }
   __syncthreads();
   if (bad) {
     if (t == 0) *p.status = -1;
     return;
   }
-  const int rows = p.cu[p.n_req];
+  const int rows = cu[p.n_req];
   int64_t want = 0;
-  for (int64_t base = 0; base < rows; base += kPlan) {
-    const int64_t i = base + t;
-    bool take = false;
-    int64_t slot = 0;
-    int page = -1;
-    if (i < rows) {
+  for (int64_t base = 0; base < rows; base += kPlan * kRowsPer) {
+    int64_t slot[kRowsPer];
+    int page[kRowsPer], seq_[kRowsPer], col[kRowsPer], mine = 0;
+    bool first[kRowsPer];
+#pragma unroll
+    for (int k = 0; k < kRowsPer; ++k) {
+      const int64_t i = base + t * kRowsPer + k;
+      first[k] = false;
+      if (i >= rows) continue;
       int b = 0;
       for (int step = kMaxCacheReqs / 2; step; step >>= 1)
-        if (b + step < p.n_req && p.cu[b + step] <= i) b += step;
-      const int s = p.seq ? p.seq[b] : b;
-      const int L = seq_len(c.len, c.n_seqs, c.max_seq_pages, s);
-      const int j = (int)i - p.cu[b];
-      const int shift = L - (p.cu[b + 1] - p.cu[b]);
-      const int at = p.pos ? p.pos[i] : shift + j;
+        if (b + step < p.n_req && cu[b + step] <= i) b += step;
+      const int j = (int)i - cu[b], L = lens[b];
+      const int at = p.pos ? p.pos[i] : L - (cu[b + 1] - cu[b]) + j;
       const int before = j == 0 ? -1 : p.pos ? p.pos[i - 1] : at - 1;
       if (p.pos && j > 0 && before >= at) bad = 1;  // a page would be listed twice
-      if (at >= 0 && at < L && (before < 0 || before / kPage != at / kPage)) {
-        slot = (int64_t)s * c.max_seq_pages + at / kPage;
-        page = c.table[slot];
-        take = in_range(page, c.n_pages) && c.refs[page] > 1;
+      first[k] = at >= 0 && at < L && (before < 0 || before / kPage != at / kPage);
+      seq_[k] = seqs[b];
+      col[k] = at / kPage;
+      slot[k] = (int64_t)seq_[k] * c.max_seq_pages + col[k];
+    }
+#pragma unroll
+    for (int k = 0; k < kRowsPer; ++k) page[k] = first[k] ? c.table[slot[k]] : -1;
+#pragma unroll
+    for (int k = 0; k < kRowsPer; ++k) {
+      first[k] = in_range(page[k], c.n_pages) && c.refs[page[k]] > 1;
+      mine += first[k];
+    }
+    int total;
+    int64_t rank = want + block_scan(mine, sh, &total);
+#pragma unroll
+    for (int k = 0; k < kRowsPer; ++k)
+      if (first[k]) {
+        if (rank < c.n_pages) p.w.src[rank] = page[k], p.w.seq[rank] = seq_[k], p.w.aux[rank] = col[k];
+        ++rank;
       }
-    }
-    int64_t total;
-    const int64_t rank = want + block_scan(take, sh, &total);
-    if (take && rank < c.n_pages) {
-      p.w.src[rank] = page;
-      // the table entry, in two words (dst is not needed yet)
-      p.w.aux[rank] = (int)(slot % c.max_seq_pages);
-      p.w.dst[rank] = (int)(slot / c.max_seq_pages);
-    }
     want += total;
   }
   if (bad) {  // final since the last scan's barriers
     if (t == 0) *p.status = -1;
     return;
   }
-  const int64_t found = walk_free(c.refs, c.n_pages, want, sh, [](int, int) {});
+  // free ids are found before any count changes: none of the old pages is among them
+  const int64_t found = walk_free(c.refs, c.n_pages, want, sh, [&](int r, int id) { p.w.dst[r] = id; });
   if (found < want) {
     if (t == 0) *p.status = (int)min(want - found, (int64_t)INT32_MAX);
     return;
   }
   __syncthreads();
-  // free ids are found before any count changes: none of the old pages is among them
-  walk_free(c.refs, c.n_pages, want, sh, [&](int r, int id) {
-    c.table[(int64_t)p.w.dst[r] * c.max_seq_pages + p.w.aux[r]] = id;
-    p.w.dst[r] = id;
+  for (int64_t r = t; r < want; r += kPlan) {
+    const int id = p.w.dst[r];
+    c.table[(int64_t)p.w.seq[r] * c.max_seq_pages + p.w.aux[r]] = id;
     c.refs[id] = 1;
-  });
-  __syncthreads();
-  for (int64_t r = t; r < want; r += kPlan) atomicAdd(&c.refs[p.w.src[r]], -1);
+    atomicAdd(&c.refs[p.w.src[r]], -1);
+  }
   if (t == 0) {
     p.w.count[0] = (int)want;
     *p.status = 0;
@@ -323,59 +356,50 @@ __global__ __launch_bounds__(kCopyThreads) void pages_free_kernel(const PoolView
   }
 }
 
-// One pass over refs with f(id, used, rank among the used ones); returns their number.
-template <typename F>
-__device__ __forceinline__ int64_t walk_all(const PoolView &c, int64_t *sh, F f) {
-  int64_t seen = 0;
-  for (int64_t base = 0; base < c.n_pages; base += kPlan * 4) {
-    const int64_t at = base + threadIdx.x * 4;
-    bool used[4];
-    int64_t mine = 0, total;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      used[k] = at + k < c.n_pages && c.refs[at + k] > 0;
-      mine += used[k];
-    }
-    int64_t rank = seen + block_scan(mine, sh, &total);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if (at + k < c.n_pages) f((int)(at + k), used[k], (int)rank);
-      rank += used[k];
-    }
-    seen += total;
-  }
-  return seen;
-}
-
-// The i-th used page at or past n_live and the i-th free one below: with `live`
-// used pages before id, a free id below n_live has rank id - live among the free,
-// and a used one at or past it has rank live - (used ones below n_live).
+// The i-th used page at or past n_live goes to the i-th free one below. A thread has a
+// run of pages: with u used ones before page id, it is the (id - u)-th free one or the
+// (u - below)-th used one at or past n_live, `below` of which lie below that.
 __global__ __launch_bounds__(kPlan) void pages_compact_kernel(const PoolView c, const PageWork w, int32_t *n_live) {
-  __shared__ int64_t sh[kPlan / 64 + 1];
+  __shared__ int sh[kPlan / 64];
   __shared__ int below;
-  const int live = (int)walk_all(c, sh, [](int, bool, int) {});
-  if (threadIdx.x == 0) below = 0;
+  const int t = threadIdx.x;
+  const int run = ((c.n_pages + kPlan - 1) / kPlan + 15) / 16 * 16;
+  const int64_t from = (int64_t)t * run, to = min(from + run, (int64_t)c.n_pages);
+  int mine = 0;
+  for (int64_t at = from; at < to; at += 16) mine += __builtin_popcount(used_bits(c.refs, c.n_pages, at));
+  int live;
+  const int before = block_scan(mine, sh, &live);
+  if (t == 0) below = live;  // all pages are used
   __syncthreads();
-  walk_all(c, sh, [&](int id, bool used, int rank) {
-    if (id < live) {
-      if (!used) w.dst[id - rank] = id;
-      if (id == live - 1) below = rank + used;
+  if (live >= from && live < to) {
+    int u = before;
+    for (int64_t at = from; at < live; at += 16)
+      u += __builtin_popcount(used_bits(c.refs, c.n_pages, at) & (live - at >= 16 ? 0xffffu : (1u << (live - at)) - 1));
+    below = u;
+  }
+  __syncthreads();
+  int u = before;
+  for (int64_t at = from; at < to; at += 16) {
+    const unsigned bits = used_bits(c.refs, c.n_pages, at);
+    const int end = (int)min(to - at, (int64_t)16);
+    for (int i = 0; i < end; ++i) {
+      const int id = (int)at + i;
+      const bool used = (bits >> i) & 1;
+      if (id >= live && used) w.src[u - below] = id;
+      if (id < live && !used) w.dst[id - u] = id;
+      w.aux[id] = id;
+      u += used;
     }
-    w.aux[id] = id;
-  });
-  __syncthreads();
-  walk_all(c, sh, [&](int id, bool used, int rank) {
-    if (used && id >= live) w.src[rank - below] = id;
-  });
+  }
   __syncthreads();
   const int moves = live - below;
-  for (int i = threadIdx.x; i < moves; i += kPlan) {
+  for (int i = t; i < moves; i += kPlan) {
     const int a = w.src[i], b = w.dst[i];
     w.aux[a] = b;
     c.refs[b] = c.refs[a];
     c.refs[a] = 0;
   }
-  if (threadIdx.x == 0) {
+  if (t == 0) {
     w.count[0] = moves;
     w.count[1] = 0;
     *n_live = live;
