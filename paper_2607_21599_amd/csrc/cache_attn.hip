@@ -110,11 +110,24 @@ __device__ __forceinline__ void load_q(const CacheAttnLaunch &p, size_t at, int 
   }
 }
 
-// one instruction: fmaxf on results of matrix instructions brings a second one each
+// Maxima in one instruction each: fmaxf on results of matrix instructions brings a
+// second one. max2 is for those results: the wait that they need before a vector
+// instruction reads them is put in for instructions that the compiler knows, and not
+// for max3's, which is therefore given results of vector instructions alone.
+__device__ __forceinline__ float max2(float a, float b) {
+  float inf = INFINITY;
+  asm("" : "+s"(inf));  // a known infinity makes this fmaxf again
+  return __builtin_amdgcn_fmed3f(a, b, inf);
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
   return r;
+}
+// of a lane's scores of 8 keys
+__device__ __forceinline__ float max_score(const f32x4 &a, const f32x4 &b) {
+  const float x = max2(a[0], a[1]), y = max2(a[2], a[3]), z = max2(b[0], b[1]), w = max2(b[2], b[3]);
+  return max3(max3(x, y, z), w, w);
 }
 
 struct Request {
@@ -283,14 +296,7 @@ __device__ __forceinline__ void few_rows(const CacheAttnLaunch &p, FewShared<D> 
         }
       }
     }
-    float mx = max3(s[0][0], s[0][1], s[0][2]);
-    mx = max3(mx, s[0][3], s[1][0]);
-    mx = max3(mx, s[1][1], s[1][2]);
-    mx = max3(mx, s[1][3], s[2][0]);
-    mx = max3(mx, s[2][1], s[2][2]);
-    mx = max3(mx, s[2][3], s[3][0]);
-    mx = max3(mx, s[3][1], s[3][2]);
-    mx = fmaxf(mx, s[3][3]);
+    const float upper = max_score(s[2], s[3]), mx = max3(max_score(s[0], s[1]), upper, upper);
     const float m_new = fmaxf(m_run, row_max(mx) * p.scale_log2);
     if (__ballot(m_new > m_run)) {
       const float alpha = m_new > m_run ? exp2_(m_run - m_new) : 1.f;
@@ -572,12 +578,14 @@ __device__ __forceinline__ void lds_barrier() {
 
 // One 1 KiB copy: lane i's 16 bytes at byte voff + soff of the buffer go to LDS byte
 // lds + 16 i. In asm, so that the compiler does not wait for the copies in flight at
-// each LDS read: wait_vm counts them, the barriers order them.
+// each LDS read: wait_vm counts them, the barriers order them. The s_nop makes up the
+// five wait states between a vector instruction that writes one of the scalar operands
+// and this read of it, which the compiler does not see here.
 __device__ __forceinline__ void copy_to_lds(const u32x4 &rsrc, uint32_t voff, uint32_t soff, uint32_t lds) {
 #if defined(__HIP_DEVICE_COMPILE__)
   asm volatile(
       "s_mov_b32 m0, %0\n\t"
-      "s_nop 0\n\t"
+      "s_nop 3\n\t"
       "buffer_load_dwordx4 %1, %2, %3 offen lds"
       :
       : "s"(lds), "v"(voff), "s"(rsrc), "s"(soff)
@@ -657,10 +665,7 @@ struct Wide {
     float mx[MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      mx[mt] = max3(s[mt][0][0], s[mt][0][1], s[mt][0][2]);
-      mx[mt] = max3(mx[mt], s[mt][0][3], s[mt][1][0]);
-      mx[mt] = max3(mx[mt], s[mt][1][1], s[mt][1][2]);
-      mx[mt] = max3(mx[mt], s[mt][1][3], s[mt][1][3]);
+      mx[mt] = max_score(s[mt][0], s[mt][1]);
       need |= mx[mt] > top[mt];
     }
     if (__builtin_expect(__ballot(need) == 0, 1)) return;
