@@ -73,7 +73,7 @@ struct CacheAttnLaunch {
 static_assert(sizeof(CacheAttnLaunch) < 4096, "kernel arguments must fit 4 KiB");
 // (row, head) pairs of a row block: few rows, many rows in bf16 and in fp32
 constexpr int kCacheAttnRows = 16, kCacheWideRows = 128, kCacheWideRowsF32 = 64;
-constexpr int kMaxSplitPages = 64;
+constexpr int kMinSplitPages = 6, kMaxSplitPages = 64;
 constexpr size_t kLineBytes = (2 * kMaxCacheReqs + 64) * sizeof(int32_t);
 constexpr int kMinPiece = 8;  // few rows: pages per workgroup, two for each wave
 hipError_t launch_cache_attn(bool bf16, const CacheAttnLaunch &p, hipStream_t st);

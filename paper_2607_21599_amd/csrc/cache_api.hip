@@ -223,7 +223,7 @@ AttnPlan plan_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_ca
   const int64_t jobs = std::max<int64_t>(1, blocks * c->n_kv_heads);
   if (a.wide) {
     int64_t splits = std::max<int64_t>(std::max<int64_t>(1, 512 / jobs), (pages + kMaxSplitPages - 1) / kMaxSplitPages);
-    splits = std::min(splits, (pages + 1) / 2);
+    splits = std::min(splits, (pages + kMinSplitPages - 1) / kMinSplitPages);
     a.split_pages = (int)((pages + splits - 1) / splits);
     a.n_splits = (int)((pages + a.split_pages - 1) / a.split_pages);
   } else {

@@ -65,6 +65,12 @@ __device__ __forceinline__ f32x4 mfma(const bf16x8 &a, const bf16x8 &b, const f3
 #endif
 }
 
+// row sums of weights in bf16, in each of a lane's four accumulators
+__device__ __forceinline__ f32x4 add_weights(const bf16x8 &w, const f32x4 &sum) {
+  const __bf16 one = (__bf16)1.0f;
+  return mfma(bf16x8{one, one, one, one, one, one, one, one}, w, sum);
+}
+
 // x and the same register of the lanes that hold the same row (lane ^ 16, ^ 32)
 __device__ __forceinline__ float row_max(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
@@ -197,7 +203,7 @@ struct Frags {
 template <int D>
 struct FewShared {
   float o[kWaves][kRows][D + 4];
-  float m[kWaves][kRows], l[kWaves][kRows];
+  float m[kWaves][kRows], l[kWaves][kRows], r[kWaves][kRows];
 };
 
 // Row block r.block of a request over the pages pg0 .. pg_end - 1 of its sequence, by
@@ -235,7 +241,7 @@ __device__ __forceinline__ void few_rows(const CacheAttnLaunch &p, FewShared<D> 
   lim_lo = __builtin_amdgcn_readfirstlane(lim_lo);
   const int pg1 = min(min(pg_end, (r.L + kPage - 1) / kPage), (lim_hi >> 6) + 1);  // lim_hi < 0: none
 
-  f32x4 o[DB] = {};
+  f32x4 o[DB] = {}, rounded = {};  // rounded: sum of the weights as they enter the product
   float m_run = -INFINITY, l_run = 0.f;
 
   auto page_id = [&](int i) {  // i-th page of this wave
@@ -301,6 +307,7 @@ __device__ __forceinline__ void few_rows(const CacheAttnLaunch &p, FewShared<D> 
     if (__ballot(m_new > m_run)) {
       const float alpha = m_new > m_run ? exp2_(m_run - m_new) : 1.f;
       l_run *= alpha;
+      rounded *= alpha;
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[db] *= alpha;
       m_run = m_new;
@@ -318,6 +325,7 @@ __device__ __forceinline__ void few_rows(const CacheAttnLaunch &p, FewShared<D> 
     for (int ks = 0; ks < 2; ++ks) {
       bf16x8 pf[T];
       split_terms<T>(e[ks], pf);
+      if constexpr (BF16) rounded = add_weights(pf[0], rounded);
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
         const bf16x8 a = widen(f.v[db][2 * ks], f.v[db][2 * ks + 1], f.vs);
@@ -342,7 +350,7 @@ __device__ __forceinline__ void few_rows(const CacheAttnLaunch &p, FewShared<D> 
 
   // join the waves
   l_run = row_sum(l_run);
-  if (quad == 0) sh.m[wave][n16] = m_run, sh.l[wave][n16] = l_run;
+  if (quad == 0) sh.m[wave][n16] = m_run, sh.l[wave][n16] = l_run, sh.r[wave][n16] = BF16 ? rounded[0] : l_run;
 #pragma unroll
   for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4 *>(&sh.o[wave][n16][db * 16 + quad * 4]) = o[db];
   __syncthreads();
@@ -350,15 +358,16 @@ __device__ __forceinline__ void few_rows(const CacheAttnLaunch &p, FewShared<D> 
   const int out = r.block * kRows + rr;
   if (out >= total) return;
   const int orow = r.row0 + out / p.group, ohead = h * p.group + out % p.group;
-  float m = sh.m[0][rr], w[kWaves], l = 0.f;
+  float m = sh.m[0][rr], w[kWaves], l = 0.f, sum = 0.f;
 #pragma unroll
   for (int k = 1; k < kWaves; ++k) m = fmaxf(m, sh.m[k][rr]);
 #pragma unroll
   for (int k = 0; k < kWaves; ++k) {
     w[k] = sh.m[k][rr] == -INFINITY ? 0.f : exp2_(sh.m[k][rr] - m);
     l += w[k] * sh.l[k][rr];
+    sum += w[k] * sh.r[k][rr];
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
   const float lse = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
 #pragma unroll
   for (int c = c0 * 4; c < D; c += 64) {
@@ -598,12 +607,13 @@ struct Wide {
   static constexpr int T = BF16 ? 1 : 3, DS = D / 32, DB = D / 16;
   static constexpr int C = D / 64;                         // 16-byte pieces of a key that a lane reads
   static constexpr int UNITS = 4 * C;                      // steps of the scores of a half
-  static constexpr int MFMAS = (UNITS + DB) * MT * T;      // of a block
+  static constexpr int MFMAS = ((UNITS + DB) * T + BF16) * MT;  // of a block
   static constexpr int PAGE_BYTES = 2 * kPage * D;
   using Scores = f32x4[MT][2];   // a lane's 8 keys of a half, per row
   using Weights = bf16x8[MT][T];
   bf16x8 q[T][MT][DS];
   f32x4 o[MT][DB];
+  f32x4 rounded[MT];             // sums of the weights as they enter the product (bf16)
   float m[MT], l[MT], top[MT];   // reference, sum, largest score that needs no raise
   int limit[MT];
   float scale_log2;
@@ -641,6 +651,11 @@ struct Wide {
 #pragma unroll
       for (int j = T - 1; j >= 0; --j) o[mt][db] = mfma(a, pf[mt][j], o[mt][db]);
   }
+  __device__ __forceinline__ void sum_weights(const Weights &pf) {
+    if constexpr (BF16)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) rounded[mt] = add_weights(pf[mt][0], rounded[mt]);
+  }
   // keys (key, key + 1, ...: a lane's 8) past a row's limit get no weight, and the
   // values of those that no row of the wave sees, which may be NaN codes, become 0
   __device__ __forceinline__ void mask_scores(Scores &s, int key) const {
@@ -676,6 +691,7 @@ struct Wide {
       m[mt] = to;
       top[mt] = (to + kSlack) / scale_log2;
       l[mt] *= alpha;
+      rounded[mt] *= alpha;
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[mt][db] *= alpha;
 #pragma unroll
@@ -691,6 +707,7 @@ struct Wide {
                                         float vs) {
     Scores next;
     float e[MT][8];
+    sum_weights(pf);
 #pragma unroll
     for (int step = 0; step < 8; ++step) {
 #pragma unroll
@@ -755,6 +772,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
     w.m[mt] = kNoReference;
     w.top[mt] = kNoReference / p.scale_log2;
     w.l[mt] = 0.f;
+    w.rounded[mt] = f32x4{};
 #pragma unroll
     for (int db = 0; db < DB; ++db) w.o[mt][db] = f32x4{};
   }
@@ -842,6 +860,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
     int i = 0;
     for (; i < whole; ++i) step(i, std::false_type{});
     for (; i < n; ++i) step(i, std::true_type{});
+    w.sum_weights(pf);
 #pragma unroll
     for (int db = 0; db < DB; ++db) w.template value_unit<1>(db, v, of_page(vss, n - 1), pf);
   }
@@ -849,8 +868,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
   // results
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
-    const float l = row_sum(w.l[mt]);
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float l = row_sum(w.l[mt]), sum = BF16 ? w.rounded[mt][0] : l;
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
     const float lse = l > 0.f ? (w.m[mt] + log2f(l)) * kLn2 : -INFINITY;
     const int tile = (r.block * kWaves + wave) * MT + mt, idx = tile * 16 + n16;
     if (p.n_splits > 1) {
@@ -875,11 +894,13 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
 // Join the splits of one tile of 16 pairs. The waves take the splits in turn, with
 // everything of a split in flight at once, and join their sums through LDS; a lane has
 // the same pair and features as in the kernel above.
+constexpr int kJoinWaves = 8;
+static_assert(kJoinWaves >= 128 / 16, "a wave per 16 features");
 template <bool BF16, int D, int MT>
-__global__ __launch_bounds__(kThreads) void cache_wide_join_kernel(const CacheAttnLaunch p) {
-  constexpr int DB = D / 16, PER = DB / kWaves;
-  __shared__ f32x4 sh_x[kWaves][DB][64];
-  __shared__ float sh_m[kWaves][16], sh_l[kWaves][16];
+__global__ __launch_bounds__(kJoinWaves * 64) void cache_wide_join_kernel(const CacheAttnLaunch p) {
+  constexpr int DB = D / 16;
+  __shared__ f32x4 sh_x[kJoinWaves][DB][64];
+  __shared__ float sh_m[kJoinWaves][16], sh_l[kJoinWaves][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n16 = lane & 15, quad = lane >> 4;
   const int tile = blockIdx.x % (kWaves * MT), rest = blockIdx.x / (kWaves * MT);
   const int h = rest % p.c.hkv, blk = rest / p.c.hkv;
@@ -891,7 +912,7 @@ __global__ __launch_bounds__(kThreads) void cache_wide_join_kernel(const CacheAt
   const size_t part = (size_t)blockIdx.x * p.n_splits;
   f32x4 x[DB] = {};
   float m = -INFINITY, l = 0.f;
-  for (int s = wave; s < n; s += kWaves) {
+  for (int s = wave; s < n; s += kJoinWaves) {
     const float lse = p.part_lse[(part + s) * 16 + n16];
     f32x4 y[DB];
 #pragma unroll
@@ -909,25 +930,25 @@ __global__ __launch_bounds__(kThreads) void cache_wide_join_kernel(const CacheAt
   if (quad == 0) sh_m[wave][n16] = m, sh_l[wave][n16] = l;
   __syncthreads();
   if (idx >= total) return;
-  m = fmaxf(fmaxf(sh_m[0][n16], sh_m[1][n16]), fmaxf(sh_m[2][n16], sh_m[3][n16]));
-  float w[kWaves];
+  m = sh_m[0][n16];
+#pragma unroll
+  for (int k = 1; k < kJoinWaves; ++k) m = fmaxf(m, sh_m[k][n16]);
+  float w[kJoinWaves];
   l = 0.f;
 #pragma unroll
-  for (int k = 0; k < kWaves; ++k) {
+  for (int k = 0; k < kJoinWaves; ++k) {
     w[k] = sh_m[k][n16] == -INFINITY ? 0.f : __expf(sh_m[k][n16] - m);
     l += w[k] * sh_l[k][n16];
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
   const int row = r.row0 + idx / p.group, head = h * p.group + idx % p.group;
+  if (wave < DB) {
+    f32x4 v = {};
 #pragma unroll
-  for (int k = 0; k < PER; ++k) {
-    const int db = wave * PER + k;
-    f32x4 v = sh_x[0][db][lane] * w[0];
-#pragma unroll
-    for (int j = 1; j < kWaves; ++j) v += sh_x[j][db][lane] * w[j];
+    for (int k = 0; k < kJoinWaves; ++k) v += sh_x[k][wave][lane] * w[k];
     v *= inv;
     const float y[4] = {v[0], v[1], v[2], v[3]};
-    store_out<BF16>(p, row, head, db * 16 + quad * 4, y, D);
+    store_out<BF16>(p, row, head, wave * 16 + quad * 4, y, D);
   }
   if (wave == 0 && quad == 0 && p.lse) p.lse[(size_t)head * p.lse_stride + row] = l > 0.f ? m + __logf(l) : -INFINITY;
 }
@@ -946,7 +967,7 @@ hipError_t launch(const CacheAttnLaunch &p, hipStream_t st) {
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.n_splits == 1) return e;
-  if (p.wide) cache_wide_join_kernel<BF16, D, MT><<<jobs * kWaves * MT, kThreads, 0, st>>>(p);
+  if (p.wide) cache_wide_join_kernel<BF16, D, MT><<<jobs * kWaves * MT, kJoinWaves * 64, 0, st>>>(p);
   else cache_line_join_kernel<BF16, D><<<pairs, kThreads, 0, st>>>(p);
   return hipGetLastError();
 }
