@@ -216,7 +216,10 @@ AttnPlan plan_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_ca
   AttnPlan a{};
   int64_t most = 0, blocks = 0;
   for (int b = 0; b < rows->n; ++b) most = std::max<int64_t>(most, rows->cu[b + 1] - rows->cu[b]);
-  a.wide = most * (cfg->n_q_heads / cfg->n_kv_heads) > 2 * kCacheAttnRows;
+  // Up to four of few rows' blocks read a page from the caches as often before the wide
+  // kernel's larger tiles pay (7 heads on one, us, few rows and wide: 8000 keys, 9 rows
+  // 18.5 and 20.3, 18 rows 22.6 and 20.9; 131072 keys 65.5 and 67.7, 111 and 71.8).
+  a.wide = most * (cfg->n_q_heads / cfg->n_kv_heads) > 4 * kCacheAttnRows;
   a.block_rows = !a.wide ? kCacheAttnRows : cfg->dtype == DAF_BF16 ? kCacheWideRows : kCacheWideRowsF32;
   for (int b = 0; b < rows->n; ++b) blocks += row_blocks(cfg, rows->cu[b + 1] - rows->cu[b], a.block_rows);
   const int64_t pages = std::max<int64_t>(1, ((int64_t)max_len + kPage - 1) / kPage);
@@ -232,7 +235,8 @@ AttnPlan plan_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_ca
     a.n_splits = 1;
     if (pages > 16) {
       const int64_t line = std::min<int64_t>(blocks, INT32_MAX) * pages;
-      a.n_splits = (int)std::max<int64_t>(2, std::min<int64_t>(512 / c->n_kv_heads, (line + kMinPiece - 1) / kMinPiece));
+      const int wgs = cfg->dtype == DAF_BF16 || cfg->head_dim == 64 ? 512 : 256;  // as many as run at once
+      a.n_splits = (int)std::max<int64_t>(2, std::min<int64_t>(wgs / c->n_kv_heads, (line + kMinPiece - 1) / kMinPiece));
     }
   }
   if (a.n_splits > 1) {

@@ -445,8 +445,13 @@ __device__ __forceinline__ Line build_line(const CacheAttnLaunch &p) {
   return s;
 }
 
+// fp32's terms of 128 features need more than 256 registers: one workgroup per CU, with
+// whole pages in flight, for two whose registers spill (131072 keys, a row for 28
+// heads: 30.4 us for 45.3).
 template <bool BF16, int D>
-__global__ __launch_bounds__(kThreads, 2) void cache_line_kernel(const CacheAttnLaunch p) {
+constexpr int kLineWgs = BF16 || D == 64 ? 2 : 1;
+template <bool BF16, int D>
+__global__ __launch_bounds__(kThreads, (kLineWgs<BF16, D>)) void cache_line_kernel(const CacheAttnLaunch p) {
   __shared__ FewShared<D> sh;
   const int lane = threadIdx.x & 63;
   const int h = blockIdx.x % p.c.hkv, k = blockIdx.x / p.c.hkv;
@@ -891,66 +896,62 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
   }
 }
 
-// Join the splits of one tile of 16 pairs. The waves take the splits in turn, with
-// everything of a split in flight at once, and join their sums through LDS; a lane has
-// the same pair and features as in the kernel above.
-constexpr int kJoinWaves = 8;
-static_assert(kJoinWaves >= 128 / 16, "a wave per 16 features");
+// Join the splits of one tile of 16 pairs: a wave per 16 features, a lane with the same
+// pair and features as in the kernel above, 8 splits in flight. The first ones do not
+// wait for the length, which says how many splits hold keys; those beyond it were not
+// written and are left out.
 template <bool BF16, int D, int MT>
-__global__ __launch_bounds__(kJoinWaves * 64) void cache_wide_join_kernel(const CacheAttnLaunch p) {
-  constexpr int DB = D / 16;
-  __shared__ f32x4 sh_x[kJoinWaves][DB][64];
-  __shared__ float sh_m[kJoinWaves][16], sh_l[kJoinWaves][16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n16 = lane & 15, quad = lane >> 4;
+__global__ __launch_bounds__(D * 4) void cache_wide_join_kernel(const CacheAttnLaunch p) {
+  constexpr int DB = D / 16, FLIGHT = 8;
+  const int lane = threadIdx.x & 63, db = threadIdx.x >> 6, n16 = lane & 15, quad = lane >> 4;
   const int tile = blockIdx.x % (kWaves * MT), rest = blockIdx.x / (kWaves * MT);
   const int h = rest % p.c.hkv, blk = rest / p.c.hkv;
+  const size_t part = (size_t)blockIdx.x * p.n_splits;
+  const float *lses = p.part_lse + part * 16 + n16, *os = p.part_o + (part * DB + db) * 256 + lane * 4;
+  float lse[FLIGHT];
+  f32x4 y[FLIGHT];
+  auto load = [&](int s0) {
+#pragma unroll
+    for (int j = 0; j < FLIGHT; ++j) {
+      const int s = min(s0 + j, p.n_splits - 1);
+      lse[j] = lses[s * 16];
+      y[j] = *reinterpret_cast<const f32x4 *>(os + (size_t)s * (DB * 256));
+    }
+  };
+  load(0);
   const Request r = find_request(p, blk);
   const int idx = (r.block * kWaves * MT + tile) * 16 + n16, total = r.n * p.group;
-  if ((r.block * kWaves * MT + tile) * 16 >= total) return;
   const int pages = (r.L + kPage - 1) / kPage;
   const int n = max(1, (pages + p.split_pages - 1) / p.split_pages);  // splits that hold keys
-  const size_t part = (size_t)blockIdx.x * p.n_splits;
-  f32x4 x[DB] = {};
   float m = -INFINITY, l = 0.f;
-  for (int s = wave; s < n; s += kJoinWaves) {
-    const float lse = p.part_lse[(part + s) * 16 + n16];
-    f32x4 y[DB];
+  f32x4 x = {};
+  for (int s0 = 0;;) {
+    float to = m;
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
-      y[db] = *reinterpret_cast<const f32x4 *>(p.part_o + ((part + s) * DB + db) * 256 + lane * 4);
-    if (lse == -INFINITY) continue;  // of a row that sees no key there
-    const float to = fmaxf(m, lse), a = __expf(m - to), wt = __expf(lse - to);
+    for (int j = 0; j < FLIGHT; ++j)
+      if (s0 + j < n) to = fmaxf(to, lse[j]);
+    const float ref = to == -INFINITY ? 0.f : to;  // a row that sees no key yet
+    const float a = __expf(m - ref);
     m = to;
-    l = l * a + wt;
+    l *= a;
+    x *= a;
 #pragma unroll
-    for (int db = 0; db < DB; ++db) x[db] = x[db] * a + y[db] * wt;
+    for (int j = 0; j < FLIGHT; ++j)
+      if (s0 + j < n) {
+        const float w = __expf(lse[j] - ref);
+        l += w;
+        x += y[j] * w;
+      }
+    s0 += FLIGHT;
+    if (s0 >= n) break;
+    load(s0);
   }
-#pragma unroll
-  for (int db = 0; db < DB; ++db) sh_x[wave][db][lane] = x[db];
-  if (quad == 0) sh_m[wave][n16] = m, sh_l[wave][n16] = l;
-  __syncthreads();
   if (idx >= total) return;
-  m = sh_m[0][n16];
-#pragma unroll
-  for (int k = 1; k < kJoinWaves; ++k) m = fmaxf(m, sh_m[k][n16]);
-  float w[kJoinWaves];
-  l = 0.f;
-#pragma unroll
-  for (int k = 0; k < kJoinWaves; ++k) {
-    w[k] = sh_m[k][n16] == -INFINITY ? 0.f : __expf(sh_m[k][n16] - m);
-    l += w[k] * sh_l[k][n16];
-  }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  x *= l > 0.f ? 1.f / l : 0.f;
   const int row = r.row0 + idx / p.group, head = h * p.group + idx % p.group;
-  if (wave < DB) {
-    f32x4 v = {};
-#pragma unroll
-    for (int k = 0; k < kJoinWaves; ++k) v += sh_x[k][wave][lane] * w[k];
-    v *= inv;
-    const float y[4] = {v[0], v[1], v[2], v[3]};
-    store_out<BF16>(p, row, head, wave * 16 + quad * 4, y, D);
-  }
-  if (wave == 0 && quad == 0 && p.lse) p.lse[(size_t)head * p.lse_stride + row] = l > 0.f ? m + __logf(l) : -INFINITY;
+  const float out[4] = {x[0], x[1], x[2], x[3]};
+  store_out<BF16>(p, row, head, db * 16 + quad * 4, out, D);
+  if (db == 0 && quad == 0 && p.lse) p.lse[(size_t)head * p.lse_stride + row] = l > 0.f ? m + __logf(l) : -INFINITY;
 }
 
 template <bool BF16, int D>
@@ -967,7 +968,7 @@ hipError_t launch(const CacheAttnLaunch &p, hipStream_t st) {
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.n_splits == 1) return e;
-  if (p.wide) cache_wide_join_kernel<BF16, D, MT><<<jobs * kWaves * MT, kJoinWaves * 64, 0, st>>>(p);
+  if (p.wide) cache_wide_join_kernel<BF16, D, MT><<<jobs * kWaves * MT, D * 4, 0, st>>>(p);
   else cache_line_join_kernel<BF16, D><<<pairs, kThreads, 0, st>>>(p);
   return hipGetLastError();
 }
