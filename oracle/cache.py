@@ -162,14 +162,14 @@ class CacheOracle:
                 any(self.len[s] for s in dst):
             return -1
         ids = self.free_ids()
-        need = sum(1 for s in src if self.len[s] % PAGE)
+        need = sum(1 for s in src if self.len[s] % PAGE and self.page(s, int(self.len[s]) // PAGE) is not None)
         if need > len(ids):
             return need - len(ids)
         for a, b in zip(src, dst):
             full = int(self.len[a]) // PAGE
             for i in range(self.used(a)):
                 p = int(self.table[a, i])
-                if i < full:
+                if i < full or not 0 <= p < len(self.refs):
                     self.table[b, i] = p
                     if 0 <= p < len(self.refs):
                         self.refs[p] += 1

@@ -211,12 +211,13 @@ __global__ __launch_bounds__(kPlan) void pages_fork_kernel(const PoolView c, con
 #pragma unroll
   for (int k = 0; k < kPer; ++k)  // the last page, where it is not full
     last[k] = L[k] % kPage ? c.table[(int64_t)s[k] * c.max_seq_pages + L[k] / kPage] : -1;
+  auto own = [&](int k) { return in_range(last[k], c.n_pages); };  // one that is not there stays so
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     if (t * kPer + k >= n) continue;
     if (!in_range(s[k], c.n_seqs) || !in_range(d[k], c.n_seqs) || held[k] > 0 || !set_add(set, d[k])) bad = 1;
-    mine += L[k] % kPage > 0;
+    mine += own(k);
   }
   int want;
   int rank = block_scan(mine, sh, &want);
@@ -237,12 +238,14 @@ __global__ __launch_bounds__(kPlan) void pages_fork_kernel(const PoolView c, con
   for (int k = 0; k < kPer; ++k) {
     if (t * kPer + k >= n) continue;
     if (L[k] % kPage) {
-      const int id = list[rank];
-      w.src[rank] = last[k];
-      w.dst[rank] = id;
+      const int id = own(k) ? list[rank] : last[k];
       c.table[(int64_t)d[k] * c.max_seq_pages + L[k] / kPage] = id;
-      c.refs[id] = 1;
-      ++rank;
+      if (own(k)) {
+        w.src[rank] = last[k];
+        w.dst[rank] = id;
+        c.refs[id] = 1;
+        ++rank;
+      }
     }
     c.len[d[k]] = L[k];
   }

@@ -70,6 +70,16 @@ def test_fork_shares_and_copies():
     assert p.fork([], []) == 0
 
 
+def test_fork_of_a_last_page_that_is_not_there():
+    p = _pair(pages=10, heads=1, d=64, n_seqs=6, max_seq_pages=3)
+    _fill(p, np.random.default_rng(6), [0, 1], [130, 70])
+    p.o.table[0, 2] = -1
+    p.t["table"].copy_(torch.from_numpy(p.o.table).int())
+    assert p.fork([0, 1, 0], [2, 3, 4]) == 0
+    p.same()
+    assert p.o.table[2, 2] == -1 and p.o.table[3, 1] >= 0
+
+
 def test_unshare_copies_what_the_rows_touch():
     p = _pair(layers=2, pages=40, heads=3, d=64, n_seqs=8, max_seq_pages=10)
     rng = np.random.default_rng(2)
