@@ -478,7 +478,8 @@ size_t daf_cache_attn_workspace_size(const daf_attn_cfg_t *cfg,
  * probabilities enter as three bf16 terms each (24 bits). Sums hold probabilities
  * of at most 2^8, so |V| must stay below 2^100.
  *   workspace: at least daf_cache_attn_workspace_size bytes, 16-byte aligned,
- * contents undefined after the call. */
+ * contents undefined after the call; calls that may run at the same time, captured
+ * ones included, need one each. */
 daf_status_t daf_cache_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *cache,
                             int32_t layer, const daf_cache_rows_t *rows,
                             int32_t max_len, const void *q, void *o, float *lse,
@@ -493,7 +494,8 @@ daf_status_t daf_cache_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *cache,
  * nothing else changes.
  *
  * Workspace of any of them (fork, unshare, compact); 0 on bad input. 16-byte
- * aligned, contents undefined after the call. */
+ * aligned, contents undefined after the call; calls on different caches that may run
+ * at the same time need one each. */
 size_t daf_pages_workspace_size(const daf_cache_t *cache);
 
 /* Lengthen n (<= 4096) distinct sequences by n_new[i] >= 0 tokens: pages as needed,
@@ -504,7 +506,7 @@ daf_status_t daf_pages_extend(const daf_cache_t *cache, int32_t n,
 
 /* Make the empty (len 0) sequence dst[i] a copy of src[i], i < n (<= 4096): full
  * pages are shared (refs + 1), a last page that is not full is copied into a page
- * of its own. dst are distinct and none of them is a src; a src may be named
+ * of its own (one that is not there stays so). dst are distinct and none of them is a src; a src may be named
  * several times. */
 daf_status_t daf_pages_fork(const daf_cache_t *cache, int32_t n,
                             const int32_t *src, const int32_t *dst,
@@ -517,7 +519,7 @@ daf_status_t daf_pages_unshare(const daf_cache_t *cache,
                                const daf_cache_rows_t *rows, int32_t *status,
                                void *workspace, size_t ws_bytes, hipStream_t stream);
 
-/* Empty n sequences: refs - 1 for their pages (free at 0), their table entries
+/* Empty n (<= 2^23) sequences: refs - 1 for their pages (free at 0), their table entries
  * become -1, len 0. A sequence named twice or out of range is no error. seq NULL:
  * sequences 0 .. n-1. */
 daf_status_t daf_pages_free(const daf_cache_t *cache, int32_t n,

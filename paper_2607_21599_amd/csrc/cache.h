@@ -11,7 +11,9 @@ namespace daf {
 constexpr int kPage = DAF_PAGE_TOKENS;  // tokens of a page
 constexpr int kMaxCacheReqs = 256;      // requests per launch (their prefix sums are a kernel argument)
 constexpr int kMaxPageSeqs = 4096;      // sequences per page call (one workgroup plans it)
+constexpr int kMaxFree = 1 << 23;       // sequences per call that frees them (a workgroup each)
 constexpr int kMinScaleExp = -100;      // exponent of the smallest scale
+constexpr int kStoreThreads = 256, kCacheAttnThreads = 256;  // of the workgroups
 
 // Error text of the calling thread (api.hip).
 daf_status_t set_error(daf_status_t st, const char *text);

@@ -37,6 +37,9 @@ daf_status_t need_ptr(const void *p, const char *name) {
   return aligned(p, name);
 }
 
+// a launch has less than 2^32 threads
+bool fits(int64_t workgroups, int threads) { return workgroups <= (int64_t)UINT32_MAX / threads; }
+
 #define CHECK(expr)                \
   do {                             \
     daf_status_t st_ = (expr);     \
@@ -176,7 +179,7 @@ daf_status_t store(bool write, const daf_attn_cfg_t *cfg, const daf_cache_t *c, 
       p.c = view(c, layer);
       p.n_req = std::min(kMaxCacheReqs, rows->n - b0);
       p.units = fill(rows, b0, p.n_req, p.cu, p.unit0, &p.per_req, units_of);
-      if (p.units < 0 || (int64_t)p.units * c->n_kv_heads > INT32_MAX / 2)
+      if (p.units < 0 || !fits((int64_t)p.units * c->n_kv_heads * 2, kStoreThreads))
         return fail(DAF_ERR_UNSUPPORTED, "%d rows of %d heads are too many for one call", total, c->n_kv_heads);
       if (pass == 0 || p.units == 0) continue;
       const int64_t row0 = rows->cu[b0];
@@ -235,8 +238,14 @@ AttnPlan plan_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_ca
     a.n_splits = 1;
     if (pages > 16) {
       const int64_t line = std::min<int64_t>(blocks, INT32_MAX) * pages;
-      const int wgs = cfg->dtype == DAF_BF16 || cfg->head_dim == 64 ? 512 : 256;  // as many as run at once
-      a.n_splits = (int)std::max<int64_t>(2, std::min<int64_t>(wgs / c->n_kv_heads, (line + kMinPiece - 1) / kMinPiece));
+      // Two workgroups per CU hide the ends of requests behind each other's loads; within
+      // one request one is enough, with half as much to join (bf16 of 128 features, us with
+      // 512 and 256: 32 ragged sequences 30.9 and 34.8, two of 30000 keys 20.5 and 22.0;
+      // one of 131072 keys 38.0 and 36.0, four rows of it 48.5 and 42.3). fp32 of 128
+      // features has one.
+      const bool two = rows->n > 1 && (cfg->dtype == DAF_BF16 || cfg->head_dim == 64);
+      const int64_t wgs = (two ? 512 : 256) / c->n_kv_heads;
+      a.n_splits = (int)std::max<int64_t>(2, std::min<int64_t>(wgs, (line + kMinPiece - 1) / kMinPiece));
     }
   }
   if (a.n_splits > 1) {
@@ -289,9 +298,12 @@ daf_status_t attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, int32_t layer
       p.blocks = fill(rows, b0, p.n_req, p.cu, p.blk0, &p.per_req, 
                       [&](int64_t n) { return row_blocks(cfg, n, a.block_rows); });
       const int64_t pages = ((int64_t)max_len + kPage - 1) / kPage;
-      // grids, and few rows' line of pages with a piece of it more
-      if (p.blocks < 0 || (int64_t)p.blocks * c->n_kv_heads * (a.wide ? std::max(a.n_splits, 8) : 1) > INT32_MAX - 8 ||
-          (!a.wide && (int64_t)p.blocks * std::max<int64_t>(pages, 1) > INT32_MAX / 2))
+      const int64_t jobs = (int64_t)p.blocks * c->n_kv_heads, pairs = (int64_t)p.cu[p.n_req] * cfg->n_q_heads;
+      // the grids of the kernel and of the join, and few rows' line of pages with a piece more
+      const bool grids = a.wide ? fits(jobs * a.n_splits + 8, kCacheAttnThreads) &&
+                                      (a.n_splits == 1 || fits(jobs * (a.block_rows / 16), cfg->head_dim * 4))
+                                : fits(jobs, kCacheAttnThreads) && fits(pairs, kCacheAttnThreads);
+      if (p.blocks < 0 || !grids || (!a.wide && (int64_t)p.blocks * std::max<int64_t>(pages, 1) > INT32_MAX / 2))
         return fail(DAF_ERR_UNSUPPORTED, "%d rows over %d keys are too many for one call", total, max_len);
       if (pass == 0 || p.blocks == 0) continue;
       const int64_t row0 = rows->cu[b0];
@@ -424,7 +436,7 @@ daf_status_t daf_pages_unshare(const daf_cache_t *cache, const daf_cache_rows_t 
 
 daf_status_t daf_pages_free(const daf_cache_t *cache, int32_t n, const int32_t *seq, hipStream_t stream) {
   CHECK(check_cache(cache));
-  if (n < 0) return fail(DAF_ERR_INVALID_ARG, "n=%d must be >= 0", n);
+  CHECK(check_count(n, kMaxFree));
   CHECK(aligned(seq, "seq"));
   if (n == 0) return ok();
   return launched(launch_pages_free(pool(cache), n, seq, stream), "page free launch");

@@ -36,7 +36,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kCacheAttnThreads;
 constexpr int kWaves = kThreads / 64;
 constexpr int kRows = kCacheAttnRows;
 constexpr int kXcdCount = 8;  // workgroups go to the XCDs in turn
@@ -171,9 +171,9 @@ __device__ __forceinline__ Request find_request(const CacheAttnLaunch &p, int bl
   return r;
 }
 
-// last key that row j of the request sees
+// last key that row j of the request sees, -1 if none
 __device__ __forceinline__ int row_limit(const CacheAttnLaunch &p, const Request &r, int j) {
-  return p.pos ? min(p.pos[r.row0 + j], r.L - 1) : r.L - r.n + j;
+  return max(-1, p.pos ? min(p.pos[r.row0 + j], r.L - 1) : r.L - r.n + j);
 }
 
 __device__ __forceinline__ u32x2 pack4(const f32x4 &x) {
@@ -239,7 +239,7 @@ __device__ __forceinline__ void few_rows(const CacheAttnLaunch &p, FewShared<D> 
   }
   lim_hi = __builtin_amdgcn_readfirstlane(lim_hi);
   lim_lo = __builtin_amdgcn_readfirstlane(lim_lo);
-  const int pg1 = min(min(pg_end, (r.L + kPage - 1) / kPage), (lim_hi >> 6) + 1);  // lim_hi < 0: none
+  const int pg1 = min(min(pg_end, (r.L + kPage - 1) / kPage), (lim_hi >> 6) + 1);
 
   f32x4 o[DB] = {}, rounded = {};  // rounded: sum of the weights as they enter the product
   float m_run = -INFINITY, l_run = 0.f;
@@ -760,6 +760,18 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
   const int pages = (r.L + kPage - 1) / kPage;
   if (split > 0 && pg0 >= pages) return;  // no keys here: the join leaves this split out
   const int total = r.n * p.group;
+  constexpr int PAIRS = kWaves * 16 * MT;  // of a row block
+  int last = -1;                           // last key that a row of the block sees
+  if (p.pos) {
+#pragma unroll
+    for (int i = 0; i < PAIRS; i += 64)
+      last = max(last, row_limit(p, r, min(r.block * PAIRS + i + lane, total - 1) / p.group));
+#pragma unroll
+    for (int m = 32; m; m >>= 1) last = max(last, __shfl_xor(last, m));
+  } else {
+    last = row_limit(p, r, (min((r.block + 1) * PAIRS, total) - 1) / p.group);
+  }
+  const int seen = __builtin_amdgcn_readfirstlane((last >> 6) + 1);  // pages
 
   W w;
   w.scale_log2 = p.scale_log2;
@@ -789,9 +801,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
   w.lim_hi = __builtin_amdgcn_readfirstlane(lim_hi);
   lim_lo = __builtin_amdgcn_readfirstlane(lim_lo);
 
-  // this split's pages that are there, one per lane (split_pages <= 64), in order
+  // this split's pages that are there and that a row of the block sees, one per lane
+  // (split_pages <= 64), in order
   const unsigned long long mask =
-      __ballot(lane < p.split_pages && pg0 + lane < pages && (unsigned)id < (unsigned)p.c.n_pages);
+      __ballot(lane < p.split_pages && pg0 + lane < seen && (unsigned)id < (unsigned)p.c.n_pages);
   const int n = __builtin_popcountll(mask);
   int firsts = (pg0 + lane) * kPage;  // first key of the page
   if (mask & (mask + 1)) {            // pages are missing in between: close the gaps

@@ -23,7 +23,7 @@ typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kStoreThreads;
 
 // Rows of one dtype, held as they are in memory until they are converted: N elements
 // in words() 32-bit words.

@@ -114,6 +114,10 @@ def test_bad_arguments():
         assert _status(fn, _cfg(n_q_heads=1024, n_kv_heads=1024), wide, 0, daf.CacheRows([0, 2 ** 31 - 1]), FAKE, FAKE,
                        0) == UNSUPPORTED
     long = _cache(max_seq_pages=2048)
+    # 2^25 workgroups of 256: more threads than a launch has
+    assert _status(attn, cfg, long, 0, daf.CacheRows([0, 2 ** 31 // cfg.n_q_heads - 1]), 131072, FAKE, FAKE, None, FAKE,
+                   2 ** 62, 0) == UNSUPPORTED
+    assert _status(daf.daf_pages_free, c, 2 ** 23 + 1, FAKE, 0) == UNSUPPORTED
     one = daf.CacheRows([0, 1])
     need = daf.daf_cache_attn_workspace_size(cfg, long, one, 131072)
     assert need > 0

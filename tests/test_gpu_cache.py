@@ -268,6 +268,23 @@ def test_what_no_row_sees_may_be_nan():
     p.check_attn(0, [0, 3, 4], [0, 1], q, [10, 70, 130, 64])
 
 
+def test_rows_before_a_sequence_see_nothing():
+    """Positions as low as they go: no key, whatever the pages hold; rows of the same block
+    that do see keys."""
+    p = _pair(pages=12, heads=1, d=64, hq=8, n_seqs=2, max_seq_pages=6)
+    for n in "kv":
+        p.t[n].view(torch.uint8).fill_(0x7F)  # NaN
+        p.o.code[n][:] = np.nan
+    rng = np.random.default_rng(9)
+    _fill(p, rng, [0], [128])
+    assert p.extend([0, 1], [172, 300]) == 0
+    q = torch.from_numpy(rng.standard_normal((20, 8, 64))).float()
+    for rows in (20, 8, 1):
+        o, lse = p.attn(0, [0, rows], [1], q[:rows].to(BF16).cuda(), [-2 ** 31] * rows)
+        assert not o.any() and torch.isneginf(lse).all()
+        p.check_attn(0, [0, rows], [0], q[:rows], ([-2 ** 31] * 5 + [70] * 15)[-rows:])
+
+
 def test_pages_that_are_not_there_hold_no_keys():
     p = _pair(pages=12, heads=2, d=64, hq=6, n_seqs=2, max_seq_pages=10)
     rng = np.random.default_rng(8)
