@@ -909,17 +909,19 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
   }
 }
 
-// Join the splits of one tile of 16 pairs: a wave per 16 features, a lane with the same
-// pair and features as in the kernel above, 8 splits in flight. The first ones do not
+// Join the splits of one tile of 16 pairs: a wave per 16 features, a workgroup of its own
+// (few tiles of many splits are read by the whole device), a lane with the same pair and
+// features as in the kernel above, 8 splits in flight. The first ones do not
 // wait for the length, which says how many splits hold keys; those beyond it were not
 // written and are left out.
 template <bool BF16, int D, int MT>
-__global__ __launch_bounds__(D * 4) void cache_wide_join_kernel(const CacheAttnLaunch p) {
+__global__ __launch_bounds__(64) void cache_wide_join_kernel(const CacheAttnLaunch p) {
   constexpr int DB = D / 16, FLIGHT = 8;
-  const int lane = threadIdx.x & 63, db = threadIdx.x >> 6, n16 = lane & 15, quad = lane >> 4;
-  const int tile = blockIdx.x % (kWaves * MT), rest = blockIdx.x / (kWaves * MT);
+  const int lane = threadIdx.x, n16 = lane & 15, quad = lane >> 4;
+  const int db = blockIdx.x % DB, job = blockIdx.x / DB;
+  const int tile = job % (kWaves * MT), rest = job / (kWaves * MT);
   const int h = rest % p.c.hkv, blk = rest / p.c.hkv;
-  const size_t part = (size_t)blockIdx.x * p.n_splits;
+  const size_t part = (size_t)job * p.n_splits;
   const float *lses = p.part_lse + part * 16 + n16, *os = p.part_o + (part * DB + db) * 256 + lane * 4;
   float lse[FLIGHT];
   f32x4 y[FLIGHT];
@@ -981,7 +983,7 @@ hipError_t launch(const CacheAttnLaunch &p, hipStream_t st) {
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.n_splits == 1) return e;
-  if (p.wide) cache_wide_join_kernel<BF16, D, MT><<<jobs * kWaves * MT, D * 4, 0, st>>>(p);
+  if (p.wide) cache_wide_join_kernel<BF16, D, MT><<<jobs * kWaves * MT * (D / 16), 64, 0, st>>>(p);
   else cache_line_join_kernel<BF16, D><<<pairs, kThreads, 0, st>>>(p);
   return hipGetLastError();
 }
