@@ -6,7 +6,9 @@
 // looks through refs for that many before anything is changed, so that a call does
 // all or nothing without the host. A second launch moves the bytes with the whole
 // device. Counts change by integer additions, so no result depends on an order.
-// Planning is bound by latency (a few passes over LDS and refs), copies by HBM.
+// Planning is bound by latency, copies by HBM. A plan's code runs once per call, so its
+// fetch is part of the latency: loops over sequences and pages take one per thread and
+// step and are not unrolled, and loads that depend on nothing come first.
 #include "cache.h"
 
 namespace daf {
@@ -16,7 +18,6 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kPlan = 1024;               // threads of a planning workgroup
-constexpr int kPer = kMaxPageSeqs / kPlan;  // sequences per thread
 constexpr int kHash = 2 * kMaxPageSeqs;   // slots of the set of sequences
 constexpr int kCopyThreads = 256;
 constexpr int kPiece = 4 * kCopyThreads * 16;  // bytes a workgroup moves at a time
@@ -68,32 +69,29 @@ __device__ __forceinline__ bool set_has(const int *set, int key) {
 // refs of the 16 pages from `at` on (a multiple of 4) as bits: used ones
 __device__ __forceinline__ unsigned used_bits(const int32_t *refs, int n_pages, int64_t at) {
   unsigned bits = 0;
-  i32x4 v[4];
+  i32x4 v[4] = {};
+  const int whole = n_pages & ~3;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const int64_t i = at + 4 * q;
-    v[q] = i32x4{};
-    if (i + 4 <= n_pages) {
-      v[q] = *reinterpret_cast<const i32x4 *>(refs + i);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[q][k] = i + k < n_pages ? refs[i + k] : 0;
-    }
-  }
+  for (int q = 0; q < 4; ++q)
+    if (at + 4 * q < whole) v[q] = *reinterpret_cast<const i32x4 *>(refs + at + 4 * q);
+  if (at + 16 > whole && at < n_pages)  // the last pages, one by one
+    for (int i = whole; i < n_pages; ++i) bits |= (unsigned)(refs[i] > 0) << (i - at);
 #pragma unroll
   for (int i = 0; i < 16; ++i) bits |= (unsigned)(v[i >> 2][i & 3] > 0) << i;
   return bits;
 }
 
 // Walks the free pages in order of their ids, 16 per thread and step, until `want` of
-// them were seen: f(rank, id) for each. Returns how many there were (<= want).
+// them were seen: f(rank, id) for each. Returns how many there were (<= want). used0:
+// used_bits of the thread's first 16 pages.
 template <typename F>
-__device__ __forceinline__ int64_t walk_free(const int32_t *refs, int n_pages, int64_t want, int *sh, F f) {
+__device__ __forceinline__ int64_t walk_free(const int32_t *refs, int n_pages, int64_t want, unsigned used0, int *sh,
+                                             F f) {
   int64_t seen = 0;
   for (int64_t base = 0; base < n_pages && seen < want; base += kPlan * 16) {
     const int64_t at = base + threadIdx.x * 16;
     const int here = (int)min(max((int64_t)n_pages - at, (int64_t)0), (int64_t)16);
-    unsigned free_ = ~used_bits(refs, n_pages, at) & ((1u << here) - 1);
+    unsigned free_ = ~(base ? used_bits(refs, n_pages, at) : used0) & ((1u << here) - 1);
     int total;
     int64_t rank = seen + block_scan(__builtin_popcount(free_), sh, &total);
     for (; free_ && rank < want; free_ &= free_ - 1, ++rank) f((int)rank, (int)at + __builtin_ctz(free_));
@@ -102,15 +100,7 @@ __device__ __forceinline__ int64_t walk_free(const int32_t *refs, int n_pages, i
   return seen < want ? seen : want;
 }
 
-// The same into a list of kShort in LDS, which is complete if `want` is not more.
-constexpr int kShort = kMaxPageSeqs;
-__device__ __forceinline__ int64_t list_free(const PoolView &c, int64_t want, int *sh, int *list) {
-  const int64_t found = walk_free(c.refs, c.n_pages, want, sh, [&](int rank, int id) {
-    if (rank < kShort) list[rank] = id;
-  });
-  __syncthreads();
-  return found;
-}
+constexpr int kShort = kMaxPageSeqs;  // lists of pages in LDS
 
 __device__ __forceinline__ int pages_of(int tokens) { return (tokens + kPage - 1) / kPage; }
 __device__ __forceinline__ bool in_range(int x, int n) { return (unsigned)x < (unsigned)n; }
@@ -118,136 +108,118 @@ __device__ __forceinline__ bool in_range(int x, int n) { return (unsigned)x < (u
 __global__ __launch_bounds__(kPlan) void pages_extend_kernel(const PoolView c, int n, const int32_t *seq,
                                                              const int32_t *n_new, int32_t *status) {
   __shared__ int set[kHash];
-  __shared__ int off[kMaxPageSeqs], list[kShort];
+  __shared__ int seqs[kMaxPageSeqs], held[kMaxPageSeqs], off[kMaxPageSeqs];  // off: first of its new pages
+  __shared__ int to[kMaxPageSeqs], list[kShort];
   __shared__ int64_t sh64[kPlan / 64];
   __shared__ int sh[kPlan / 64];
   __shared__ int bad;
   const int t = threadIdx.x;
+  const unsigned used0 = used_bits(c.refs, c.n_pages, t * 16);
   if (n > 1)  // one sequence has no double
     for (int i = t; i < kHash; i += kPlan) set[i] = -1;
   if (t == 0) bad = 0;
-  int s[kPer], have[kPer], add[kPer], need[kPer];
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const int i = t * kPer + k;
-    s[k] = i >= n ? -1 : seq ? seq[i] : i;
-    add[k] = i >= n ? 0 : n_new ? n_new[i] : 1;
-  }
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) have[k] = seq_len(c.len, c.n_seqs, c.max_seq_pages, s[k]);
-  __syncthreads();
-  int64_t mine = 0;
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    need[k] = 0;
-    if (t * kPer + k >= n) continue;
-    if (!in_range(s[k], c.n_seqs) || add[k] < 0 || (n > 1 && !set_add(set, s[k])) ||
-        (int64_t)have[k] + add[k] > (int64_t)c.max_seq_pages * kPage) {
-      bad = 1;
-      continue;
+  int64_t want = 0;
+  for (int i0 = 0; i0 < n; i0 += kPlan) {
+    const int i = i0 + t;
+    const int s = i >= n ? -1 : seq ? seq[i] : i, add = i >= n ? 0 : n_new ? n_new[i] : 1;
+    const int have = seq_len(c.len, c.n_seqs, c.max_seq_pages, s);
+    __syncthreads();  // the set is empty
+    int64_t need = 0;
+    if (i < n) {
+      if (!in_range(s, c.n_seqs) || add < 0 || (n > 1 && !set_add(set, s)) ||
+          (int64_t)have + add > (int64_t)c.max_seq_pages * kPage)
+        bad = 1;
+      else
+        need = pages_of(have + add) - pages_of(have);
     }
-    need[k] = pages_of(have[k] + add[k]) - pages_of(have[k]);
-    mine += need[k];
+    int64_t total;
+    const int64_t at = want + block_scan(need, sh64, &total);
+    if (i < n) seqs[i] = s, held[i] = have, off[i] = (int)at, to[i] = have + add;  // at is used if it fits
+    want += total;
   }
-  int64_t want;
-  int64_t at = block_scan(mine, sh64, &want);  // its barriers make `bad` final
+  __syncthreads();
   if (bad) {
     if (t == 0) *status = -1;
     return;
   }
-  const int64_t found = list_free(c, want, sh, list);
-  if (found < want) {
-    if (t == 0) *status = (int)min(want - found, (int64_t)INT32_MAX);
-    return;
-  }
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    off[t * kPer + k] = (int)at;  // want <= n_pages here
-    at += need[k];
-  }
-  __syncthreads();
   auto give = [&](int rank, int id) {
     int i = 0;  // the last request whose pages start at or below the rank
     for (int step = kMaxPageSeqs / 2; step; step >>= 1)
-      if (off[i + step] <= rank) i += step;
-    const int to = seq ? seq[i] : i;
-    const int first = pages_of(seq_len(c.len, c.n_seqs, c.max_seq_pages, to));
-    c.table[(int64_t)to * c.max_seq_pages + first + rank - off[i]] = id;
+      if (i + step < n && off[i + step] <= rank) i += step;
+    c.table[(int64_t)seqs[i] * c.max_seq_pages + pages_of(held[i]) + rank - off[i]] = id;
     c.refs[id] = 1;
   };
-  if (want <= kShort) {
-    for (int r = t; r < want; r += kPlan) give(r, list[r]);
-  } else {
-    walk_free(c.refs, c.n_pages, want, sh, give);
+  // a walk that looks for the pages and lists them; where the list is too short, another
+  // that gives them
+  const bool in_list = want <= kShort;
+#pragma unroll 1
+  for (int pass = 0; pass < (in_list ? 1 : 2); ++pass) {
+    const int64_t found = walk_free(c.refs, c.n_pages, want, used0, sh, [&](int rank, int id) {
+      if (in_list) list[rank] = id;
+      else if (pass) give(rank, id);
+    });
+    if (found < want) {
+      if (t == 0) *status = (int)min(want - found, (int64_t)INT32_MAX);
+      return;
+    }
+    __syncthreads();
   }
-  __syncthreads();  // lengths are read above
-#pragma unroll
-  for (int k = 0; k < kPer; ++k)
-    if (t * kPer + k < n) c.len[s[k]] = have[k] + add[k];
+  if (in_list)
+    for (int r = t; r < want; r += kPlan) give(r, list[r]);
+  for (int i = t; i < n; i += kPlan) c.len[seqs[i]] = to[i];
   if (t == 0) *status = 0;
 }
 
 __global__ __launch_bounds__(kPlan) void pages_fork_kernel(const PoolView c, const PageWork w, int n,
                                                            const int32_t *src, const int32_t *dst, int32_t *status) {
   __shared__ int set[kHash];
+  __shared__ int from[kMaxPageSeqs], to[kMaxPageSeqs], lens[kMaxPageSeqs];
+  __shared__ int last[kMaxPageSeqs], rank[kMaxPageSeqs];  // last page, where it is not full, and its copy's rank
   __shared__ int list[kShort];
   __shared__ int sh[kPlan / 64];
   __shared__ int bad;
   const int t = threadIdx.x;
+  const unsigned used0 = used_bits(c.refs, c.n_pages, t * 16);
   for (int i = t; i < kHash; i += kPlan) set[i] = -1;
   if (t == 0) bad = 0, w.count[0] = 0, w.count[1] = 0;
-  int s[kPer], d[kPer], L[kPer], held[kPer], last[kPer], mine = 0;
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const int i = t * kPer + k;
-    s[k] = i < n ? src[i] : -1;
-    d[k] = i < n ? dst[i] : -1;
+  int want = 0;
+  for (int i0 = 0; i0 < n; i0 += kPlan) {
+    const int i = i0 + t;
+    const int s = i < n ? src[i] : -1, d = i < n ? dst[i] : -1;
+    const int held = in_range(d, c.n_seqs) ? c.len[d] : 0;
+    const int L = seq_len(c.len, c.n_seqs, c.max_seq_pages, s);
+    const int page = L % kPage ? c.table[(int64_t)s * c.max_seq_pages + L / kPage] : -1;
+    __syncthreads();  // the set is empty
+    if (i < n && (!in_range(s, c.n_seqs) || !in_range(d, c.n_seqs) || held > 0 || !set_add(set, d))) bad = 1;
+    int total;
+    const int at = want + block_scan((int)in_range(page, c.n_pages), sh, &total);  // one that is not there stays so
+    if (i < n) from[i] = s, to[i] = d, lens[i] = L, last[i] = page, rank[i] = at;
+    want += total;
   }
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    held[k] = in_range(d[k], c.n_seqs) ? c.len[d[k]] : 0;
-    L[k] = seq_len(c.len, c.n_seqs, c.max_seq_pages, s[k]);
-  }
-#pragma unroll
-  for (int k = 0; k < kPer; ++k)  // the last page, where it is not full
-    last[k] = L[k] % kPage ? c.table[(int64_t)s[k] * c.max_seq_pages + L[k] / kPage] : -1;
-  auto own = [&](int k) { return in_range(last[k], c.n_pages); };  // one that is not there stays so
   __syncthreads();
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    if (t * kPer + k >= n) continue;
-    if (!in_range(s[k], c.n_seqs) || !in_range(d[k], c.n_seqs) || held[k] > 0 || !set_add(set, d[k])) bad = 1;
-    mine += own(k);
-  }
-  int want;
-  int rank = block_scan(mine, sh, &want);
-#pragma unroll
-  for (int k = 0; k < kPer; ++k)
-    if (in_range(s[k], c.n_seqs) && !bad && set_has(set, s[k])) bad = 1;
+  if (!bad)
+    for (int i = t; i < n; i += kPlan)
+      if (set_has(set, from[i])) bad = 1;
+  const int found = (int)walk_free(c.refs, c.n_pages, want, used0, sh, [&](int r, int id) { list[r] = id; });
   __syncthreads();
-  if (bad) {
-    if (t == 0) *status = -1;
+  if (bad || found < want) {
+    if (t == 0) *status = bad ? -1 : want - found;
     return;
   }
-  const int found = (int)list_free(c, want, sh, list);
-  if (found < want) {
-    if (t == 0) *status = want - found;
-    return;
-  }
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    if (t * kPer + k >= n) continue;
-    if (L[k] % kPage) {
-      const int id = own(k) ? list[rank] : last[k];
-      c.table[(int64_t)d[k] * c.max_seq_pages + L[k] / kPage] = id;
-      if (own(k)) {
-        w.src[rank] = last[k];
-        w.dst[rank] = id;
+  for (int i = t; i < n; i += kPlan) {
+    const int L = lens[i];
+    if (L % kPage) {
+      int id = last[i];
+      if (in_range(id, c.n_pages)) {
+        const int r = rank[i];
+        w.src[r] = id;
+        id = list[r];
+        w.dst[r] = id;
         c.refs[id] = 1;
-        ++rank;
       }
+      c.table[(int64_t)to[i] * c.max_seq_pages + L / kPage] = id;
     }
-    c.len[d[k]] = L[k];
+    c.len[to[i]] = L;
   }
   if (t == 0) {
     w.count[0] = want;
@@ -256,16 +228,19 @@ __global__ __launch_bounds__(kPlan) void pages_fork_kernel(const PoolView c, con
   }
 }
 
-constexpr int kRowsPer = 8;
-// Rows of the launch, kRowsPer per thread and step; a row that is its page's first in its
-// request stands for the page. The pages that are shared are listed in order.
+// Rows of the launch, kRowsPer per thread and step. A row that is its page's first in its
+// request stands for the page: these are listed, and the list's shared pages again.
+constexpr int kRowsPer = 8, kStepRows = kRowsPer * kPlan;
 __global__ __launch_bounds__(kPlan) void pages_unshare_kernel(const UnshareLaunch p) {
   __shared__ int set[2 * kMaxCacheReqs];
   __shared__ int seqs[kMaxCacheReqs], lens[kMaxCacheReqs], cu[kMaxCacheReqs + 1];
+  __shared__ int touched_req[kStepRows], touched_col[kStepRows];
+  __shared__ int old[kShort], of_seq[kShort], of_col[kShort], list[kShort];  // the shared ones and their new pages
   __shared__ int sh[kPlan / 64];
   __shared__ int bad;
   const PoolView &c = p.c;
   const int t = threadIdx.x;
+  const unsigned used0 = used_bits(c.refs, c.n_pages, t * 16);
   if (t < 2 * kMaxCacheReqs) set[t] = -1;
   if (t == 0) bad = 0, p.w.count[0] = 0, p.w.count[1] = 0;
   if (t <= p.n_req) cu[t] = p.cu[t];
@@ -283,60 +258,84 @@ __global__ __launch_bounds__(kPlan) void pages_unshare_kernel(const UnshareLaunc
   }
   const int rows = cu[p.n_req];
   int64_t want = 0;
-  for (int64_t base = 0; base < rows; base += kPlan * kRowsPer) {
-    int64_t slot[kRowsPer];
-    int page[kRowsPer], seq_[kRowsPer], col[kRowsPer], mine = 0;
-    bool first[kRowsPer];
+  for (int64_t base = 0; base < rows; base += kStepRows) {
+    const int64_t i0 = base + t * kRowsPer;
+    const int here = (int)min(max(rows - i0, (int64_t)0), (int64_t)kRowsPer);
+    int pos[kRowsPer + 1] = {}, of[kRowsPer], col[kRowsPer];  // pos: from the row before the thread's first on
+    if (p.pos && here > 0) {
+      const int32_t *at = p.pos + i0;
+      pos[0] = at[i0 > 0 ? -1 : 0];
+      if (here == kRowsPer) {
+#pragma unroll
+        for (int q = 0; q < kRowsPer; q += 4) {
+          const i32x4 v = *reinterpret_cast<const i32x4 *>(at + q);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) pos[1 + q + k] = v[k];
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < kRowsPer; ++k)
+          if (k < here) pos[1 + k] = at[k];
+      }
+    }
+    int b = 0;  // request of the row
+    for (int step = kMaxCacheReqs / 2; step; step >>= 1)
+      if (b + step < p.n_req && cu[b + step] <= i0) b += step;
+    int row0 = cu[b], next = cu[b + 1], L = lens[b];
+    unsigned first = 0;
 #pragma unroll
     for (int k = 0; k < kRowsPer; ++k) {
-      const int64_t i = base + t * kRowsPer + k;
-      first[k] = false;
-      if (i >= rows) continue;
-      int b = 0;
-      for (int step = kMaxCacheReqs / 2; step; step >>= 1)
-        if (b + step < p.n_req && cu[b + step] <= i) b += step;
-      const int j = (int)i - cu[b], L = lens[b];
-      const int at = p.pos ? p.pos[i] : L - (cu[b + 1] - cu[b]) + j;
-      const int before = j == 0 ? -1 : p.pos ? p.pos[i - 1] : at - 1;
-      if (p.pos && j > 0 && before >= at) bad = 1;  // a page would be listed twice
-      first[k] = at >= 0 && at < L && (before < 0 || before / kPage != at / kPage);
-      seq_[k] = seqs[b];
+      if (k >= here) continue;
+      const int i = (int)i0 + k;
+      while (next <= i) row0 = next, ++b, next = cu[b + 1], L = lens[b];
+      const int at = p.pos ? pos[k + 1] : L - next + i, before = p.pos ? pos[k] : at - 1;
+      if (i > row0 && before >= at) bad = 1;  // a page would be listed twice
+      if (at >= 0 && at < L && (i == row0 || before < 0 || before / kPage != at / kPage)) first |= 1u << k;
+      of[k] = b;
       col[k] = at / kPage;
-      slot[k] = (int64_t)seq_[k] * c.max_seq_pages + col[k];
     }
-#pragma unroll
-    for (int k = 0; k < kRowsPer; ++k) page[k] = first[k] ? c.table[slot[k]] : -1;
-#pragma unroll
-    for (int k = 0; k < kRowsPer; ++k) {
-      first[k] = in_range(page[k], c.n_pages) && c.refs[page[k]] > 1;
-      mine += first[k];
-    }
-    int total;
-    int64_t rank = want + block_scan(mine, sh, &total);
+    int touched;
+    int to = block_scan(__builtin_popcount(first), sh, &touched);
 #pragma unroll
     for (int k = 0; k < kRowsPer; ++k)
-      if (first[k]) {
-        if (rank < c.n_pages) p.w.src[rank] = page[k], p.w.seq[rank] = seq_[k], p.w.aux[rank] = col[k];
-        ++rank;
+      if ((first >> k) & 1) touched_req[to] = of[k], touched_col[to++] = col[k];
+    __syncthreads();
+    for (int e0 = 0; e0 < touched; e0 += kPlan) {
+      const int e = e0 + t, seq = e < touched ? seqs[touched_req[e]] : 0, col = e < touched ? touched_col[e] : 0;
+      const int page = e < touched ? c.table[(int64_t)seq * c.max_seq_pages + col] : -1;
+      const bool shared = in_range(page, c.n_pages) && c.refs[page] > 1;
+      int total;
+      const int64_t r = want + block_scan((int)shared, sh, &total);
+      if (shared && r < c.n_pages) {
+        p.w.src[r] = page, p.w.seq[r] = seq, p.w.aux[r] = col;
+        if (r < kShort) old[r] = page, of_seq[r] = seq, of_col[r] = col;
       }
-    want += total;
+      want += total;
+    }
+    __syncthreads();  // the lists of this step are read
   }
-  if (bad) {  // final since the last scan's barriers
+  __syncthreads();
+  if (bad) {
     if (t == 0) *p.status = -1;
     return;
   }
   // free ids are found before any count changes: none of the old pages is among them
-  const int64_t found = walk_free(c.refs, c.n_pages, want, sh, [&](int r, int id) { p.w.dst[r] = id; });
+  const int64_t found = walk_free(c.refs, c.n_pages, want, used0, sh, [&](int r, int id) {
+    p.w.dst[r] = id;
+    if (r < kShort) list[r] = id;
+  });
   if (found < want) {
     if (t == 0) *p.status = (int)min(want - found, (int64_t)INT32_MAX);
     return;
   }
   __syncthreads();
   for (int64_t r = t; r < want; r += kPlan) {
-    const int id = p.w.dst[r];
-    c.table[(int64_t)p.w.seq[r] * c.max_seq_pages + p.w.aux[r]] = id;
+    const bool in_lds = r < kShort;
+    const int id = in_lds ? list[r] : p.w.dst[r], from = in_lds ? old[r] : p.w.src[r];
+    const int seq = in_lds ? of_seq[r] : p.w.seq[r], col = in_lds ? of_col[r] : p.w.aux[r];
+    c.table[(int64_t)seq * c.max_seq_pages + col] = id;
     c.refs[id] = 1;
-    atomicAdd(&c.refs[p.w.src[r]], -1);
+    atomicAdd(&c.refs[from], -1);
   }
   if (t == 0) {
     p.w.count[0] = (int)want;
