@@ -213,8 +213,7 @@ size_t wide_pairs(const daf_attn_cfg_t *cfg, int64_t blocks, int block_rows) {
   return (size_t)blocks * cfg->n_kv_heads * block_rows;
 }
 
-// Kernel and pages per split, from the sizes that the host knows: about two
-// workgroups per CU.
+// Kernel and its splits, from the sizes that the host knows.
 AttnPlan plan_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_cache_rows_t *rows, int32_t max_len) {
   AttnPlan a{};
   int64_t most = 0, blocks = 0;
@@ -228,15 +227,22 @@ AttnPlan plan_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_ca
   const int64_t pages = std::max<int64_t>(1, ((int64_t)max_len + kPage - 1) / kPage);
   const int64_t jobs = std::max<int64_t>(1, blocks * c->n_kv_heads);
   if (a.wide) {
+    // Two workgroups per CU, at once (128 rows of 7 heads on each of 4 over 32896 keys, us
+    // by workgroups in all: 256 87.8 + 5.5, 512 79.3 + 7.7, 768 83.6 + 9.7, 1024 86.7 + 11.8).
     int64_t splits = std::max<int64_t>(std::max<int64_t>(1, 512 / jobs), (pages + kMaxSplitPages - 1) / kMaxSplitPages);
     splits = std::min(splits, (pages + kMinSplitPages - 1) / kMinSplitPages);
     a.split_pages = (int)((pages + splits - 1) / splits);
     a.n_splits = (int)((pages + a.split_pages - 1) / a.split_pages);
   } else {
-    // Workgroups per head on the line of all row blocks' pages. Up to 16 pages, four for
-    // each wave, are a workgroup's own: a join would take longer.
+    // One workgroup per row block and head, or workgroups per head on the line of all row
+    // blocks' pages. One takes up to 16 pages sooner than a join does (us, one and the
+    // line: a row of 1024 keys 11.3 and 15.3, of 1500 keys 13.5 and 12.4). With one per CU
+    // the device is full without the line's ends inside of workgroups (64 rows by 4 heads
+    // of up to 2000 keys, ragged, 18.7 and 28.4, 4000 keys 32.4 and 40.9; 128 rows of 4000
+    // keys 94.6 and 104): up to 64 pages, of which a single long sequence among short ones
+    // takes about 30 us.
     a.n_splits = 1;
-    if (pages > 16) {
+    if (pages > (jobs >= 256 ? 64 : 16)) {
       const int64_t line = std::min<int64_t>(blocks, INT32_MAX) * pages;
       // Two workgroups per CU hide the ends of requests behind each other's loads; within
       // one request one is enough, with half as much to join (bf16 of 128 features, us with

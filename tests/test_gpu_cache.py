@@ -268,6 +268,25 @@ def test_what_no_row_sees_may_be_nan():
     p.check_attn(0, [0, 3, 4], [0, 1], q, [10, 70, 130, 64])
 
 
+@pytest.mark.parametrize("dtype,d,most", [(BF16, 64, 3), (F32, 128, 3), (BF16, 128, 40)])
+def test_more_requests_than_a_launch_takes_on_long_tables(dtype, d, most):
+    """300 requests of 0 to 3 rows, then with some of 40 among them, planned for far longer
+    sequences than most have: every launch shares its workgroups out over the pages, and
+    the launches share the workspace."""
+    n = 300
+    p = _pair(pages=700, heads=1, d=d, n_seqs=n, max_seq_pages=80, hq=3, dtype=dtype)
+    rng = np.random.default_rng(most + d)
+    seq = rng.permutation(n).tolist()
+    lens = rng.integers(0, 100, n).tolist()
+    lens[7], lens[260], lens[299] = 4500, 1500, 777
+    _fill(p, rng, seq, lens)
+    few = rng.integers(0, 4, n).tolist()
+    for i in (3, 7, 250, 258, 299):
+        few[i] = most
+    q = torch.from_numpy(rng.standard_normal((sum(few), 3, d))).float()
+    p.check_attn(0, _cu(few), seq, q)
+
+
 def test_rows_before_a_sequence_see_nothing():
     """Positions as low as they go: no key, whatever the pages hold; rows of the same block
     that do see keys."""
