@@ -6,10 +6,7 @@
 // rescaled where m grows (fp32). The G query heads of a K/V head share its pages,
 // so a row block is 16 (row, head) pairs of one K/V head.
 //
-// Data path of a wave, one page (64 keys) of one head at a time:
-//  * K and V go from memory to registers in the layout that the matrix
-//    instructions take, 16 bytes per lane and load; the next page's loads are in
-//    flight while a page is worked on. No LDS.
+// Matrix instructions (both kernels):
 //  * e4m3 codes become bf16 exactly, and times their scale (a power of two) by the
 //    same conversion instruction, so no multiplication carries the scales.
 //  * S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_16x16x32_bf16. With the rows of K
@@ -17,10 +14,20 @@
 //    of the operand, a lane of group g (lane / 16) ends up with the probabilities
 //    of keys 16 g .. 16 g + 15 of row lane % 16, which is how the second product
 //    wants them, and V^T, stored transposed, is read as 16 consecutive keys.
+//  * bf16: a weight's rounding to bf16 is its only one, and the row is divided by the
+//    sum of the rounded weights (one more product, with ones), which leaves a mean of
+//    values; the LSE takes the sum of the unrounded ones. (8-bit scores are not exact
+//    enough: the 8-bit product keeps about 13 bits of a small term beside a large one.)
 //  * fp32: q and the probabilities enter as three bf16 terms each.
-// Few rows: the four waves of a workgroup take its pages in turn and join their (m,
-// sum, O) through LDS; bound by the pages' bytes. Many rows: below. What workgroups
-// share of a row block is joined by a second kernel.
+//
+// Few rows: a wave takes a page (64 keys) of one head at a time from memory to
+// registers, in the layout that the matrix instructions take, 16 bytes per lane and
+// load, with the next page's loads in flight and without LDS; the waves of a workgroup
+// take its pages in turn and join their (m, sum, O) through LDS. Bound by the pages'
+// bytes: 131072 keys of 4 heads of 128 (134 MB) in 31 us, 4.3 TB/s; a short sequence
+// by what one CU keeps in flight (777 keys 10 us, 64 keys 4.7; 8 waves or 4).
+// Many rows: below. What workgroups share of a row block is joined by a second kernel
+// (4 to 5 us, most of it its launch).
 #include <math.h>
 
 #include <type_traits>
@@ -568,9 +575,15 @@ __global__ __launch_bounds__(kThreads) void cache_line_join_kernel(const CacheAt
 // Half pages (32 keys) go through three stages, each of another half: the scores of
 // half h + 1, the weights of half h and the value product of half h - 1 make one
 // block of straight code, in which every matrix instruction has 3 to 4 vector
-// instructions of the other stages beside it (one wave's matrix and vector
-// instructions overlap when they are mixed: 1 and 3 take 9.4 ns on a SIMD with two
-// waves, against 7.8 and 4.8 alone; 4 and 16 in turn take 40 of 31 and 26).
+// instructions of the other stages beside it: a SIMD with two waves overlaps them (4
+// matrix and 9 vector instructions in turn take 35.5 ns, alone 27.5 and 19.9).
+//
+// Bound by that issue: 128 rows of 28 heads on 4 of 128 over 32896 keys, 60 GFLOP, take
+// 75 us (800 TFLOP/s), with the matrix cores busy half of the time at 2.1 GHz; the
+// prologue is 4 us of it, and of the two workgroups of a CU the older is served first
+// and leaves the younger alone for the last quarter. 8 waves per workgroup,
+// weights through LDS, K converted once for all waves and pages further ahead did not
+// take less.
 //
 // The reference m of a row is an integer (base-2 units), so that raising it scales O,
 // the sum and the weights in flight by a power of two, exactly. It is raised, to the
@@ -578,7 +591,7 @@ __global__ __launch_bounds__(kThreads) void cache_line_join_kernel(const CacheAt
 // 2^8, so a weight is at most that.
 constexpr int kStages = 3;
 constexpr float kNoReference = -3e38f;  // before the first visible key
-constexpr float kSlack = 8.f;
+constexpr float kSlack = 8.f;           // a weight is at most 2^kSlack
 
 template <int N>
 __device__ __forceinline__ void wait_vm() {

@@ -11,7 +11,11 @@
 // one writer. K goes 8 elements per lane; for V a lane takes two features of 16
 // (D = 64: 8) consecutive slots, so that its transposed codes are whole pieces
 // without a pass through LDS. All rows are loaded before the maximum is taken.
-// Bound by HBM for long runs of rows, by latency for a few.
+// Bound by HBM for long runs of rows: 32768 rows of 4 heads of 128 (67 MB in bf16, 34 MB
+// of codes) are written in 28 us and read back in 17; by latency for scattered ones
+// (4915 rows over 512 pages, 55 MB, 23 us: chains of dependent loads, a page's at a
+// time, of which more rows per unit or fewer took as long) and for a few (32 rows 5.0 and
+// 3.6 us).
 #include "cache.h"
 
 namespace daf {
