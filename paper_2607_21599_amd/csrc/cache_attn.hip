@@ -579,11 +579,11 @@ __global__ __launch_bounds__(kThreads) void cache_line_join_kernel(const CacheAt
 // matrix and 9 vector instructions in turn take 35.5 ns, alone 27.5 and 19.9).
 //
 // Bound by that issue: 128 rows of 28 heads on 4 of 128 over 32896 keys, 60 GFLOP, take
-// 75 us (800 TFLOP/s), with the matrix cores busy half of the time at 2.1 GHz; the
-// prologue is 4 us of it, and of the two workgroups of a CU the older is served first
-// and leaves the younger alone for the last quarter. 8 waves per workgroup,
-// weights through LDS, K converted once for all waves and pages further ahead did not
-// take less.
+// 76 us (790 TFLOP/s), of which a SIMD's matrix instructions are 38% and its vector
+// instructions 43% (per 64 keys and 32 rows 34 and 150, 64 of them conversions of codes).
+// The prologue is 4 us, and of the two workgroups of a CU the older is served first and
+// leaves the younger alone for the last quarter. 8 waves per workgroup, weights through
+// LDS, K converted once for all waves and pages further ahead did not take less.
 //
 // The reference m of a row is an integer (base-2 units), so that raising it scales O,
 // the sum and the weights in flight by a power of two, exactly. It is raised, to the

@@ -287,6 +287,24 @@ def test_more_requests_than_a_launch_takes_on_long_tables(dtype, d, most):
     p.check_attn(0, _cu(few), seq, q)
 
 
+@pytest.mark.parametrize("dtype,rows", [(BF16, 1), (BF16, 9), (F32, 1), (F32, 30)])
+def test_max_len_bounds_what_counts(dtype, rows):
+    """Tokens past max_len do not count, and rows without positions end there; sequences
+    named twice; the same in one workgroup, on a line and for many rows."""
+    p = _pair(pages=130, heads=2, d=64, hq=16, n_seqs=3, max_seq_pages=100, dtype=dtype)
+    rng = np.random.default_rng(rows)
+    lens = [5200, 700, 40]
+    _fill(p, rng, [0, 1, 2], lens)
+    seq = [1, 0, 2, 0, 1]
+    q = torch.from_numpy(rng.standard_normal((5 * rows, 16, 64))).float()
+    pos = np.concatenate([np.sort(rng.choice(6000, rows, replace=False)) for _ in seq]).tolist()
+    for max_len in (0, 1, 300, 5199, 6400):
+        for s in range(3):
+            p.o.len[s] = min(lens[s], max_len)
+        for at in (None, pos):
+            p.check_attn(0, _cu([rows] * 5), seq, q, at, max_len=max_len)
+
+
 def test_rows_before_a_sequence_see_nothing():
     """Positions as low as they go: no key, whatever the pages hold; rows of the same block
     that do see keys."""
