@@ -236,13 +236,13 @@ AttnPlan plan_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_ca
   } else {
     // One workgroup per row block and head, or workgroups per head on the line of all row
     // blocks' pages. One takes up to 16 pages sooner than a join does (us, one and the
-    // line: a row of 1024 keys 11.3 and 15.3, of 1500 keys 13.5 and 12.4). With one per CU
-    // the device is full without the line's ends inside of workgroups (64 rows by 4 heads
-    // of up to 2000 keys, ragged, 18.7 and 28.4, 4000 keys 32.4 and 40.9; 128 rows of 4000
-    // keys 94.6 and 104): up to 64 pages, of which a single long sequence among short ones
-    // takes about 30 us.
+    // line: a row of 1024 keys 11.3 and 15.3, of 1500 keys 13.5 and 12.4). With more of
+    // them the device fills without the line's ends inside of workgroups (ragged rows by 4
+    // heads over up to 2000 keys: 24 rows 16.0 and 18.5, 64 rows 18.7 and 28.4, 64 in fp32
+    // 22.6 and 36.9; 64 rows over up to 4000 keys 32.4 and 40.9): up to a third as many
+    // pages as workgroups, and 64, of which a long sequence among short ones takes 27 us.
     a.n_splits = 1;
-    if (pages > (jobs >= 256 ? 64 : 16)) {
+    if (pages > std::clamp<int64_t>(jobs / 3, 16, 64)) {
       const int64_t line = std::min<int64_t>(blocks, INT32_MAX) * pages;
       // Two workgroups per CU hide the ends of requests behind each other's loads; within
       // one request one is enough, with half as much to join (bf16 of 128 features, us with
