@@ -499,7 +499,9 @@ daf_status_t daf_cache_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *cache,
 size_t daf_pages_workspace_size(const daf_cache_t *cache);
 
 /* Lengthen n (<= 4096) distinct sequences by n_new[i] >= 0 tokens: pages as needed,
- * len raised. seq NULL: sequences 0 .. n-1; n_new NULL: one token each. */
+ * len raised. The scales of the pages taken become 0 in every layer, so that nothing of
+ * what lay there counts in a later write; a token's K/V are undefined until it is
+ * written. seq NULL: sequences 0 .. n-1; n_new NULL: one token each. */
 daf_status_t daf_pages_extend(const daf_cache_t *cache, int32_t n,
                               const int32_t *seq, const int32_t *n_new,
                               int32_t *status, hipStream_t stream);

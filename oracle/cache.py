@@ -146,6 +146,8 @@ class CacheOracle:
             for i in range(self.used(s), self.used(s) + c):
                 self.table[s, i] = ids.pop(0)
                 self.refs[self.table[s, i]] = 1
+                for x in self.scale.values():
+                    x[:, self.table[s, i]] = 0
             self.len[s] += n
         return 0
 

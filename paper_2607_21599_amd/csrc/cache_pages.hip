@@ -6,7 +6,7 @@
 // looks through refs for that many before anything is changed, so that a call does
 // all or nothing without the host. A second launch moves the bytes with the whole
 // device. Counts change by integer additions, so no result depends on an order.
-// Planning is bound by latency (4 to 7 us, unshare of 4915 rows 10.6), copies by HBM (512
+// Planning is bound by latency (4 to 8 us, unshare of 4915 rows 10.6), copies by HBM (512
 // pages of 128 KiB 31 us, 4.3 TB/s). A plan's code runs once per call, so its fetch is
 // part of the latency: loops over sequences and pages take one per thread and
 // step and are not unrolled, and loads that depend on nothing come first.
@@ -143,11 +143,14 @@ __global__ __launch_bounds__(kPlan) void pages_extend_kernel(const PoolView c, i
     if (t == 0) *status = -1;
     return;
   }
-  auto give = [&](int rank, int id) {
+  auto entry = [&](int rank) {  // the table entry that the rank-th page is for
     int i = 0;  // the last request whose pages start at or below the rank
     for (int step = kMaxPageSeqs / 2; step; step >>= 1)
       if (i + step < n && off[i + step] <= rank) i += step;
-    c.table[(int64_t)seqs[i] * c.max_seq_pages + pages_of(held[i]) + rank - off[i]] = id;
+    return c.table + (int64_t)seqs[i] * c.max_seq_pages + pages_of(held[i]) + rank - off[i];
+  };
+  auto give = [&](int rank, int id) {
+    *entry(rank) = id;
     c.refs[id] = 1;
   };
   // a walk that looks for the pages and lists them; where the list is too short, another
@@ -169,6 +172,24 @@ __global__ __launch_bounds__(kPlan) void pages_extend_kernel(const PoolView c, i
     for (int r = t; r < want; r += kPlan) give(r, list[r]);
   for (int i = t; i < n; i += kPlan) c.len[seqs[i]] = to[i];
   if (t == 0) *status = 0;
+  if (want == 0) return;
+  // Scale 0, in every layer: what a page's last owner or a new pool left there would
+  // count for the tokens that a write leaves out. (The pages' heads have 4 KiB of K
+  // each, so their number fits 32 bits.) Few beside the bytes that are written there
+  // next: a plan of 512 pages of 4 heads in 2 layers takes 7.7 us, without them 7.1.
+  __syncthreads();  // ids past the list are read from the table
+  const unsigned hkv = c.hkv, all = (unsigned)want * hkv;
+  for (unsigned j = t; j < all; j += kPlan) {
+    const unsigned r = j / hkv;
+    const int64_t id = in_list ? list[r] : *entry(r);
+    float *ks = c.k_scale + id * hkv + j % hkv, *vs = c.v_scale + id * hkv + j % hkv;
+#pragma unroll 1
+    for (int layer = 0; layer < c.n_layers; ++layer) {
+      const int64_t at = (int64_t)layer * c.n_pages * hkv;
+      ks[at] = 0.f;
+      vs[at] = 0.f;
+    }
+  }
 }
 
 __global__ __launch_bounds__(kPlan) void pages_fork_kernel(const PoolView c, const PageWork w, int n,

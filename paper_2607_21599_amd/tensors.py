@@ -131,7 +131,7 @@ class LayerBuffers:
 def cache_tensors(n_layers: int, n_pages: int, n_kv_heads: int, head_dim: int, n_seqs: int, max_seq_pages: int,
                   device="cuda") -> dict:
     """The tensors of an empty paged 8-bit cache, for ``Cache.from_tensors``. The
-    codes and scales need no values; nothing reads them before they are written."""
+    codes and scales need no values: a page's scales become 0 when it is taken."""
     def empty(*shape, dtype):
         return torch.empty(shape, dtype=dtype, device=device)
 
