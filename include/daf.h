@@ -468,7 +468,9 @@ size_t daf_cache_attn_workspace_size(const daf_attn_cfg_t *cfg,
  * A row sees the keys 0 .. its position of its sequence, as far as len goes (pos =
  * NULL: causal, aligned to the end; pos need not increase here). A row that sees
  * no key gets o = 0 and lse = -infinity. Keys that no row of the call sees may
- * hold anything, NaN included; all others must be finite.
+ * hold anything, NaN included; all others must be finite. A score of NaN or infinity,
+ * as q may give, makes the row's o and lse of that head NaN; one of -infinity counts as
+ * a key that is not seen.
  *   max_len: a HOST bound on the sequences' len (at most max_seq_pages * 64) that
  * the launch is planned for; len is read on the device, at most max_len counts.
  *   Softmax and sums in fp32; the codes, and q in bf16, enter the products

@@ -88,6 +88,10 @@ __device__ __forceinline__ float row_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
+// 1 / sum of a row's weights. 0 is the row that sees no key; a NaN among the scores makes
+// the sum NaN, which goes on to o and the LSE (a test for > 0 would turn it into no key).
+__device__ __forceinline__ float over(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
+
 // TERMS bf16 values whose sum is x: one rounding for bf16, 24 bits for fp32
 template <int TERMS>
 __device__ __forceinline__ void split_terms(const float (&x)[8], bf16x8 (&out)[TERMS]) {
@@ -374,8 +378,8 @@ __device__ __forceinline__ void few_rows(const CacheAttnLaunch &p, FewShared<D> 
     l += w[k] * sh.l[k][rr];
     sum += w[k] * sh.r[k][rr];
   }
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
-  const float lse = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+  const float inv = over(sum);
+  const float lse = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 #pragma unroll
   for (int c = c0 * 4; c < D; c += 64) {
     float x[4] = {};
@@ -536,14 +540,14 @@ __global__ __launch_bounds__(kThreads) void cache_line_join_kernel(const CacheAt
       y[j] = s < n ? *reinterpret_cast<const f32x4 *>(p.part_o + at(s) * D + c * 4) : f32x4{};
     }
     const float to = fmaxf(m, fmaxf(fmaxf(lse[0], lse[1]), fmaxf(lse[2], lse[3])));
-    if (to == -INFINITY) continue;  // a row that sees no key there
-    const float a = __expf(m - to);
+    const float ref = to == -INFINITY ? 0.f : to;  // a row that sees no key there, or NaN
+    const float a = __expf(m - ref);
     m = to;
     l *= a;
     x *= a;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float w = __expf(lse[j] - to);
+      const float w = __expf(lse[j] - ref);
       l += w;
       x += w * y[j];
     }
@@ -561,10 +565,10 @@ __global__ __launch_bounds__(kThreads) void cache_line_join_kernel(const CacheAt
     l += w * sh_l[k];
     x += w * sh_o[k][c];
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const float inv = over(l);
   const float y[4] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
   store_out<BF16>(p, row, head, c * 4, y, D);
-  if (c == 0 && p.lse) p.lse[(size_t)head * p.lse_stride + row] = l > 0.f ? m + __logf(l) : -INFINITY;
+  if (c == 0 && p.lse) p.lse[(size_t)head * p.lse_stride + row] = l == 0.f ? -INFINITY : m + __logf(l);
 }
 
 // ---- many rows -------------------------------------------------------------------
@@ -900,8 +904,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const float l = row_sum(w.l[mt]), sum = BF16 ? w.rounded[mt][0] : l;
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
-    const float lse = l > 0.f ? (w.m[mt] + log2f(l)) * kLn2 : -INFINITY;
+    const float inv = over(sum);
+    const float lse = l == 0.f ? -INFINITY : (w.m[mt] + log2f(l)) * kLn2;
     const int tile = (r.block * kWaves + wave) * MT + mt, idx = tile * 16 + n16;
     if (p.n_splits > 1) {
       const size_t part = (((size_t)(blk * p.c.hkv + h) * kWaves + wave) * MT + mt) * p.n_splits + split;
@@ -975,11 +979,11 @@ __global__ __launch_bounds__(64) void cache_wide_join_kernel(const CacheAttnLaun
     load(s0);
   }
   if (idx >= total) return;
-  x *= l > 0.f ? 1.f / l : 0.f;
+  x *= over(l);
   const int row = r.row0 + idx / p.group, head = h * p.group + idx % p.group;
   const float out[4] = {x[0], x[1], x[2], x[3]};
   store_out<BF16>(p, row, head, db * 16 + quad * 4, out, D);
-  if (db == 0 && quad == 0 && p.lse) p.lse[(size_t)head * p.lse_stride + row] = l > 0.f ? m + __logf(l) : -INFINITY;
+  if (db == 0 && quad == 0 && p.lse) p.lse[(size_t)head * p.lse_stride + row] = l == 0.f ? -INFINITY : m + __logf(l);
 }
 
 template <bool BF16, int D>
