@@ -473,12 +473,10 @@ size_t daf_cache_attn_workspace_size(const daf_attn_cfg_t *cfg,
  * a key that is not seen.
  *   max_len: a HOST bound on the sequences' len (at most max_seq_pages * 64) that
  * the launch is planned for; len is read on the device, at most max_len counts.
- *   Softmax and sums in fp32; the codes, and q in bf16, enter the products
- * exactly. bf16: probabilities are rounded to bf16 for the value product, which is
- * divided by the sum of the rounded ones (a row is a weighted mean of values with
- * weights that sum to one); the LSE is that of the unrounded ones. fp32: q and the
- * probabilities enter as three bf16 terms each (24 bits). Sums hold probabilities
- * of at most 2^8, so |V| must stay below 2^100.
+ *   Softmax and sums in fp32; the codes, and q in bf16, enter the products exactly.
+ * bf16: a probability enters the value product with an error of at most 2^-11 of itself,
+ * or 2^-35 of its row's largest one; fp32: q and the probabilities enter as three bf16
+ * terms each (24 bits). |V| must stay below 2^100.
  *   workspace: at least daf_cache_attn_workspace_size bytes, 16-byte aligned,
  * contents undefined after the call; calls that may run at the same time, captured
  * ones included, need one each. */

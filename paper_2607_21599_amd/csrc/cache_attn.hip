@@ -14,10 +14,12 @@
 //    of the operand, a lane of group g (lane / 16) ends up with the probabilities
 //    of keys 16 g .. 16 g + 15 of row lane % 16, which is how the second product
 //    wants them, and V^T, stored transposed, is read as 16 consecutive keys.
-//  * bf16: a weight's rounding to bf16 is its only one, and the row is divided by the
-//    sum of the rounded weights (one more product, with ones), which leaves a mean of
-//    values; the LSE takes the sum of the unrounded ones. (8-bit scores are not exact
-//    enough: the 8-bit product keeps about 13 bits of a small term beside a large one.)
+//  * Weights enter the product in more bits than a bf16 output shows (one bf16 value of 8
+//    bits each makes the output's error 1.4 times that of its own rounding). Few rows: two
+//    bf16 terms, 16 bits, whose second products the loads of pages hide. Many rows: one
+//    fp16 value, 11 bits, with the codes in fp16 too; see HalfWeights.
+//    (8-bit scores are not exact enough: the 8-bit product keeps about 13 bits of a small
+//    term beside a large one.)
 //  * fp32: q and the probabilities enter as three bf16 terms each.
 //
 // Few rows: a wave takes a page (64 keys) of one head at a time from memory to
@@ -39,6 +41,8 @@ namespace {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
@@ -64,6 +68,19 @@ __device__ __forceinline__ bf16x8 widen(unsigned lo, unsigned hi, float scale) {
 #endif
 }
 
+// the same as fp16, exactly for scales from 2^-15 to 1
+__device__ __forceinline__ f16x8 widen_f16(unsigned lo, unsigned hi, float scale) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, false);
+  const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, true);
+  const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, false);
+  const f16x2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, true);
+  return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+#else
+  return f16x8{};
+#endif
+}
+
 __device__ __forceinline__ f32x4 mfma(const bf16x8 &a, const bf16x8 &b, const f32x4 &c) {
 #if defined(__HIP_DEVICE_COMPILE__)
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -71,11 +88,12 @@ __device__ __forceinline__ f32x4 mfma(const bf16x8 &a, const bf16x8 &b, const f3
   return c;
 #endif
 }
-
-// row sums of weights in bf16, in each of a lane's four accumulators
-__device__ __forceinline__ f32x4 add_weights(const bf16x8 &w, const f32x4 &sum) {
-  const __bf16 one = (__bf16)1.0f;
-  return mfma(bf16x8{one, one, one, one, one, one, one, one}, w, sum);
+__device__ __forceinline__ f32x4 mfma(const f16x8 &a, const f16x8 &b, const f32x4 &c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+#else
+  return c;
+#endif
 }
 
 // x and the same register of the lanes that hold the same row (lane ^ 16, ^ 32)
@@ -92,7 +110,7 @@ __device__ __forceinline__ float row_sum(float x) {
 // the sum NaN, which goes on to o and the LSE (a test for > 0 would turn it into no key).
 __device__ __forceinline__ float over(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
 
-// TERMS bf16 values whose sum is x: one rounding for bf16, 24 bits for fp32
+// TERMS bf16 values whose sum is x, to 8 bits each
 template <int TERMS>
 __device__ __forceinline__ void split_terms(const float (&x)[8], bf16x8 (&out)[TERMS]) {
 #pragma unroll
@@ -214,7 +232,7 @@ struct Frags {
 template <int D>
 struct FewShared {
   float o[kWaves][kRows][D + 4];
-  float m[kWaves][kRows], l[kWaves][kRows], r[kWaves][kRows];
+  float m[kWaves][kRows], l[kWaves][kRows];
 };
 
 // Row block r.block of a request over the pages pg0 .. pg_end - 1 of its sequence, by
@@ -223,7 +241,7 @@ struct FewShared {
 template <bool BF16, int D>
 __device__ __forceinline__ void few_rows(const CacheAttnLaunch &p, FewShared<D> &sh, const Request &r, int h, int pg0,
                                          int pg_end, int slot) {
-  constexpr int T = BF16 ? 1 : 3, DS = D / 32, DB = D / 16;
+  constexpr int T = BF16 ? 1 : 3, TW = BF16 ? 2 : 3, DS = D / 32, DB = D / 16;  // terms of q and of a weight
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n16 = lane & 15, quad = lane >> 4;
   // the ids of this wave's pages (pg0 + wave + 4 i), 64 at a time in the lanes; they do
@@ -252,7 +270,7 @@ __device__ __forceinline__ void few_rows(const CacheAttnLaunch &p, FewShared<D> 
   lim_lo = __builtin_amdgcn_readfirstlane(lim_lo);
   const int pg1 = min(min(pg_end, (r.L + kPage - 1) / kPage), (lim_hi >> 6) + 1);
 
-  f32x4 o[DB] = {}, rounded = {};  // rounded: sum of the weights as they enter the product
+  f32x4 o[DB] = {};
   float m_run = -INFINITY, l_run = 0.f;
 
   auto page_id = [&](int i) {  // i-th page of this wave
@@ -318,7 +336,6 @@ __device__ __forceinline__ void few_rows(const CacheAttnLaunch &p, FewShared<D> 
     if (__ballot(m_new > m_run)) {
       const float alpha = m_new > m_run ? exp2_(m_run - m_new) : 1.f;
       l_run *= alpha;
-      rounded *= alpha;
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[db] *= alpha;
       m_run = m_new;
@@ -334,14 +351,13 @@ __device__ __forceinline__ void few_rows(const CacheAttnLaunch &p, FewShared<D> 
       }
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
-      bf16x8 pf[T];
-      split_terms<T>(e[ks], pf);
-      if constexpr (BF16) rounded = add_weights(pf[0], rounded);
+      bf16x8 pf[TW];
+      split_terms<TW>(e[ks], pf);
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
         const bf16x8 a = widen(f.v[db][2 * ks], f.v[db][2 * ks + 1], f.vs);
 #pragma unroll
-        for (int j = T - 1; j >= 0; --j) o[db] = mfma(a, pf[j], o[db]);
+        for (int j = TW - 1; j >= 0; --j) o[db] = mfma(a, pf[j], o[db]);
       }
     }
   };
@@ -361,7 +377,7 @@ __device__ __forceinline__ void few_rows(const CacheAttnLaunch &p, FewShared<D> 
 
   // join the waves
   l_run = row_sum(l_run);
-  if (quad == 0) sh.m[wave][n16] = m_run, sh.l[wave][n16] = l_run, sh.r[wave][n16] = BF16 ? rounded[0] : l_run;
+  if (quad == 0) sh.m[wave][n16] = m_run, sh.l[wave][n16] = l_run;
 #pragma unroll
   for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4 *>(&sh.o[wave][n16][db * 16 + quad * 4]) = o[db];
   __syncthreads();
@@ -369,16 +385,15 @@ __device__ __forceinline__ void few_rows(const CacheAttnLaunch &p, FewShared<D> 
   const int out = r.block * kRows + rr;
   if (out >= total) return;
   const int orow = r.row0 + out / p.group, ohead = h * p.group + out % p.group;
-  float m = sh.m[0][rr], w[kWaves], l = 0.f, sum = 0.f;
+  float m = sh.m[0][rr], w[kWaves], l = 0.f;
 #pragma unroll
   for (int k = 1; k < kWaves; ++k) m = fmaxf(m, sh.m[k][rr]);
 #pragma unroll
   for (int k = 0; k < kWaves; ++k) {
     w[k] = sh.m[k][rr] == -INFINITY ? 0.f : exp2_(sh.m[k][rr] - m);
     l += w[k] * sh.l[k][rr];
-    sum += w[k] * sh.r[k][rr];
   }
-  const float inv = over(sum);
+  const float inv = over(l);
   const float lse = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 #pragma unroll
   for (int c = c0 * 4; c < D; c += 64) {
@@ -589,13 +604,40 @@ __global__ __launch_bounds__(kThreads) void cache_line_join_kernel(const CacheAt
 // leaves the younger alone for the last quarter. 8 waves per workgroup, weights through
 // LDS, K converted once for all waves and pages further ahead did not take less.
 //
-// The reference m of a row is an integer (base-2 units), so that raising it scales O,
-// the sum and the weights in flight by a power of two, exactly. It is raised, to the
-// ceiling of the row's maximum, before a half whose scores would give a weight above
-// 2^8, so a weight is at most that.
+// The reference m of a row is an integer (base-2 units), so that raising it scales O and
+// the sum by a power of two, exactly. It is raised before a half whose scores pass it by
+// more than kLift + kSlack, to kLift below the ceiling of the row's maximum: a weight is
+// at most 2^(kLift + kSlack), a row's largest one at least 2^(kLift - 1).
 constexpr int kStages = 3;
 constexpr float kNoReference = -3e38f;  // before the first visible key
-constexpr float kSlack = 8.f;           // a weight is at most 2^kSlack
+
+// How weights enter the value product: as bf16 terms, with the values in bf16, at any
+// scales; a weight is off by 2^-8N of itself.
+template <int N>
+struct BfWeights {
+  static constexpr int TERMS = N;
+  static constexpr float kLift = 0.f, kSlack = 8.f;
+  using V = bf16x8;
+  static __device__ __forceinline__ V values(unsigned lo, unsigned hi, float scale) { return widen(lo, hi, scale); }
+  static __device__ __forceinline__ void weights(const float (&x)[8], V (&out)[N]) { split_terms<N>(x, out); }
+};
+// Or in fp16, with the codes in fp16 in units of the workgroup's largest scale of V: one
+// product where two bf16 terms are two (question of 128 rows over 32896 keys 76 us for 96).
+// A weight is off by 2^-11 of itself, or 2^-35 of the row's largest one: small ones are
+// held in steps of 2^-24. So that this does not show beside the values of any page, the
+// scales may be 2^4 apart; where they are further, the workgroup takes two bf16 terms.
+// (Slack of 4: raises cost nothing yet; 76.4 us, with 8 76.4, with 2 78.7, with 1 82.)
+struct HalfWeights {
+  static constexpr int TERMS = 1;
+  static constexpr float kLift = 11.f, kSlack = 4.f;
+  using V = f16x8;
+  static __device__ __forceinline__ V values(unsigned lo, unsigned hi, float scale) { return widen_f16(lo, hi, scale); }
+  static __device__ __forceinline__ void weights(const float (&x)[8], V (&out)[1]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) out[0][i] = (_Float16)x[i];
+  }
+};
+constexpr float kHalfSpread = 16.f;
 
 template <int N>
 __device__ __forceinline__ void wait_vm() {
@@ -629,13 +671,12 @@ struct Wide {
   static constexpr int T = BF16 ? 1 : 3, DS = D / 32, DB = D / 16;
   static constexpr int C = D / 64;                         // 16-byte pieces of a key that a lane reads
   static constexpr int UNITS = 4 * C;                      // steps of the scores of a half
-  static constexpr int MFMAS = ((UNITS + DB) * T + BF16) * MT;  // of a block
   static constexpr int PAGE_BYTES = 2 * kPage * D;
   using Scores = f32x4[MT][2];   // a lane's 8 keys of a half, per row
-  using Weights = bf16x8[MT][T];
+  template <typename P>
+  using Weights = typename P::V[MT][P::TERMS];
   bf16x8 q[T][MT][DS];
   f32x4 o[MT][DB];
-  f32x4 rounded[MT];             // sums of the weights as they enter the product (bf16)
   float m[MT], l[MT], top[MT];   // reference, sum, largest score that needs no raise
   int limit[MT];
   float scale_log2;
@@ -665,18 +706,13 @@ struct Wide {
       for (int j = T - 1; j >= 0; --j)
         s[mt][t] = mfma(a, q[j][mt][2 * c + e], c + e == 0 && j == T - 1 ? f32x4{} : s[mt][t]);
   }
-  template <int HALF>
-  __device__ __forceinline__ void value_unit(int db, const u32x4 (&v)[DB], float vs, const Weights &pf) {
-    const bf16x8 a = widen(v[db][2 * HALF], v[db][2 * HALF + 1], vs);
+  template <typename P, int HALF>
+  __device__ __forceinline__ void value_unit(int db, const u32x4 (&v)[DB], float vs, const Weights<P> &pf) {
+    const typename P::V a = P::values(v[db][2 * HALF], v[db][2 * HALF + 1], vs);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int j = T - 1; j >= 0; --j) o[mt][db] = mfma(a, pf[mt][j], o[mt][db]);
-  }
-  __device__ __forceinline__ void sum_weights(const Weights &pf) {
-    if constexpr (BF16)
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) rounded[mt] = add_weights(pf[mt][0], rounded[mt]);
+      for (int j = P::TERMS - 1; j >= 0; --j) o[mt][db] = mfma(a, pf[mt][j], o[mt][db]);
   }
   // keys (key, key + 1, ...: a lane's 8) past a row's limit get no weight, and the
   // values of those that no row of the wave sees, which may be NaN codes, become 0
@@ -696,8 +732,10 @@ struct Wide {
       for (int db = 0; db < DB; ++db) v[db][t] &= keep;
     }
   }
-  // raises the references that the scores s need raised; pf are the weights in flight
-  __device__ __forceinline__ void raise(const Scores &s, Weights &pf) {
+  // Raises the references that the scores s need raised; true if there are any. O follows
+  // after the block, with the weights in flight: rescale.
+  template <typename P>
+  __device__ __forceinline__ bool raise(const Scores &s, float (&alpha)[MT]) {
     bool need = false;
     float mx[MT];
 #pragma unroll
@@ -705,31 +743,30 @@ struct Wide {
       mx[mt] = max_score(s[mt][0], s[mt][1]);
       need |= mx[mt] > top[mt];
     }
-    if (__builtin_expect(__ballot(need) == 0, 1)) return;
+    if (__builtin_expect(__ballot(need) == 0, 1)) return false;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      const float to = fmaxf(m[mt], ceilf(row_max(mx[mt]) * scale_log2));
-      const float alpha = exp2_(m[mt] - to);  // a power of two; 0 for the first keys
+      const float to = fmaxf(m[mt], ceilf(row_max(mx[mt]) * scale_log2) - P::kLift);
+      alpha[mt] = exp2_(m[mt] - to);  // a power of two; 0 for the first keys
       m[mt] = to;
-      top[mt] = (to + kSlack) / scale_log2;
-      l[mt] *= alpha;
-      rounded[mt] *= alpha;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) o[mt][db] *= alpha;
-#pragma unroll
-      for (int j = 0; j < T; ++j)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) pf[mt][j][i] = (__bf16)((float)pf[mt][j][i] * alpha);
+      top[mt] = (to + P::kLift + P::kSlack) / scale_log2;
+      l[mt] *= alpha[mt];
     }
+    return true;
+  }
+  __device__ __forceinline__ void rescale(const float (&alpha)[MT]) {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[mt][db] *= alpha[mt];
   }
   // The block: weights of scores s into pf (l grows), scores of K k into s, value
   // product of the weights that pf held.
-  template <int HALF>  // of v's page
-  __device__ __forceinline__ void block(Scores &s, Weights &pf, const u32x4 (&k)[2][C], float ks, const u32x4 (&v)[DB],
+  template <typename P, int HALF>  // of v's page
+  __device__ __forceinline__ void block(Scores &s, Weights<P> &pf, const u32x4 (&k)[2][C], float ks, const u32x4 (&v)[DB],
                                         float vs) {
     Scores next;
     float e[MT][8];
-    sum_weights(pf);
 #pragma unroll
     for (int step = 0; step < 8; ++step) {
 #pragma unroll
@@ -738,17 +775,17 @@ struct Wide {
         l[mt] += e[mt][step];
       }
       if (step * UNITS % 8 == 0) score_unit(step * UNITS / 8, k, ks, next);
-      if (step * DB % 8 == 0) value_unit<HALF>(step * DB / 8, v, vs, pf);
+      if (step * DB % 8 == 0) value_unit<P, HALF>(step * DB / 8, v, vs, pf);
     }
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      split_terms<T>(e[mt], pf[mt]);
+      P::weights(e[mt], pf[mt]);
       s[mt][0] = next[mt][0];
       s[mt][1] = next[mt][1];
     }
     // a matrix instruction, then four others, and so on
 #pragma unroll
-    for (int i = 0; i < MFMAS; ++i) {
+    for (int i = 0; i < (UNITS * T + DB * P::TERMS) * MT; ++i) {  // its matrix instructions
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x402, 4, 0);
     }
@@ -806,7 +843,6 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
     w.m[mt] = kNoReference;
     w.top[mt] = kNoReference / p.scale_log2;
     w.l[mt] = 0.f;
-    w.rounded[mt] = f32x4{};
 #pragma unroll
     for (int db = 0; db < DB; ++db) w.o[mt][db] = f32x4{};
   }
@@ -831,7 +867,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
     firsts = f;
   }
   const size_t at = (size_t)(lane < n ? id : 0) * p.c.hkv + h;
-  const float kss = p.c.k_scale[at], vss = p.c.v_scale[at];
+  const float kss = p.c.k_scale[at];
+  float vss = p.c.v_scale[at];
   auto of_page = [](float x, int i) {
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), i));
   };
@@ -853,37 +890,44 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
   };
   auto stage = [&](int i) { return lds + i % kStages * PAGE_BYTES; };
 
-  typename W::Scores s;
-  typename W::Weights pf = {};
-  u32x4 v[DB] = {};
-  // Page i: its scores of half 0 are in s, the weights of the page before's half 1 in pf.
-  auto step = [&](int i, auto masked) {
-    constexpr bool MASK = decltype(masked)::value;
-    const int key = __builtin_amdgcn_readlane(firsts, i) + quad * 16;
-    const float ks = of_page(kss, i), vs = of_page(vss, i);
-    const float ks_next = of_page(kss, min(i + 1, n - 1)), vs_before = of_page(vss, max(i - 1, 0));
-    // page i + 1 is here for every wave, and all are done with page i - 1, whose place
-    // the copies of page i + 2 take
-    wait_vm<0>();
-    lds_barrier();
-    if (i + 2 < n) fetch(i + 2);
-    u32x4 k[2][C];
-    w.template read_k<1>(stage(i), k);
-    if constexpr (MASK) w.mask_scores(s, key);
-    w.raise(s, pf);
-    w.template block<1>(s, pf, k, ks, v, vs_before);  // v: of page i - 1 (zeros for the first)
-    w.template read_k<0>(stage(i + 1), k);
-    w.read_v(stage(i), v);
-    if constexpr (MASK) {
-      w.mask_scores(s, key + 8);
-      w.mask_values(v, key);
-    }
-    w.raise(s, pf);
-    w.template block<0>(s, pf, k, ks_next, v, vs);  // past the last page: scores that nobody uses
-  };
   if (n > 0) {
     fetch(0);
     if (n > 1) fetch(1);
+  }
+  // The pages' products, with weights as P has them.
+  auto run = [&](auto weights) {
+    using P = decltype(weights);
+    typename W::Scores s;
+    typename W::template Weights<P> pf = {};
+    u32x4 v[DB] = {};
+    // Page i: its scores of half 0 are in s, the weights of the page before's half 1 in pf.
+    auto step = [&](int i, auto masked) {
+      constexpr bool MASK = decltype(masked)::value;
+      const int key = __builtin_amdgcn_readlane(firsts, i) + quad * 16;
+      const float ks = of_page(kss, i), vs = of_page(vss, i);
+      const float ks_next = of_page(kss, min(i + 1, n - 1)), vs_before = of_page(vss, max(i - 1, 0));
+      // page i + 1 is here for every wave, and all are done with page i - 1, whose place
+      // the copies of page i + 2 take
+      wait_vm<0>();
+      lds_barrier();
+      if (i + 2 < n) fetch(i + 2);
+      u32x4 k[2][C];
+      w.template read_k<1>(stage(i), k);
+      if constexpr (MASK) w.mask_scores(s, key);
+      float alpha[MT];
+      bool raised = w.template raise<P>(s, alpha);
+      w.template block<P, 1>(s, pf, k, ks, v, vs_before);  // v: of page i - 1 (zeros for the first)
+      if (__builtin_expect(raised, 0)) w.rescale(alpha);
+      w.template read_k<0>(stage(i + 1), k);
+      w.read_v(stage(i), v);
+      if constexpr (MASK) {
+        w.mask_scores(s, key + 8);
+        w.mask_values(v, key);
+      }
+      raised = w.template raise<P>(s, alpha);
+      w.template block<P, 0>(s, pf, k, ks_next, v, vs);  // past the last page: scores that nobody uses
+      if (__builtin_expect(raised, 0)) w.rescale(alpha);
+    };
     wait_vm<0>();
     __syncthreads();
     u32x4 k[2][C];
@@ -895,16 +939,31 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
     int i = 0;
     for (; i < whole; ++i) step(i, std::false_type{});
     for (; i < n; ++i) step(i, std::true_type{});
-    w.sum_weights(pf);
 #pragma unroll
-    for (int db = 0; db < DB; ++db) w.template value_unit<1>(db, v, of_page(vss, n - 1), pf);
+    for (int db = 0; db < DB; ++db) w.template value_unit<P, 1>(db, v, of_page(vss, n - 1), pf);
+  };
+  float unit = 1.f;  // of O
+  if (n > 0) {
+    if constexpr (BF16) {
+      float most = lane < n ? vss : 0.f;
+#pragma unroll
+      for (int m = 32; m; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
+      if (__ballot(lane < n && !(vss == 0.f || vss * kHalfSpread >= most)) == 0) {
+        unit = most;
+        vss *= most > 0.f ? 1.f / most : 0.f;
+        run(HalfWeights{});
+      } else {
+        run(BfWeights<2>{});
+      }
+    } else {
+      run(BfWeights<3>{});
+    }
   }
 
   // results
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
-    const float l = row_sum(w.l[mt]), sum = BF16 ? w.rounded[mt][0] : l;
-    const float inv = over(sum);
+    const float l = row_sum(w.l[mt]), inv = over(l);
     const float lse = l == 0.f ? -INFINITY : (w.m[mt] + log2f(l)) * kLn2;
     const int tile = (r.block * kWaves + wave) * MT + mt, idx = tile * 16 + n16;
     if (p.n_splits > 1) {
@@ -912,12 +971,12 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
       if (quad == 0) p.part_lse[part * 16 + n16] = lse;
 #pragma unroll
       for (int db = 0; db < DB; ++db)
-        *reinterpret_cast<f32x4 *>(p.part_o + (part * DB + db) * 256 + lane * 4) = w.o[mt][db] * inv;
+        *reinterpret_cast<f32x4 *>(p.part_o + (part * DB + db) * 256 + lane * 4) = w.o[mt][db] * inv * unit;
     } else if (idx < total) {
       const int row = r.row0 + idx / p.group, head = h * p.group + idx % p.group;
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
-        const f32x4 x = w.o[mt][db] * inv;
+        const f32x4 x = w.o[mt][db] * inv * unit;
         const float y[4] = {x[0], x[1], x[2], x[3]};
         store_out<BF16>(p, row, head, db * 16 + quad * 4, y, D);
       }
