@@ -456,7 +456,8 @@ daf_status_t daf_cache_read(const daf_attn_cfg_t *cfg, const daf_cache_t *cache,
                             int32_t layer, const daf_cache_rows_t *rows, void *k,
                             void *v, hipStream_t stream);
 
-/* Bytes of workspace daf_cache_attn needs (0 on bad input or none needed). */
+/* Bytes of workspace daf_cache_attn needs (0 on bad input or none needed), at most
+ * 272 MB. */
 size_t daf_cache_attn_workspace_size(const daf_attn_cfg_t *cfg,
                                      const daf_cache_t *cache,
                                      const daf_cache_rows_t *rows, int32_t max_len);

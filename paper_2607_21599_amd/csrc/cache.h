@@ -64,7 +64,7 @@ struct CacheAttnLaunch {
   int32_t max_len;
   int32_t wide;                   // the kernel for many rows
   int32_t n_splits;               // wide: splits of a row block; else workgroups per head
-  int32_t split_pages;            // wide: pages per split, at most kMaxSplitPages
+  int32_t split_pages;            // wide: pages per split
   float scale_log2;               // softmax scale * log2(e)
   int32_t n_req;
   int32_t blocks;                 // row blocks of all requests
@@ -75,10 +75,9 @@ struct CacheAttnLaunch {
 static_assert(sizeof(CacheAttnLaunch) < 4096, "kernel arguments must fit 4 KiB");
 // (row, head) pairs of a row block: few rows, many rows in bf16 and in fp32
 constexpr int kCacheAttnRows = 16, kCacheWideRows = 128, kCacheWideRowsF32 = 64;
-// Many rows: pages of a split. At least 6 (fp32 questions over up to 7000 keys 15.8 us,
-// 17.1 with 3, 20.1 with 12; 18 rows of 7 heads over 8000 keys 18.6, 18.9, 25.4); at most
-// one per lane, which has its id.
-constexpr int kMinSplitPages = 6, kMaxSplitPages = 64;
+// Many rows: pages of a split, at least 6 (fp32 questions over up to 7000 keys 15.8 us,
+// 17.1 with 3, 20.1 with 12; 18 rows of 7 heads over 8000 keys 18.6, 18.9, 25.4).
+constexpr int kMinSplitPages = 6;
 constexpr size_t kLineBytes = (2 * kMaxCacheReqs + 64) * sizeof(int32_t);
 // Few rows: least pages per workgroup, one for each wave (one sequence of 8000 keys takes
 // 12.1 us with 4, 14.5 with 8, 17.3 with 16; from 16000 keys on every piece is longer).

@@ -229,7 +229,13 @@ AttnPlan plan_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_ca
   if (a.wide) {
     // Two workgroups per CU, at once (128 rows of 7 heads on each of 4 over 32896 keys, us
     // by workgroups in all: 256 87.8 + 5.5, 512 79.3 + 7.7, 768 83.6 + 9.7, 1024 86.7 + 11.8).
-    int64_t splits = std::max<int64_t>(std::max<int64_t>(1, 512 / jobs), (pages + kMaxSplitPages - 1) / kMaxSplitPages);
+    // More row blocks than that still gain from splits of 64 pages, which end more evenly,
+    // up to 4096 workgroups, whose partial results are at most 271 MB (4915 rows of 28 heads
+    // on 4 over 32768 keys, ms and MiB by the bound: 4096 2.20 and 203, 2048 2.49 and 0, none
+    // 2.19 and 542; 4096 rows over 131072 keys 7.0 and 226, 7.2 and 113, 7.5 and 1806; 32768
+    // rows over 32768 keys 10.9 and 0, 10.9 and 0, 14.1 and 3612).
+    int64_t splits = std::max<int64_t>(512 / jobs, std::min<int64_t>((pages + 63) / 64, 4096 / jobs));
+    splits = std::max<int64_t>(splits, 1);
     splits = std::min(splits, (pages + kMinSplitPages - 1) / kMinSplitPages);
     a.split_pages = (int)((pages + splits - 1) / splits);
     a.n_splits = (int)((pages + a.split_pages - 1) / a.split_pages);

@@ -793,7 +793,7 @@ struct Wide {
 };
 
 template <bool BF16, int D, int MT>
-__global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttnLaunch p) {
+__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void cache_wide_kernel(const CacheAttnLaunch p) {
   using W = Wide<BF16, D, MT>;
   constexpr int DB = W::DB, C = W::C;
   constexpr int PAGE_BYTES = W::PAGE_BYTES, IPW = PAGE_BYTES / 1024 / kWaves;  // copies per wave and page
@@ -809,8 +809,11 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
   const int h = g % p.c.hkv, split = g / p.c.hkv;
   const Request r = find_request(p, blk);
   const int pg0 = split * p.split_pages;
-  // the page ids do not wait for the length
-  int id = lane < p.split_pages && pg0 + lane < p.c.max_seq_pages ? r.pages[pg0 + lane] : -1;
+  // page ids, 64 at a time in the lanes; the first ones do not wait for the length
+  auto load_ids = [&](int i) {
+    return i + lane < p.split_pages && pg0 + i + lane < p.c.max_seq_pages ? r.pages[pg0 + i + lane] : -1;
+  };
+  int id = load_ids(0);
   const int pages = (r.L + kPage - 1) / kPage;
   if (split > 0 && pg0 >= pages) return;  // no keys here: the join leaves this split out
   const int total = r.n * p.group;
@@ -854,21 +857,25 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
   w.lim_hi = __builtin_amdgcn_readfirstlane(lim_hi);
   lim_lo = __builtin_amdgcn_readfirstlane(lim_lo);
 
-  // this split's pages that are there and that a row of the block sees, one per lane
-  // (split_pages <= 64), in order
-  const unsigned long long mask =
-      __ballot(lane < p.split_pages && pg0 + lane < seen && (unsigned)id < (unsigned)p.c.n_pages);
-  const int n = __builtin_popcountll(mask);
-  int firsts = (pg0 + lane) * kPage;  // first key of the page
-  if (mask & (mask + 1)) {            // pages are missing in between: close the gaps
-    const int to = (mask >> lane) & 1 ? __builtin_popcountll(mask & ((1ull << lane) - 1)) * 4 : 252;
-    const int a = __builtin_amdgcn_ds_permute(to, id), f = __builtin_amdgcn_ds_permute(to, firsts);
-    id = a;
-    firsts = f;
-  }
-  const size_t at = (size_t)(lane < n ? id : 0) * p.c.hkv + h;
-  const float kss = p.c.k_scale[at];
-  float vss = p.c.v_scale[at];
+  // Of 64 of this split's pages, from the i-th on, those that are there and that a row of
+  // the block sees, one per lane, in order: id becomes theirs.
+  const int span = min(p.split_pages, seen - pg0);  // pages of the split that a row sees
+  int n = 0, firsts = 0;                            // how many; first keys
+  float kss = 0.f, vss = 0.f;                       // scales
+  auto settle = [&](int i) {
+    const unsigned long long mask = __ballot(i + lane < span && (unsigned)id < (unsigned)p.c.n_pages);
+    n = __builtin_popcountll(mask);
+    firsts = (pg0 + i + lane) * kPage;
+    if (mask & (mask + 1)) {  // pages are missing in between: close the gaps
+      const int to = (mask >> lane) & 1 ? __builtin_popcountll(mask & ((1ull << lane) - 1)) * 4 : 252;
+      const int a = __builtin_amdgcn_ds_permute(to, id), f = __builtin_amdgcn_ds_permute(to, firsts);
+      id = a;
+      firsts = f;
+    }
+    const size_t at = (size_t)(lane < n ? id : 0) * p.c.hkv + h;
+    kss = p.c.k_scale[at];
+    vss = lane < n ? p.c.v_scale[at] : 0.f;
+  };
   auto of_page = [](float x, int i) {
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), i));
   };
@@ -890,12 +897,12 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
   };
   auto stage = [&](int i) { return lds + i % kStages * PAGE_BYTES; };
 
-  if (n > 0) {
-    fetch(0);
+  auto begin = [&] {
+    if (n > 0) fetch(0);
     if (n > 1) fetch(1);
-  }
-  // The pages' products, with weights as P has them.
-  auto run = [&](auto weights) {
+  };
+  // The products of the n pages, with weights as P has them.
+  auto pages_of_64 = [&](auto weights) {
     using P = decltype(weights);
     typename W::Scores s;
     typename W::template Weights<P> pf = {};
@@ -942,22 +949,45 @@ __global__ __launch_bounds__(kThreads, 2) void cache_wide_kernel(const CacheAttn
 #pragma unroll
     for (int db = 0; db < DB; ++db) w.template value_unit<P, 1>(db, v, of_page(vss, n - 1), pf);
   };
-  float unit = 1.f;  // of O
-  if (n > 0) {
-    if constexpr (BF16) {
-      float most = lane < n ? vss : 0.f;
-#pragma unroll
-      for (int m = 32; m; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
-      if (__ballot(lane < n && !(vss == 0.f || vss * kHalfSpread >= most)) == 0) {
-        unit = most;
-        vss *= most > 0.f ? 1.f / most : 0.f;
-        run(HalfWeights{});
-      } else {
-        run(BfWeights<2>{});
-      }
-    } else {
-      run(BfWeights<3>{});
+  float unit = 1.f, per_unit = 1.f;  // of O and V's scales
+  auto run = [&](auto weights) {
+    for (int i = 0;;) {
+      vss *= per_unit;
+      if (n > 0) pages_of_64(weights);
+      i += 64;
+      if (i >= span) break;
+      id = load_ids(i);
+      settle(i);
+      lds_barrier();  // every wave is done with the pages before
+      begin();
     }
+  };
+  settle(0);
+  begin();
+  if constexpr (BF16) {
+    // the largest scale of V of all pages, and whether one is further from it than fp16 takes
+    float most = vss, least = vss > 0.f ? vss : INFINITY;
+    bool odd = !(vss >= 0.f);
+    for (int i = 64; i < span; i += 64) {
+      const int next = load_ids(i);
+      if (i + lane < span && (unsigned)next < (unsigned)p.c.n_pages) {
+        const float vs = p.c.v_scale[(size_t)next * p.c.hkv + h];
+        most = fmaxf(most, vs);
+        least = vs > 0.f ? fminf(least, vs) : least;
+        odd |= !(vs >= 0.f);
+      }
+    }
+#pragma unroll
+    for (int m = 32; m; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
+    if (__ballot(odd || least * kHalfSpread < most) == 0) {
+      unit = most;
+      per_unit = most > 0.f ? 1.f / most : 0.f;
+      run(HalfWeights{});
+    } else {
+      run(BfWeights<2>{});
+    }
+  } else {
+    run(BfWeights<3>{});
   }
 
   // results
