@@ -140,15 +140,16 @@ class Cache(ctypes.Structure):
 
 class CacheRows(ctypes.Structure):
     """daf_cache_rows_t: rows of a ragged batch of requests on a cache. ``cu`` are
-    the host prefix sums of the rows per request; ``seq`` and ``pos`` (device, or
-    None) are kept alive."""
+    the host prefix sums of the rows per request; ``seq`` and ``pos`` (int32 on the
+    device, or None) are kept alive."""
     _fields_ = [("n", ctypes.c_int32), ("cu", ctypes.POINTER(ctypes.c_int32)), ("seq", _vp), ("pos", _vp)]
 
     def __init__(self, cu, seq=None, pos=None):
         self._cu = np.ascontiguousarray(cu, dtype=np.int32)
         self._keep = (seq, pos)
-        super().__init__(len(self._cu) - 1, self._cu.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)), _ptr(seq),
-                         _ptr(pos))
+        n = len(self._cu) - 1
+        super().__init__(n, self._cu.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)), _list(seq, "seq", n),
+                         _list(pos, "pos", int(self._cu[-1]) if n >= 0 else 0))
 
 
 _lib = None
@@ -222,6 +223,24 @@ def _ptr(x):
         return None
     if isinstance(x, int):
         return x or None
+    return x.data_ptr() or None
+
+
+_int32 = None
+
+
+def _list(x, name: str, n: int):
+    """Device address of a list of n int32 (a tensor, an int address, or None). A tensor of
+    another type, torch's default int64 for one, would be read as other numbers."""
+    global _int32
+    if x is None or isinstance(x, int):
+        return _ptr(x)
+    if _int32 is None:
+        import torch
+        _int32 = torch.int32
+    if x.dtype != _int32 or not x.is_cuda or not x.is_contiguous() or x.numel() < n:
+        raise ValueError(f"{name} must be contiguous int32 on the GPU, {n} elements, not {x.numel()} of {x.dtype} "
+                         f"on {x.device}")
     return x.data_ptr() or None
 
 
@@ -391,28 +410,30 @@ def daf_pages_workspace_size(cache: Cache) -> int:
 
 
 def daf_pages_extend(cache: Cache, n: int, seq, n_new, status, stream=None):
-    _check(lib().daf_pages_extend(cache, n, _ptr(seq), _ptr(n_new), _ptr(status), _stream(stream)))
+    _check(lib().daf_pages_extend(cache, n, _list(seq, "seq", n), _list(n_new, "n_new", n), _list(status, "status", 1),
+                                  _stream(stream)))
 
 
 def daf_pages_fork(cache: Cache, n: int, src, dst, status, workspace, ws_bytes: int, stream=None):
-    _check(lib().daf_pages_fork(cache, n, _ptr(src), _ptr(dst), _ptr(status), _ptr(workspace), ws_bytes,
-                                _stream(stream)))
+    _check(lib().daf_pages_fork(cache, n, _list(src, "src", n), _list(dst, "dst", n), _list(status, "status", 1),
+                                _ptr(workspace), ws_bytes, _stream(stream)))
 
 
 def daf_pages_unshare(cache: Cache, rows: CacheRows, status, workspace, ws_bytes: int, stream=None):
-    _check(lib().daf_pages_unshare(cache, rows, _ptr(status), _ptr(workspace), ws_bytes, _stream(stream)))
+    _check(lib().daf_pages_unshare(cache, rows, _list(status, "status", 1), _ptr(workspace), ws_bytes,
+                                   _stream(stream)))
 
 
 def daf_pages_free(cache: Cache, n: int, seq=None, stream=None):
-    _check(lib().daf_pages_free(cache, n, _ptr(seq), _stream(stream)))
+    _check(lib().daf_pages_free(cache, n, _list(seq, "seq", n), _stream(stream)))
 
 
 def daf_pages_copy(cache: Cache, n: int, src, dst, stream=None):
-    _check(lib().daf_pages_copy(cache, n, _ptr(src), _ptr(dst), _stream(stream)))
+    _check(lib().daf_pages_copy(cache, n, _list(src, "src", n), _list(dst, "dst", n), _stream(stream)))
 
 
 def daf_pages_compact(cache: Cache, n_live, workspace, ws_bytes: int, stream=None):
-    _check(lib().daf_pages_compact(cache, _ptr(n_live), _ptr(workspace), ws_bytes, _stream(stream)))
+    _check(lib().daf_pages_compact(cache, _list(n_live, "n_live", 1), _ptr(workspace), ws_bytes, _stream(stream)))
 
 
 def daf_status_string(status: int) -> str:
