@@ -924,9 +924,9 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void cache_wide_kernel(c
       float alpha[MT];
       bool raised = w.template raise<P>(s, alpha);
       w.template block<P, 1>(s, pf, k, ks, v, vs_before);  // v: of page i - 1 (zeros for the first)
-      if (__builtin_expect(raised, 0)) w.rescale(alpha);
       w.template read_k<0>(stage(i + 1), k);
       w.read_v(stage(i), v);
+      if (__builtin_expect(raised, 0)) w.rescale(alpha);
       if constexpr (MASK) {
         w.mask_scores(s, key + 8);
         w.mask_values(v, key);
