@@ -75,12 +75,13 @@ struct CacheAttnLaunch {
 static_assert(sizeof(CacheAttnLaunch) < 4096, "kernel arguments must fit 4 KiB");
 // (row, head) pairs of a row block: few rows, many rows in bf16 and in fp32
 constexpr int kCacheAttnRows = 16, kCacheWideRows = 128, kCacheWideRowsF32 = 64;
-// Many rows: pages of a split, at least 6 (fp32 questions over up to 7000 keys 15.8 us,
-// 17.1 with 3, 20.1 with 12; 18 rows of 7 heads over 8000 keys 18.6, 18.9, 25.4).
+// Many rows: pages of a split, at least 6 (us a call: fp32 questions over up to 7000 keys
+// 15.4, 16.5 with 3, 19.7 with 12; 18 rows of 7 heads over 8000 keys 20.0, 20.9, 25.9).
 constexpr int kMinSplitPages = 6;
 constexpr size_t kLineBytes = (2 * kMaxCacheReqs + 64) * sizeof(int32_t);
-// Few rows: least pages per workgroup, one for each wave (one sequence of 8000 keys takes
-// 12.1 us with 4, 14.5 with 8, 17.3 with 16; from 16000 keys on every piece is longer).
+// Few rows: least pages per workgroup, one for each wave (us a call: one sequence of 8000
+// keys 11.1 with 4, 13.4 with 8, 17.2 with 16; of 16000 keys 12.0, 13.7, 17.9; with four
+// K/V heads pieces grow longer by themselves past 16384 keys).
 constexpr int kMinPiece = 4;
 hipError_t launch_cache_attn(bool bf16, const CacheAttnLaunch &p, hipStream_t st);
 

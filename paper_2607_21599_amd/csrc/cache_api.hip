@@ -219,16 +219,17 @@ AttnPlan plan_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_ca
   int64_t most = 0, blocks = 0;
   for (int b = 0; b < rows->n; ++b) most = std::max<int64_t>(most, rows->cu[b + 1] - rows->cu[b]);
   // Up to four of few rows' blocks read a page from the caches as often before the wide
-  // kernel's larger tiles pay (7 heads on one, us, few rows and wide: 8000 keys, 9 rows
-  // 18.5 and 20.3, 18 rows 22.6 and 20.9; 131072 keys 65.5 and 67.7, 111 and 71.8).
+  // kernel's larger tiles pay (7 heads on one, us a call, few rows and wide: 8000 keys, 9
+  // rows 17.4 and 19.7, 18 rows 21.3 and 20.0; 131072 keys 58.0 and 56.9, 103 and 57.4).
   a.wide = most * (cfg->n_q_heads / cfg->n_kv_heads) > 4 * kCacheAttnRows;
   a.block_rows = !a.wide ? kCacheAttnRows : cfg->dtype == DAF_BF16 ? kCacheWideRows : kCacheWideRowsF32;
   for (int b = 0; b < rows->n; ++b) blocks += row_blocks(cfg, rows->cu[b + 1] - rows->cu[b], a.block_rows);
   const int64_t pages = std::max<int64_t>(1, ((int64_t)max_len + kPage - 1) / kPage);
   const int64_t jobs = std::max<int64_t>(1, blocks * c->n_kv_heads);
   if (a.wide) {
-    // Two workgroups per CU, at once (128 rows of 7 heads on each of 4 over 32896 keys, us
-    // by workgroups in all: 256 87.8 + 5.5, 512 79.3 + 7.7, 768 83.6 + 9.7, 1024 86.7 + 11.8).
+    // Two workgroups per CU, at once (128 rows of 7 heads on each of 4 over 32896 keys, us of
+    // kernel and join by workgroups in all: 256 86.7 + 5.3, 512 71.8 + 7.5, 768 75.1 + 9.5,
+    // 1024 76.4 + 12.0).
     // More row blocks than that still gain from splits of 64 pages, which end more evenly,
     // up to 4096 workgroups, whose partial results are at most 271 MB (4915 rows of 28 heads
     // on 4 over 32768 keys, ms and MiB by the bound: 4096 2.20 and 203, 2048 2.49 and 0, none
@@ -241,20 +242,21 @@ AttnPlan plan_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_ca
     a.n_splits = (int)((pages + a.split_pages - 1) / a.split_pages);
   } else {
     // One workgroup per row block and head, or workgroups per head on the line of all row
-    // blocks' pages. One takes up to 16 pages sooner than a join does (us, one and the
-    // line: a row of 1024 keys 11.3 and 15.3, of 1500 keys 13.5 and 12.4). With more of
-    // them the device fills without the line's ends inside of workgroups (ragged rows by 4
-    // heads over up to 2000 keys: 24 rows 16.0 and 18.5, 64 rows 18.7 and 28.4, 64 in fp32
-    // 22.6 and 36.9; 64 rows over up to 4000 keys 32.4 and 40.9): up to a third as many
-    // pages as workgroups, and 64, of which a long sequence among short ones takes 27 us.
+    // blocks' pages. One takes up to 16 pages as soon as the line and its join do (us, one
+    // and the line: a row of 1024 keys 11.0 and 7.8 + 3.6, of 1500 keys 13.9 and 7.9 + 3.5).
+    // With more of them the device fills without the line's ends inside of workgroups
+    // (ragged rows by 4 heads over up to 2000 keys: 24 rows 16.6 and 15.1 + 4.0, 64 rows
+    // 18.8 and 22.9 + 5.3, 64 in fp32 22.0 and 31.0 + 4.9; 64 rows over up to 4000 keys
+    // 33.9 and 35.1 + 5.4): up to a third as many pages as workgroups, and 64, of which a
+    // long sequence among 191 short ones takes 31.6 us (22.9 on the line).
     a.n_splits = 1;
     if (pages > std::clamp<int64_t>(jobs / 3, 16, 64)) {
       const int64_t line = std::min<int64_t>(blocks, INT32_MAX) * pages;
       // Two workgroups per CU hide the ends of requests behind each other's loads; within
-      // one request one is enough, with half as much to join (bf16 of 128 features, us with
-      // 512 and 256: 32 ragged sequences 30.9 and 34.8, two of 30000 keys 20.5 and 22.0;
-      // one of 131072 keys 38.0 and 36.0, four rows of it 48.5 and 42.3). fp32 of 128
-      // features has one.
+      // one request one is enough, with half as much to join (bf16 of 128 features, us a call
+      // with 512 and 256: 32 ragged sequences 30.7 and 33.0, two of 30000 keys 20.4 and 21.3;
+      // one of 131072 keys 32.6 and 31.9, four rows of it 44.0 and 36.2). fp32 of 128
+      // features has one (32 ragged sequences 40.3 and 36.2).
       const bool two = rows->n > 1 && (cfg->dtype == DAF_BF16 || cfg->head_dim == 64);
       const int64_t wgs = (two ? 512 : 256) / c->n_kv_heads;
       a.n_splits = (int)std::max<int64_t>(2, std::min<int64_t>(wgs, (line + kMinPiece - 1) / kMinPiece));

@@ -16,8 +16,10 @@
 //    wants them, and V^T, stored transposed, is read as 16 consecutive keys.
 //  * Weights enter the product in more bits than a bf16 output shows (one bf16 value of 8
 //    bits each makes the output's error 1.4 times that of its own rounding). Few rows: two
-//    bf16 terms, 16 bits, whose second products the loads of pages hide. Many rows: one
-//    fp16 value, 11 bits, with the codes in fp16 too; see HalfWeights.
+//    bf16 terms, 16 bits, whose second products the loads of pages hide for the most part
+//    (131072 keys 32.0 us for 30.8 with one term, 32 ragged sequences 27.1 for 25.0). Many
+//    rows: one fp16 value, 11 bits, with the codes in fp16 too; see HalfWeights. (That in
+//    the few rows' kernel, with the terms beside it, needs more registers than it has.)
 //    (8-bit scores are not exact enough: the 8-bit product keeps about 13 bits of a small
 //    term beside a large one.)
 //  * fp32: q and the probabilities enter as three bf16 terms each.
@@ -26,8 +28,8 @@
 // registers, in the layout that the matrix instructions take, 16 bytes per lane and
 // load, with the next page's loads in flight and without LDS; the waves of a workgroup
 // take its pages in turn and join their (m, sum, O) through LDS. Bound by the pages'
-// bytes: 131072 keys of 4 heads of 128 (134 MB) in 31 us, 4.3 TB/s; a short sequence
-// by what one CU keeps in flight (777 keys 10 us, 64 keys 4.7; 8 waves or 4).
+// bytes: 131072 keys of 4 heads of 128 (134 MB) in 32 us, 4.2 TB/s; a short sequence
+// by what one CU keeps in flight (777 keys 10.5 us, 64 keys 4.7; 8 waves or 4).
 // Many rows: below. What workgroups share of a row block is joined by a second kernel
 // (4 to 5 us, most of it its launch).
 #include <math.h>
@@ -598,8 +600,9 @@ __global__ __launch_bounds__(kThreads) void cache_line_join_kernel(const CacheAt
 // matrix and 9 vector instructions in turn take 35.5 ns, alone 27.5 and 19.9).
 //
 // Bound by that issue: 128 rows of 28 heads on 4 of 128 over 32896 keys, 60 GFLOP, take
-// 76 us (790 TFLOP/s), of which a SIMD's matrix instructions are 38% and its vector
-// instructions 43% (per 64 keys and 32 rows 34 and 150, 64 of them conversions of codes).
+// 70 us (860 TFLOP/s; the first calls after a pause 77). Of the 145,000 cycles that a CU is
+// busy its SIMDs' matrix instructions are 40% and their vector instructions 48% (per 32
+// keys and 32 rows 32 and 155, 64 of them conversions of codes).
 // The prologue is 4 us, and of the two workgroups of a CU the older is served first and
 // leaves the younger alone for the last quarter. 8 waves per workgroup, weights through
 // LDS, K converted once for all waves and pages further ahead did not take less.
@@ -622,11 +625,12 @@ struct BfWeights {
   static __device__ __forceinline__ void weights(const float (&x)[8], V (&out)[N]) { split_terms<N>(x, out); }
 };
 // Or in fp16, with the codes in fp16 in units of the workgroup's largest scale of V: one
-// product where two bf16 terms are two (question of 128 rows over 32896 keys 76 us for 96).
+// product where two bf16 terms are two (128 question rows over 32896 keys, us a call: 76
+// for 96).
 // A weight is off by 2^-11 of itself, or 2^-35 of the row's largest one: small ones are
 // held in steps of 2^-24. So that this does not show beside the values of any page, the
 // scales may be 2^4 apart; where they are further, the workgroup takes two bf16 terms.
-// (Slack of 4: raises cost nothing yet; 76.4 us, with 8 76.4, with 2 78.7, with 1 82.)
+// (Slack of 4: raises cost nothing yet; 76.4 us, with 8 76.4, with 2 78.7, with 1 82.2.)
 struct HalfWeights {
   static constexpr int TERMS = 1;
   static constexpr float kLift = 11.f, kSlack = 4.f;

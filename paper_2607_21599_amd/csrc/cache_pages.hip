@@ -6,7 +6,7 @@
 // looks through refs for that many before anything is changed, so that a call does
 // all or nothing without the host. A second launch moves the bytes with the whole
 // device. Counts change by integer additions, so no result depends on an order.
-// Planning is bound by latency (4 to 8 us, unshare of 4915 rows 10.6), copies by HBM (512
+// Planning is bound by latency (4 to 8 us, unshare of 4915 rows 10.4), copies by HBM (512
 // pages of 128 KiB 31 us, 4.3 TB/s). A plan's code runs once per call, so its fetch is
 // part of the latency: loops over sequences and pages take one per thread and
 // step and are not unrolled, and loads that depend on nothing come first.
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(kPlan) void pages_extend_kernel(const PoolView c, i
   // Scale 0, in every layer: what a page's last owner or a new pool left there would
   // count for the tokens that a write leaves out. (The pages' heads have 4 KiB of K
   // each, so their number fits 32 bits.) Few beside the bytes that are written there
-  // next: a plan of 512 pages of 4 heads in 2 layers takes 7.7 us, without them 7.1.
+  // next: a plan of 512 pages of 4 heads in 2 layers takes 7.9 us, without them 7.1.
   __syncthreads();  // ids past the list are read from the table
   const unsigned hkv = c.hkv, all = (unsigned)want * hkv;
   for (unsigned j = t; j < all; j += kPlan) {

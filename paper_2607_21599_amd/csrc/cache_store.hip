@@ -13,9 +13,9 @@
 // without a pass through LDS. All rows are loaded before the maximum is taken.
 // Bound by HBM for long runs of rows: 32768 rows of 4 heads of 128 (67 MB in bf16, 34 MB
 // of codes) are written in 28 us and read back in 17; by latency for scattered ones
-// (4915 rows over 512 pages, 55 MB, 23 us: chains of dependent loads, a page's at a
-// time, of which more rows per unit or fewer took as long) and for a few (32 rows 5.0 and
-// 3.6 us).
+// (4915 rows over 512 pages, 57 MB, 23 us: chains of dependent loads, a page's at a
+// time, of which more rows per unit or fewer took as long) and for a few (32 rows 4.9 and
+// 3.5 us).
 #include "cache.h"
 
 namespace daf {
