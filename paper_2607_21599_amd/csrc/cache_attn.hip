@@ -804,12 +804,21 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void cache_wide_kernel(c
   __shared__ __align__(16) unsigned char lds[kStages * PAGE_BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n16 = lane & 15, quad = lane >> 4;
-  // the row blocks of one (head, split) read the same pages: neighbours, on one XCD but
-  // for the few at the ends of its equal share
-  const int per_xcd = gridDim.x / kXcdCount;
-  const int wg = blockIdx.x % kXcdCount * per_xcd + blockIdx.x / kXcdCount;
-  if (wg >= p.c.hkv * p.n_splits * p.blocks) return;
-  const int g = wg / p.blocks, blk = wg % p.blocks;
+  // The row blocks of one (head, split) read the same pages: neighbours, on one XCD. These
+  // groups go to the XCDs in turn, first splits first, so that every XCD has work where
+  // sequences are far shorter than max_len (128 sequences of 8192 keys planned for 131072,
+  // 10 rows each: 567 us; with a run of groups for each XCD, of which the first has all the
+  // keys, 1910); the last few in equal shares.
+  const int groups = p.c.hkv * p.n_splits, turns = groups / kXcdCount;
+  const int xcd = blockIdx.x % kXcdCount, at_xcd = blockIdx.x / kXcdCount;
+  int g = at_xcd / p.blocks * kXcdCount + xcd, blk = at_xcd % p.blocks;
+  if (at_xcd >= turns * p.blocks) {
+    const int rest = groups % kXcdCount * p.blocks, share = (rest + kXcdCount - 1) / kXcdCount;
+    const int k = at_xcd - turns * p.blocks, i = xcd * share + k;
+    if (k >= share || i >= rest) return;
+    g = turns * kXcdCount + i / p.blocks;
+    blk = i % p.blocks;
+  }
   const int h = g % p.c.hkv, split = g / p.c.hkv;
   const Request r = find_request(p, blk);
   const int pg0 = split * p.split_pages;
@@ -1084,8 +1093,9 @@ hipError_t launch(const CacheAttnLaunch &p, hipStream_t st) {
   constexpr int MT = BF16 ? kCacheWideRows / 64 : kCacheWideRowsF32 / 64;
   const int jobs = p.blocks * p.c.hkv, pairs = p.cu[p.n_req] * p.hq;
   if (p.wide) {
-    const int wgs = (jobs * p.n_splits + kXcdCount - 1) / kXcdCount * kXcdCount;
-    cache_wide_kernel<BF16, D, MT><<<wgs, kThreads, 0, st>>>(p);
+    const int groups = p.c.hkv * p.n_splits, rest = groups % kXcdCount * p.blocks;
+    const int per_xcd = groups / kXcdCount * p.blocks + (rest + kXcdCount - 1) / kXcdCount;
+    cache_wide_kernel<BF16, D, MT><<<per_xcd * kXcdCount, kThreads, 0, st>>>(p);
   } else if (p.n_splits > 1) {
     cache_line_kernel<BF16, D><<<p.n_splits * p.c.hkv, kThreads, 0, st>>>(p);
   } else {

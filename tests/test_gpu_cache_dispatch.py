@@ -102,6 +102,21 @@ def test_softmax_scales(dtype, d, keys, rows, times):
     p.within_bounds(o, lse, 0, [0, rows], [0], q * times, None)
 
 
+@pytest.mark.parametrize("heads,rows,lens", [(1, [9, 70, 200], [1500, 40, 900]), (3, [65, 1, 0, 130], [700, 64, 0, 1300]),
+                                             (5, [300], [2000]), (8, [40, 40, 33], [64, 3000, 500]), (9, [17, 80], [400, 1])])
+def test_every_row_block_and_split(heads, rows, lens):
+    """Numbers of (head, split) pairs and row blocks that do not divide by each other, planned
+    for the lengths and for far longer ones."""
+    p = _pair(pages=sum(-(-n // 64) for n in lens) + 2, heads=heads, d=64, hq=heads * 8, n_seqs=len(lens),
+              max_seq_pages=400)
+    rng = np.random.default_rng(heads)
+    _fill(p, rng, list(range(len(lens))), lens)
+    q = torch.from_numpy(rng.standard_normal((sum(rows), heads * 8, 64))).float()
+    cu = [0] + np.cumsum(rows).tolist()
+    for max_len in (max(lens), 5000, 25600):
+        p.check_attn(0, cu, list(range(len(lens))), q, max_len=max_len)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_more_pages_than_a_waves_lanes_hold(dtype):
     """Few rows, many heads, a long sequence: 4 workgroups per head, of 65 pages a wave. Some
