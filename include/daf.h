@@ -457,7 +457,7 @@ daf_status_t daf_cache_read(const daf_attn_cfg_t *cfg, const daf_cache_t *cache,
                             void *v, hipStream_t stream);
 
 /* Bytes of workspace daf_cache_attn needs (0 on bad input or none needed), at most
- * 272 MB. */
+ * 544 MB. */
 size_t daf_cache_attn_workspace_size(const daf_attn_cfg_t *cfg,
                                      const daf_cache_t *cache,
                                      const daf_cache_rows_t *rows, int32_t max_len);

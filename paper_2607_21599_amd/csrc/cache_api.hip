@@ -216,14 +216,18 @@ size_t wide_pairs(const daf_attn_cfg_t *cfg, int64_t blocks, int block_rows) {
 // Kernel and its splits, from the sizes that the host knows.
 AttnPlan plan_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_cache_rows_t *rows, int32_t max_len) {
   AttnPlan a{};
-  int64_t most = 0, blocks = 0;
+  int64_t most = 0, blocks = 0, least = INT32_MAX;
   for (int b = 0; b < rows->n; ++b) most = std::max<int64_t>(most, rows->cu[b + 1] - rows->cu[b]);
   // Up to four of few rows' blocks read a page from the caches as often before the wide
   // kernel's larger tiles pay (7 heads on one, us a call, few rows and wide: 8000 keys, 9
   // rows 17.4 and 19.7, 18 rows 21.3 and 20.0; 131072 keys 58.0 and 56.9, 103 and 57.4).
   a.wide = most * (cfg->n_q_heads / cfg->n_kv_heads) > 4 * kCacheAttnRows;
   a.block_rows = !a.wide ? kCacheAttnRows : cfg->dtype == DAF_BF16 ? kCacheWideRows : kCacheWideRowsF32;
-  for (int b = 0; b < rows->n; ++b) blocks += row_blocks(cfg, rows->cu[b + 1] - rows->cu[b], a.block_rows);
+  for (int b = 0; b < rows->n; ++b) {
+    const int64_t n = row_blocks(cfg, rows->cu[b + 1] - rows->cu[b], a.block_rows);
+    blocks += n;
+    if (n > 0) least = std::min(least, n);  // row blocks of a request
+  }
   const int64_t pages = std::max<int64_t>(1, ((int64_t)max_len + kPage - 1) / kPage);
   const int64_t jobs = std::max<int64_t>(1, blocks * c->n_kv_heads);
   if (a.wide) {
@@ -232,10 +236,14 @@ AttnPlan plan_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_ca
     // 1024 76.4 + 12.0).
     // More row blocks than that still gain from splits of 64 pages, which end more evenly,
     // up to 4096 workgroups, whose partial results are at most 271 MB (4915 rows of 28 heads
-    // on 4 over 32768 keys, ms and MiB by the bound: 4096 2.20 and 203, 2048 2.49 and 0, none
-    // 2.19 and 542; 4096 rows over 131072 keys 7.0 and 226, 7.2 and 113, 7.5 and 1806; 32768
-    // rows over 32768 keys 10.9 and 0, 10.9 and 0, 14.1 and 3612).
-    int64_t splits = std::max<int64_t>(512 / jobs, std::min<int64_t>((pages + 63) / 64, 4096 / jobs));
+    // on 4 over 32768 keys, ms and MiB by the bound: 4096 2.18 and 203, 16384 2.25 and 542;
+    // 4096 rows over 131072 keys 7.3 and 226, 7.6 and 1016; 32768 rows over 32768 keys 10.8
+    // and 0, 10.6 and 903). A request of few row blocks may be the only long one, and has to
+    // fill the device by itself: up to 8192 (10 rows on each of 128 sequences, of which one
+    // has 131072 keys and the others 1000, us and MiB: 4096 531 and 258, 8192 384 and 516,
+    // 16384 320 and 1032).
+    const int64_t alone = std::min(8192 / jobs, 512 / (least * c->n_kv_heads));
+    int64_t splits = std::max(512 / jobs, std::min((pages + 63) / 64, std::max(4096 / jobs, alone)));
     splits = std::max<int64_t>(splits, 1);
     splits = std::min(splits, (pages + kMinSplitPages - 1) / kMinSplitPages);
     a.split_pages = (int)((pages + splits - 1) / splits);

@@ -7,8 +7,8 @@ import pytest
 import paper_2607_21599_amd as daf
 from test_cache_checks import FAKE
 
-# partial results of at most 4096 workgroups: 128 rows of D values and an LSE in fp32 each
-MOST = {d: 4096 * 128 * (d + 1) * 4 + 256 for d in (64, 128)}
+# partial results of at most 8192 workgroups: 128 rows of D values and an LSE in fp32 each
+MOST = {d: 8192 * 128 * (d + 1) * 4 + 256 for d in (64, 128)}
 
 
 def _size(rows, max_len, hq=28, hkv=4, d=128, dtype=daf.DAF_BF16):
@@ -23,6 +23,8 @@ def test_of_many_rows():
     assert 0 < _size([4915], 32768) <= 220 << 20
     assert 0 < _size([4096], 131072) <= 240 << 20
     assert 0 < _size([128], 32896) <= 32 << 20
+    # many sequences of few rows, any of which may be the only long one
+    assert 0 < _size([10] * 128, 131072) <= 520 << 20
 
 
 @pytest.mark.parametrize("dtype", [daf.DAF_BF16, daf.DAF_F32])
