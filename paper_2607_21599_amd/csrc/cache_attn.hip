@@ -807,8 +807,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void cache_wide_kernel(c
   // The row blocks of one (head, split) read the same pages: neighbours, on one XCD. These
   // groups go to the XCDs in turn, first splits first, so that every XCD has work where
   // sequences are far shorter than max_len (128 sequences of 8192 keys planned for 131072,
-  // 10 rows each: 567 us; with a run of groups for each XCD, of which the first has all the
-  // keys, 1910); the last few in equal shares.
+  // 10 rows each: 570 us; with a run of groups for each XCD, of which the first has all the
+  // keys, 1910; planned for 8192 keys 358); the last few in equal shares.
   const int groups = p.c.hkv * p.n_splits, turns = groups / kXcdCount;
   const int xcd = blockIdx.x % kXcdCount, at_xcd = blockIdx.x / kXcdCount;
   int g = at_xcd / p.blocks * kXcdCount + xcd, blk = at_xcd % p.blocks;
