@@ -308,11 +308,50 @@ daf_status_t daf_linear(int64_t M, int32_t N, int32_t K, const void *A,
 daf_status_t daf_linear_swiglu(int64_t M, int32_t I, int32_t K, const void *A,
                                const void *Wgu, void *C, hipStream_t stream);
 
+/* A projection of few rows with weights in 4 bits, as a decode step's: C = A W^T (+ bias)
+ * (+ residual), C, bias [N] and residual [M][N] in bf16.
+ *   W [N][K / 2] bytes: e2m1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6, bit 3 the sign), value k of
+ *   a row in the low (k even) or high half of byte k / 2; w_scales [N][K / 32]: a byte b per
+ *   32 of a row, for a value code * 2^(b - 127).
+ *   a_scales NULL: A [M][K] in bf16. Else A [M][K] are e4m3 codes and a_scales [M][K / 32]
+ *   their scales, as daf_add_rmsnorm writes them.
+ *   A scale's byte counts as 27 where it is less and 247 where it is more (2^-100 .. 2^120),
+ *   255 is NaN; NaN codes of A are NaN. Products are exact, sums fp32; bias and residual are
+ *   added in fp32 before the single rounding to bf16. residual may be C itself.
+ * Any N; K a positive multiple of 32 (DAF_ERR_UNSUPPORTED otherwise); any M, made for up to
+ * 64: more rows read the weights again for each 64. Scales need no alignment, all else 16
+ * bytes. M = 0 is a no-op. workspace: at least daf_linear_mx_workspace_size bytes (0: none
+ * needed, or bad input), contents undefined after the call; calls that may run at the same
+ * time, captured ones included, need one each. */
+size_t daf_linear_mx_workspace_size(int64_t M, int32_t N, int32_t K);
+daf_status_t daf_linear_mx(int64_t M, int32_t N, int32_t K, const void *A,
+                           const uint8_t *a_scales, const void *W,
+                           const uint8_t *w_scales, const void *bias,
+                           const void *residual, void *C, void *workspace,
+                           size_t ws_bytes, hipStream_t stream);
+
 /* RMS normalisation before the projections: y = x / sqrt(mean(x^2) + eps) * w
  * per row (x, y [rows][width], w [width], bf16; fp32 arithmetic). width must
  * be a positive multiple of 8; y may be x. */
 daf_status_t daf_rmsnorm(int64_t rows, int32_t width, const void *x,
                          const void *w, float eps, void *y, hipStream_t stream);
+
+/* The residual's addition and the RMS normalisation of the sum, for the projection that
+ * follows: s = x + delta, rounded to dtype; y = s / sqrt(mean(s^2) + eps) * w per row.
+ *   x, delta, sum, y [rows][width], w [width], all of `dtype` (daf_dtype_t).
+ *   delta: nullable (s = x). sum (with delta): where s goes, may be x or delta; nullable.
+ *   y: nullable, may be x or delta, but not sum.
+ *   codes, scales: both or neither, DEVICE: y in 8 bits, as daf_linear_mx takes it: e4m3
+ *   codes [rows][width] and per 32 values one byte b [rows][width / 32] (no alignment),
+ *   for a value code * 2^(b - 127): the smallest power of two >= 2^-100 under which the 32
+ *   magnitudes are at most 448. Codes are rounded once, to nearest even, from the fp32
+ *   values. Infinities count as the largest finite value, NaN stays NaN and does not
+ *   count for the scale.
+ * At least one of y and codes. fp32 arithmetic. width must be a positive multiple of 8,
+ * with codes of 32; other pointers 16-byte aligned; rows = 0 is a no-op. */
+daf_status_t daf_add_rmsnorm(int32_t dtype, int64_t rows, int32_t width, const void *x,
+                             const void *delta, const void *w, float eps, void *sum,
+                             void *y, void *codes, uint8_t *scales, hipStream_t stream);
 
 /* Rotary position embedding, in place, of n_heads heads of head_dim features
  * at the start of each of `rows` rows (row pitch row_stride elements, bf16):

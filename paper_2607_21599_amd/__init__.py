@@ -19,7 +19,7 @@ __all__ = [
     "daf_gather_important", "daf_imp_self_attn", "daf_position_attn", "daf_qdoc_workspace_size", "daf_qdoc_attn",
     "daf_fuse", "daf_layer_workspace_size", "daf_layer_attn", "daf_layer_noalloc_max_bytes",
     "daf_layer_attn_noalloc", "daf_check_indices", "daf_select_important",
-    "daf_linear", "daf_linear_swiglu", "daf_rmsnorm", "daf_rope", "daf_silu_mul", "daf_decoder_layer_workspace_size",
+    "daf_linear", "daf_linear_swiglu", "daf_linear_mx_workspace_size", "daf_linear_mx", "daf_rmsnorm", "daf_add_rmsnorm", "daf_rope", "daf_silu_mul", "daf_decoder_layer_workspace_size",
     "daf_decoder_layer", "LayerWeights", "DAF_LAYER_DAF", "DAF_LAYER_FULL",
     "DAF_PAGE_TOKENS", "Cache", "CacheRows",
     "daf_cache_write", "daf_cache_read", "daf_cache_attn_workspace_size", "daf_cache_attn",
@@ -41,7 +41,7 @@ EXPORTED = [
     "daf_gather_important", "daf_imp_self_attn", "daf_position_attn", "daf_qdoc_workspace_size", "daf_qdoc_attn",
     "daf_fuse", "daf_layer_workspace_size", "daf_layer_attn", "daf_layer_noalloc_max_bytes",
     "daf_layer_attn_noalloc", "daf_check_indices", "daf_select_important",
-    "daf_linear", "daf_linear_swiglu", "daf_rmsnorm", "daf_rope", "daf_silu_mul", "daf_decoder_layer_workspace_size",
+    "daf_linear", "daf_linear_swiglu", "daf_linear_mx_workspace_size", "daf_linear_mx", "daf_rmsnorm", "daf_add_rmsnorm", "daf_rope", "daf_silu_mul", "daf_decoder_layer_workspace_size",
     "daf_decoder_layer",
     "daf_cache_write", "daf_cache_read", "daf_cache_attn_workspace_size", "daf_cache_attn",
     "daf_pages_workspace_size", "daf_pages_extend", "daf_pages_fork", "daf_pages_unshare", "daf_pages_free",
@@ -182,7 +182,10 @@ def lib() -> ctypes.CDLL:
             "daf_check_indices": (i32, [bp, _vp, _vp, _vp]),
             "daf_linear": (i32, [i64, i32, i32, _vp, _vp, _vp, _vp, _vp, _vp]),
             "daf_linear_swiglu": (i32, [i64, i32, i32, _vp, _vp, _vp, _vp]),
+            "daf_linear_mx_workspace_size": (sz, [i64, i32, i32]),
+            "daf_linear_mx": (i32, [i64, i32, i32] + [_vp] * 8 + [sz, _vp]),
             "daf_rmsnorm": (i32, [i64, i32, _vp, _vp, ctypes.c_float, _vp, _vp]),
+            "daf_add_rmsnorm": (i32, [i32, i64, i32, _vp, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp, _vp]),
             "daf_rope": (i32, [i64, i32, i32, i64, _vp, _vp, ctypes.c_float, _vp]),
             "daf_silu_mul": (i32, [i64, i32, _vp, _vp, _vp]),
             "daf_decoder_layer_workspace_size": (sz, [cfgp, ctypes.POINTER(LayerWeights), bp, i32]),
@@ -306,8 +309,24 @@ def daf_linear_swiglu(M: int, I: int, K: int, A, Wgu, C, stream=None):
     _check(lib().daf_linear_swiglu(M, I, K, _ptr(A), _ptr(Wgu), _ptr(C), _stream(stream)))
 
 
+def daf_linear_mx_workspace_size(M: int, N: int, K: int) -> int:
+    return int(lib().daf_linear_mx_workspace_size(M, N, K))
+
+
+def daf_linear_mx(M: int, N: int, K: int, A, a_scales, W, w_scales, bias, residual, C, workspace, ws_bytes: int,
+                  stream=None):
+    _check(lib().daf_linear_mx(M, N, K, _ptr(A), _ptr(a_scales), _ptr(W), _ptr(w_scales), _ptr(bias), _ptr(residual),
+                               _ptr(C), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
 def daf_rmsnorm(rows: int, width: int, x, w, eps: float, y, stream=None):
     _check(lib().daf_rmsnorm(rows, width, _ptr(x), _ptr(w), eps, _ptr(y), _stream(stream)))
+
+
+def daf_add_rmsnorm(dtype: int, rows: int, width: int, x, delta, w, eps: float, sum=None, y=None, codes=None,
+                    scales=None, stream=None):
+    _check(lib().daf_add_rmsnorm(dtype, rows, width, _ptr(x), _ptr(delta), _ptr(w), eps, _ptr(sum), _ptr(y),
+                                 _ptr(codes), _ptr(scales), _stream(stream)))
 
 
 def daf_rope(rows: int, n_heads: int, head_dim: int, row_stride: int, x, pos, theta: float, stream=None):

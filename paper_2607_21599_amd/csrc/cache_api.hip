@@ -1,50 +1,15 @@
 // Entry points of the paged 8-bit K/V cache: argument checks and launch planning.
 // Every check that the host can make runs before anything is enqueued.
 #include <math.h>
-#include <stdarg.h>
-#include <stdio.h>
 
 #include <algorithm>
 
+#include "api_checks.h"
 #include "cache.h"
 
 namespace {
 
 using namespace daf;
-
-daf_status_t fail(daf_status_t st, const char *fmt, ...) {
-  char text[512];
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(text, sizeof(text), fmt, ap);
-  va_end(ap);
-  return set_error(st, text);
-}
-
-daf_status_t ok() { return set_error(DAF_OK, ""); }
-
-daf_status_t launched(hipError_t e, const char *what) {
-  return e == hipSuccess ? ok() : fail(DAF_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-}
-
-daf_status_t aligned(const void *p, const char *name) {
-  if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return fail(DAF_ERR_ALIGNMENT, "%s is not 16-byte aligned", name);
-  return DAF_OK;
-}
-
-daf_status_t need_ptr(const void *p, const char *name) {
-  if (!p) return fail(DAF_ERR_INVALID_ARG, "%s is NULL", name);
-  return aligned(p, name);
-}
-
-// a launch has less than 2^32 threads
-bool fits(int64_t workgroups, int threads) { return workgroups <= (int64_t)UINT32_MAX / threads; }
-
-#define CHECK(expr)                \
-  do {                             \
-    daf_status_t st_ = (expr);     \
-    if (st_ != DAF_OK) return st_; \
-  } while (0)
 
 daf_status_t check_cache(const daf_cache_t *c) {
   if (!c) return fail(DAF_ERR_INVALID_ARG, "cache is NULL");

@@ -17,11 +17,11 @@
 // time, of which more rows per unit or fewer took as long) and for a few (32 rows 4.9 and
 // 3.5 us).
 #include "cache.h"
+#include "e4m3.h"
 
 namespace daf {
 namespace {
 
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
@@ -92,38 +92,10 @@ struct Elem {
   }
 };
 
-// four values to codes / four codes to values (nearest even; NaN stays NaN)
-__device__ __forceinline__ unsigned to_codes(float a, float b, float c, float d) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-  return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
-#else
-  return 0;
-#endif
-}
-__device__ __forceinline__ void from_codes(unsigned w, float *x) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-  x[0] = a[0], x[1] = a[1], x[2] = b[0], x[3] = b[1];
-#endif
-}
 __device__ __forceinline__ unsigned rescale(unsigned w, float ratio) {
   float x[4];
   from_codes(w, x);
   return to_codes(x[0] * ratio, x[1] * ratio, x[2] * ratio, x[3] * ratio);
-}
-
-// The smallest power of two >= 2^kMinScaleExp under which top is at most 448 =
-// 1.75 * 2^8; 0 for 0. From the bits of top, so exact.
-__device__ __forceinline__ float scale_for(float top) {
-  if (top == 0.f) return 0.f;
-  const unsigned u = __builtin_bit_cast(unsigned, top);
-  const int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
-  return __builtin_bit_cast(float, (unsigned)(max(e, kMinScaleExp) + 127) << 23);
-}
-// 1 / s of a power of two in [2^-100, 2^120], 0 for 0
-__device__ __forceinline__ float inverse(float s) {
-  return s == 0.f ? 0.f : __builtin_bit_cast(float, (254u << 23) - __builtin_bit_cast(unsigned, s));
 }
 
 __device__ __forceinline__ unsigned wave_max(unsigned x) {
