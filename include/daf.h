@@ -495,6 +495,25 @@ daf_status_t daf_cache_read(const daf_attn_cfg_t *cfg, const daf_cache_t *cache,
                             int32_t layer, const daf_cache_rows_t *rows, void *k,
                             void *v, hipStream_t stream);
 
+/* daf_cache_write of rows that still lack their positions: K takes the rotary position
+ * embedding of daf_rope on its way into the cache, and q beside it, all from the rows of
+ * the projections.
+ *   q (nullable, with q_out) row stride q_stride, k and v row stride kv_stride elements
+ *   from row to row, of cfg's dtype: row i of q starts with [Hq][D], of k and v with
+ *   [Hkv][D]. The strides are multiples of 16 bytes (the parts of one joint row
+ *   [Hq + 2 Hkv][D], or arrays of their own). q_out [cu[n]][Hq][D] contiguous, as
+ *   daf_cache_attn takes it; may be q where q_stride is Hq * D.
+ * Features (i, i + D/2) of a head turn by position * theta^(-2i/D), the angle in fp64, in
+ * fp32 arithmetic; K is rounded once, to its code, V as daf_cache_write has it. Positions,
+ * scales and everything else as in daf_cache_write, with infinities and NaN of k as the
+ * rotation leaves them. q is turned at every row's position, also where that is not in
+ * [0, len) and K and V are left out. */
+daf_status_t daf_cache_write_rope(const daf_attn_cfg_t *cfg, const daf_cache_t *cache,
+                                  int32_t layer, const daf_cache_rows_t *rows,
+                                  float theta, const void *q, int64_t q_stride,
+                                  const void *k, const void *v, int64_t kv_stride,
+                                  void *q_out, hipStream_t stream);
+
 /* Bytes of workspace daf_cache_attn needs (0 on bad input or none needed), at most
  * 544 MB. */
 size_t daf_cache_attn_workspace_size(const daf_attn_cfg_t *cfg,

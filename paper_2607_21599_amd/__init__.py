@@ -22,7 +22,7 @@ __all__ = [
     "daf_linear", "daf_linear_swiglu", "daf_linear_mx_workspace_size", "daf_linear_mx", "daf_rmsnorm", "daf_add_rmsnorm", "daf_rope", "daf_silu_mul", "daf_decoder_layer_workspace_size",
     "daf_decoder_layer", "LayerWeights", "DAF_LAYER_DAF", "DAF_LAYER_FULL",
     "DAF_PAGE_TOKENS", "Cache", "CacheRows",
-    "daf_cache_write", "daf_cache_read", "daf_cache_attn_workspace_size", "daf_cache_attn",
+    "daf_cache_write", "daf_cache_write_rope", "daf_cache_read", "daf_cache_attn_workspace_size", "daf_cache_attn",
     "daf_pages_workspace_size", "daf_pages_extend", "daf_pages_fork", "daf_pages_unshare", "daf_pages_free",
     "daf_pages_copy", "daf_pages_compact",
     "daf_status_string", "daf_last_error", "daf_version", "EXPORTED",
@@ -43,7 +43,7 @@ EXPORTED = [
     "daf_layer_attn_noalloc", "daf_check_indices", "daf_select_important",
     "daf_linear", "daf_linear_swiglu", "daf_linear_mx_workspace_size", "daf_linear_mx", "daf_rmsnorm", "daf_add_rmsnorm", "daf_rope", "daf_silu_mul", "daf_decoder_layer_workspace_size",
     "daf_decoder_layer",
-    "daf_cache_write", "daf_cache_read", "daf_cache_attn_workspace_size", "daf_cache_attn",
+    "daf_cache_write", "daf_cache_write_rope", "daf_cache_read", "daf_cache_attn_workspace_size", "daf_cache_attn",
     "daf_pages_workspace_size", "daf_pages_extend", "daf_pages_fork", "daf_pages_unshare", "daf_pages_free",
     "daf_pages_copy", "daf_pages_compact",
     "daf_status_string", "daf_last_error", "daf_version",
@@ -192,6 +192,7 @@ def lib() -> ctypes.CDLL:
             "daf_decoder_layer": (i32, [cfgp, ctypes.POINTER(LayerWeights), bp, i32, _vp, _vp, _vp, _vp, _vp,
                                         _vp, sz, _vp]),
             "daf_cache_write": (i32, [cfgp, cp, i32, rp, _vp, _vp, _vp]),
+            "daf_cache_write_rope": (i32, [cfgp, cp, i32, rp, ctypes.c_float, _vp, i64, _vp, _vp, i64, _vp, _vp]),
             "daf_cache_read": (i32, [cfgp, cp, i32, rp, _vp, _vp, _vp]),
             "daf_cache_attn_workspace_size": (sz, [cfgp, cp, rp, i32]),
             "daf_cache_attn": (i32, [cfgp, cp, i32, rp, i32, _vp, _vp, _vp, _vp, sz, _vp]),
@@ -408,6 +409,13 @@ def daf_check_indices(batch: Batch, idx, d_bad_count, stream=None):
 # ---- the paged 8-bit K/V cache ------------------------------------------------
 def daf_cache_write(cfg: AttnCfg, cache: Cache, layer: int, rows: CacheRows, k, v, stream=None):
     _check(lib().daf_cache_write(_cfgp(cfg), cache, layer, rows, _ptr(k), _ptr(v), _stream(stream)))
+
+
+def daf_cache_write_rope(cfg: AttnCfg, cache: Cache, layer: int, rows: CacheRows, theta: float, q, q_stride: int, k, v,
+                         kv_stride: int, q_out, stream=None):
+    """q, k and v may be views of one joint projection's rows; strides in elements."""
+    _check(lib().daf_cache_write_rope(_cfgp(cfg), cache, layer, rows, theta, _ptr(q), q_stride, _ptr(k), _ptr(v),
+                                      kv_stride, _ptr(q_out), _stream(stream)))
 
 
 def daf_cache_read(cfg: AttnCfg, cache: Cache, layer: int, rows: CacheRows, k, v, stream=None):

@@ -40,6 +40,18 @@ struct StoreLaunch {
   int32_t unit0[kMaxCacheReqs + 1];  // first unit of each request
 };
 static_assert(sizeof(StoreLaunch) < 4096, "kernel arguments must fit 4 KiB");
+// With the rotary embedding of q and k.
+struct RopeLaunch {
+  const void *q;    // nullable; at the launch's first row
+  void *q_out;
+  int64_t q_pitch, kv_pitch;  // bytes from row to row of q, and of k and v
+  int32_t hq;
+  double turn[64];  // of pair i of a head's features, per position: theta^(-2i/D) / (2 pi)
+};
+static_assert(sizeof(StoreLaunch) + sizeof(RopeLaunch) < 4096, "kernel arguments must fit 4 KiB");
+// workgroups of q's rows
+inline int64_t rope_jobs(int64_t rows, int d) { return (rows * (d / 2) + kStoreThreads - 1) / kStoreThreads; }
+hipError_t launch_cache_rope_store(bool bf16, const StoreLaunch &p, const RopeLaunch &rope, hipStream_t st);
 constexpr int kStoreRows = 8;  // rows at positions: rows per unit
 hipError_t launch_cache_store(bool write, bool bf16, const StoreLaunch &p, hipStream_t st);
 

@@ -125,7 +125,8 @@ int fill(const daf_cache_rows_t *r, int b0, int n, int32_t *cu, int32_t *first, 
 }
 
 daf_status_t store(bool write, const daf_attn_cfg_t *cfg, const daf_cache_t *c, int32_t layer,
-                   const daf_cache_rows_t *rows, const void *k, const void *v, hipStream_t stream) {
+                   const daf_cache_rows_t *rows, const void *k, const void *v, hipStream_t stream,
+                   const RopeLaunch *rope = nullptr) {
   CHECK(check_cache(c));
   CHECK(check_cfg(cfg, c));
   CHECK(check_layer(c, layer));
@@ -135,7 +136,7 @@ daf_status_t store(bool write, const daf_attn_cfg_t *cfg, const daf_cache_t *c, 
   if (write || k) CHECK(need_ptr(k, "k"));
   if (write || v) CHECK(need_ptr(v, "v"));
   const bool bf16 = cfg->dtype == DAF_BF16;
-  const size_t row_bytes = (size_t)c->n_kv_heads * c->head_dim * (bf16 ? 2 : 4);
+  const size_t row_bytes = rope ? rope->kv_pitch : (size_t)c->n_kv_heads * c->head_dim * (bf16 ? 2 : 4);
   auto units_of = [&](int64_t n) { return n == 0 ? 0 : rows->pos ? (n + kStoreRows - 1) / kStoreRows : (n + 62) / 64 + 1; };
   // every launch's grid is checked before the first launch
   for (int pass = 0; pass < 2; ++pass)
@@ -144,7 +145,8 @@ daf_status_t store(bool write, const daf_attn_cfg_t *cfg, const daf_cache_t *c, 
       p.c = view(c, layer);
       p.n_req = std::min(kMaxCacheReqs, rows->n - b0);
       p.units = fill(rows, b0, p.n_req, p.cu, p.unit0, &p.per_req, units_of);
-      if (p.units < 0 || !fits((int64_t)p.units * c->n_kv_heads * 2, kStoreThreads))
+      const int64_t q_jobs = rope && rope->q ? rope_jobs(p.cu[p.n_req], c->head_dim) : 0;
+      if (p.units < 0 || !fits((int64_t)p.units * c->n_kv_heads * 2 + q_jobs, kStoreThreads))
         return fail(DAF_ERR_UNSUPPORTED, "%d rows of %d heads are too many for one call", total, c->n_kv_heads);
       if (pass == 0 || p.units == 0) continue;
       const int64_t row0 = rows->cu[b0];
@@ -157,6 +159,14 @@ daf_status_t store(bool write, const daf_attn_cfg_t *cfg, const daf_cache_t *c, 
       p.pos = rows->pos ? rows->pos + row0 : nullptr;
       p.k = rows_at(k, row0, row_bytes);
       p.v = rows_at(v, row0, row_bytes);
+      if (rope) {
+        RopeLaunch r = *rope;
+        r.q = rows_at(rope->q, row0, rope->q_pitch);
+        r.q_out = const_cast<char *>(rows_at(rope->q_out, row0, (size_t)cfg->n_q_heads * c->head_dim * (bf16 ? 2 : 4)));
+        const hipError_t e = launch_cache_rope_store(bf16, p, r, stream);
+        if (e != hipSuccess) return launched(e, "cache write launch");
+        continue;
+      }
       const hipError_t e = launch_cache_store(write, bf16, p, stream);
       if (e != hipSuccess) return launched(e, write ? "cache write launch" : "cache read launch");
     }
@@ -362,6 +372,42 @@ daf_status_t daf_cache_write(const daf_attn_cfg_t *cfg, const daf_cache_t *cache
 daf_status_t daf_cache_read(const daf_attn_cfg_t *cfg, const daf_cache_t *cache, int32_t layer,
                             const daf_cache_rows_t *rows, void *k, void *v, hipStream_t stream) {
   return store(false, cfg, cache, layer, rows, k, v, stream);
+}
+
+daf_status_t daf_cache_write_rope(const daf_attn_cfg_t *cfg, const daf_cache_t *cache, int32_t layer,
+                                  const daf_cache_rows_t *rows, float theta, const void *q, int64_t q_stride,
+                                  const void *k, const void *v, int64_t kv_stride, void *q_out, hipStream_t stream) {
+  CHECK(check_cache(cache));
+  CHECK(check_cfg(cfg, cache));
+  CHECK(check_layer(cache, layer));
+  CHECK(check_rows(rows));
+  if (!(theta > 0.f) || !isfinite(theta)) return fail(DAF_ERR_INVALID_ARG, "theta must be finite and > 0");
+  const int elem = cfg->dtype == DAF_BF16 ? 2 : 4, d = cache->head_dim;
+  const int64_t q_row = (int64_t)cfg->n_q_heads * d, kv_row = (int64_t)cache->n_kv_heads * d;
+  if (!q != !q_out) return fail(DAF_ERR_INVALID_ARG, "q and q_out go together");
+  if ((q && q_stride < q_row) || kv_stride < kv_row)
+    return fail(DAF_ERR_INVALID_ARG, "row strides (%lld of q, %lld of k and v) are below the rows' %lld and %lld elements",
+                (long long)q_stride, (long long)kv_stride, (long long)q_row, (long long)kv_row);
+  if (q_stride > INT32_MAX || kv_stride > INT32_MAX)
+    return fail(DAF_ERR_UNSUPPORTED, "row strides must be below 2^31 elements");
+  if ((q && q_stride * elem % 16 != 0) || kv_stride * elem % 16 != 0)
+    return fail(DAF_ERR_ALIGNMENT, "row strides must be multiples of 16 bytes");
+  if (q && q == q_out && q_stride != q_row)
+    return fail(DAF_ERR_INVALID_ARG, "q_out may be q only where q_stride is Hq * D");
+  if (rows->cu[rows->n] > 0) {
+    CHECK(need_ptr(k, "k"));
+    CHECK(need_ptr(v, "v"));
+    CHECK(aligned(q, "q"));
+    CHECK(aligned(q_out, "q_out"));
+  }
+  RopeLaunch r{};
+  r.q = q;
+  r.q_out = q_out;
+  r.q_pitch = q_stride * elem;
+  r.kv_pitch = kv_stride * elem;
+  r.hq = cfg->n_q_heads;
+  for (int i = 0; i < d / 2; ++i) r.turn[i] = pow((double)theta, -2.0 * i / d) / 6.283185307179586476925;
+  return store(true, cfg, cache, layer, rows, k, v, stream, &r);
 }
 
 size_t daf_cache_attn_workspace_size(const daf_attn_cfg_t *cfg, const daf_cache_t *cache, const daf_cache_rows_t *rows,

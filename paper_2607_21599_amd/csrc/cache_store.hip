@@ -1,4 +1,5 @@
-// Rows into and out of the paged 8-bit K/V cache (daf_cache_write, daf_cache_read).
+// Rows into and out of the paged 8-bit K/V cache (daf_cache_write, daf_cache_read,
+// daf_cache_write_rope).
 //
 // A value x is held as code * s, code in e4m3, s a power of two per page and head:
 // s = 2^e with the smallest e >= -100 for which max |x| <= 448 * 2^e. Dividing by s
@@ -172,16 +173,41 @@ __device__ __forceinline__ void put(const X &x, Old &old, unsigned char *codes, 
   }
 }
 
+// ---- the rotary embedding -----------------------------------------------------------
+// Features i and i + D/2 of a head turn by the angle pos * theta^(-2i/D). The angle is taken
+// in turns (2 pi), in fp64, where the whole turns of far positions fall away exactly;
+// what is left, within an eighth of a turn of a multiple of a quarter, goes into the Taylor
+// series of sine and cosine up to x^15 and x^14 (off by less than 2^-44), also in fp64:
+// the values are those of fp32, rounded once.
+__device__ __forceinline__ void sine_cosine(double turns, float &sine, float &cosine) {
+  const double r = turns - rint(turns), q = rint(4 * r);
+  const double x = (r - 0.25 * q) * 6.283185307179586476925, y = x * x;
+  auto f = [&](double next, double den) { return 1 - y * next * (1 / den); };
+  const double s = x * f(f(f(f(f(f(f(1, 14. * 15), 12. * 13), 10. * 11), 8. * 9), 6. * 7), 4. * 5), 2. * 3);
+  const double c = f(f(f(f(f(f(f(1, 13. * 14), 11. * 12), 9. * 10), 7. * 8), 5. * 6), 3. * 4), 1. * 2);
+  const int k = (int)q & 3;  // quarters of a turn
+  const float a = (float)(k & 1 ? c : s), b = (float)(k & 1 ? s : c);
+  sine = k & 2 ? -a : a;
+  cosine = k == 1 || k == 2 ? -b : b;
+}
+
+// Sines and cosines of a page's slots (or of some rows), [slot][pair of features]
+template <int D>
+struct Angles {
+  float cosine[kPage][D / 2], sine[kPage][D / 2];
+};
+
 // K (IS_V false) or V of one page of one head: the rows in sh.row (set, and a
-// barrier passed). tokens: of the page, at the call's end; held: before it (write).
-template <bool BF16, int D, bool WRITE, bool IS_V>
-__device__ __forceinline__ void do_page(const StoreLaunch &p, Shared &sh, int64_t row0, int h, int page, int tokens,
-                                        int held) {
+// barrier passed). pg: the page's number in its sequence; tokens: of the page, at the
+// call's end; held: before it (write). With angles, K is turned first.
+template <bool BF16, int D, bool WRITE, bool IS_V, bool ROPE>
+__device__ __forceinline__ void do_page(const StoreLaunch &p, Shared &sh, const RopeLaunch *rope, Angles<D> *angles,
+                                        int64_t row0, int h, int pg, int page, int tokens, int held) {
   using E = Elem<BF16>;
   using S = Share<D, IS_V>;
   constexpr int N = S::N, CH = S::CH, SPP = S::SPP, PASSES = S::PASSES, LPS = S::LPS, Q = S::Q;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  const size_t rowb = (size_t)p.c.hkv * D * E::kBytes;
+  const size_t rowb = ROPE ? (size_t)rope->kv_pitch : (size_t)p.c.hkv * D * E::kBytes;
   const bool there = (unsigned)page < (unsigned)p.c.n_pages;
   const size_t blk = there ? (size_t)page * p.c.hkv + h : 0;
   unsigned char *codes = (IS_V ? p.c.v : p.c.k) + blk * (kPage * D);
@@ -208,12 +234,42 @@ __device__ __forceinline__ void do_page(const StoreLaunch &p, Shared &sh, int64_
   const unsigned mine = bits(go);
 
   if constexpr (WRITE) {
-    unsigned x[PASSES][E::words(N)] = {};
+    constexpr bool TURN = ROPE && !IS_V;
+    using X = Elem<BF16 && !TURN>;  // turned values are fp32
+    unsigned given[PASSES][E::words(N)] = {};
     const unsigned rows_mine = bits(can);  // not `go`: these loads need not wait for the page's id
 #pragma unroll
     for (int i = 0; i < PASSES; ++i)
-      if ((rows_mine >> i) & 1) E::template load<N>(at(i), x[i]);
+      if ((rows_mine >> i) & 1) E::template load<N>(at(i), given[i]);
     if (!go) return;  // uniform in the workgroup
+    unsigned x[PASSES][X::words(N)];
+    if constexpr (TURN) {
+      constexpr int HALF = D / 2;
+      const double turn = rope->turn[t % HALF];
+#pragma unroll 1
+      for (int s = t / HALF; s < kPage; s += kThreads / HALF)
+        if ((go >> s) & 1) sine_cosine((pg * (double)kPage + s) * turn, angles->sine[s][t % HALF], angles->cosine[s][t % HALF]);
+      __syncthreads();
+      const bool high = d0 >= HALF;
+#pragma unroll
+      for (int i = 0; i < PASSES; ++i) {
+        unsigned other[E::words(N)];  // the half of the pairs that is another lane's
+#pragma unroll
+        for (int j = 0; j < E::words(N); ++j) other[j] = __shfl_xor((int)given[i][j], CH / 2);
+        const float *c = &angles->cosine[slot(i)][d0 % HALF], *s = &angles->sine[slot(i)][d0 % HALF];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const float b = E::template get<false>(other, j) * s[j];
+          const float y = __builtin_fmaf(E::template get<false>(given[i], j), c[j], high ? b : -b);
+          x[i][j] = (mine >> i) & 1 ? __builtin_bit_cast(unsigned, y) : 0u;  // other slots have no angles
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < PASSES; ++i)
+#pragma unroll
+        for (int j = 0; j < E::words(N); ++j) x[i][j] = given[i][j];
+    }
     float present = 0.f;
     if (t == 0) present = *scale;
     const bool kept = ((held >= 64 ? ~0ull : (1ull << held) - 1) & ~go) != 0;
@@ -229,8 +285,8 @@ __device__ __forceinline__ void do_page(const StoreLaunch &p, Shared &sh, int64_
 #pragma unroll
     for (int i = 0; i < PASSES; ++i)
 #pragma unroll
-      for (int j = 0; j < E::words(N); ++j) top = E::max_bits(top, x[i][j]);
-    top = wave_max(E::whole(top));
+      for (int j = 0; j < X::words(N); ++j) top = X::max_bits(top, x[i][j]);
+    top = wave_max(X::whole(top));
     if (lane == 0) sh.top[0][wave] = top;
     if (t == 0) sh.scale = present;
     __syncthreads();
@@ -241,7 +297,7 @@ __device__ __forceinline__ void do_page(const StoreLaunch &p, Shared &sh, int64_
 #pragma unroll
       for (int i = 0; i < PASSES; ++i)
 #pragma unroll
-        for (int j = 0; j < N; ++j) m = fmaxf(m, fabsf(E::template get<true>(x[i], j)));
+        for (int j = 0; j < N; ++j) m = fmaxf(m, fabsf(X::template get<true>(x[i], j)));
       top = wave_max(__builtin_bit_cast(unsigned, m));
       if (lane == 0) sh.top[1][wave] = top;
       __syncthreads();
@@ -252,8 +308,8 @@ __device__ __forceinline__ void do_page(const StoreLaunch &p, Shared &sh, int64_
     const float inv = inverse(s1), ratio = s0 * inv;
     const bool grow = kept && s1 > s0;
     if (t == 0) *scale = s1;
-    special ? put<BF16, D, IS_V, true>(x, old, codes, mine, kept, grow, inv, ratio, slot0, d0)
-            : put<BF16, D, IS_V, false>(x, old, codes, mine, kept, grow, inv, ratio, slot0, d0);
+    special ? put<BF16 && !TURN, D, IS_V, true>(x, old, codes, mine, kept, grow, inv, ratio, slot0, d0)
+            : put<BF16 && !TURN, D, IS_V, false>(x, old, codes, mine, kept, grow, inv, ratio, slot0, d0);
   } else {
     const unsigned out = bits(asked);
     if (!out) return;
@@ -298,9 +354,8 @@ __device__ __forceinline__ void do_page(const StoreLaunch &p, Shared &sh, int64_
 // Units of a request: with positions, kStoreRows rows each, of which every one that
 // is its page's first takes the page; else one page each of those that its n last
 // rows can touch.
-template <bool BF16, int D, bool WRITE>
-__global__ __launch_bounds__(kThreads) void cache_store_kernel(const StoreLaunch p) {
-  __shared__ Shared sh;
+template <bool BF16, int D, bool WRITE, bool ROPE>
+__device__ __forceinline__ void store_job(const StoreLaunch &p, Shared &sh, const RopeLaunch *rope, Angles<D> *angles) {
   const int t = threadIdx.x;
   const int half = p.units * p.c.hkv;  // workgroups of K, then those of V
   const bool is_v = (int)blockIdx.x >= half || !p.k;
@@ -333,8 +388,8 @@ __global__ __launch_bounds__(kThreads) void cache_store_kernel(const StoreLaunch
     const int pg = (int)(pg64 < 0 ? -1 : pg64);
     const int held = (int)min(max(first - pg64 * kPage, (int64_t)0), (int64_t)kPage);
     const int tokens = pg < 0 ? 0 : min(L - pg * kPage, kPage);
-    is_v ? do_page<BF16, D, WRITE, true>(p, sh, row0, h, page_of(pg), tokens, held)
-         : do_page<BF16, D, WRITE, false>(p, sh, row0, h, page_of(pg), tokens, held);
+    is_v ? do_page<BF16, D, WRITE, true, ROPE>(p, sh, rope, angles, row0, h, pg, page_of(pg), tokens, held)
+         : do_page<BF16, D, WRITE, false, ROPE>(p, sh, rope, angles, row0, h, pg, page_of(pg), tokens, held);
     return;
   }
   // which of the unit's rows are their page's first, from one load per lane
@@ -355,12 +410,94 @@ __global__ __launch_bounds__(kThreads) void cache_store_kernel(const StoreLaunch
     }
     __syncthreads();
     const int tokens = pg < 0 || (int64_t)pg * kPage >= L ? 0 : min(L - pg * kPage, kPage);
-    is_v ? do_page<BF16, D, WRITE, true>(p, sh, row0, h, page_of(pg), tokens, tokens)
-         : do_page<BF16, D, WRITE, false>(p, sh, row0, h, page_of(pg), tokens, tokens);
+    is_v ? do_page<BF16, D, WRITE, true, ROPE>(p, sh, rope, angles, row0, h, pg, page_of(pg), tokens, tokens)
+         : do_page<BF16, D, WRITE, false, ROPE>(p, sh, rope, angles, row0, h, pg, page_of(pg), tokens, tokens);
   }
 }
 
+template <bool BF16, int D, bool WRITE>
+__global__ __launch_bounds__(kThreads) void cache_store_kernel(const StoreLaunch p) {
+  __shared__ Shared sh;
+  store_job<BF16, D, WRITE, false>(p, sh, nullptr, nullptr);
+}
+
+// Rows of q, turned: a workgroup has kThreads / (D / 2) rows, whose angles its threads make
+// while the first pieces of the rows are on their way.
+template <bool BF16, int D>
+__device__ __forceinline__ void turn_q(const StoreLaunch &p, const RopeLaunch &rope, Angles<D> &angles, int job) {
+  using E = Elem<BF16>;
+  constexpr int HALF = D / 2, ROWS = kThreads / HALF, PIECES = HALF / 8, FLIGHT = 4;
+  const int t = threadIdx.x, row0 = job * ROWS, n = min(ROWS, p.cu[p.n_req] - row0);
+  const int items = n * rope.hq * PIECES;  // a piece: 8 features of the one half and 8 of the other
+  const unsigned char *q = static_cast<const unsigned char *>(rope.q);
+  unsigned char *out = static_cast<unsigned char *>(rope.q_out);
+  auto feature = [&](int w) { return (w / PIECES % rope.hq * D + w % PIECES * 8) * E::kBytes; };  // byte in the row
+  auto row_of = [&](int w) { return w / (PIECES * rope.hq); };
+  unsigned a[FLIGHT][E::words(8)], b[FLIGHT][E::words(8)];
+  auto load = [&](int i, int w) {
+    const unsigned char *at = q + (int64_t)(row0 + row_of(w)) * rope.q_pitch + feature(w);
+    E::template load<8>(at, a[i]);
+    E::template load<8>(at + HALF * E::kBytes, b[i]);
+  };
+#pragma unroll
+  for (int i = 0; i < FLIGHT; ++i)
+    if (t + i * kThreads < items) load(i, t + i * kThreads);
+  // the lanes of HALF have one row: its request, its position, its angles
+  const int r = t / HALF, row = row0 + min(r, n - 1);
+  int64_t at;
+  if (p.pos) {
+    at = p.pos[row];
+  } else {
+    int b = 0;
+    for (int step = kMaxCacheReqs / 2; step; step >>= 1)
+      if (b + step < p.n_req && p.cu[b + step] <= row) b += step;
+    const int seq = p.seq ? p.seq[b] : b;
+    at = (int64_t)seq_len(p.c.len, p.c.n_seqs, p.c.max_seq_pages, seq) - p.cu[b + 1] + row;
+  }
+  sine_cosine((double)at * rope.turn[t % HALF], angles.sine[r][t % HALF], angles.cosine[r][t % HALF]);
+  __syncthreads();
+  for (int w0 = t; w0 < items; w0 += FLIGHT * kThreads) {
+#pragma unroll
+    for (int i = 0; i < FLIGHT; ++i) {
+      const int w = w0 + i * kThreads;
+      if (w >= items) break;
+      if (w0 != t) load(i, w);
+      const int k = row_of(w), c = w % PIECES * 8;
+      float x[8], y[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float u = E::template get<false>(a[i], j), v = E::template get<false>(b[i], j);
+        const float co = angles.cosine[k][c + j], si = angles.sine[k][c + j];
+        x[j] = __builtin_fmaf(u, co, -(v * si));
+        y[j] = __builtin_fmaf(v, co, u * si);
+        if constexpr (BF16) x[j] = (float)(__bf16)x[j], y[j] = (float)(__bf16)y[j];
+      }
+      unsigned char *to = out + (int64_t)(row0 + k) * rope.hq * (D * E::kBytes) + feature(w);
+      E::template store<8>(to, x);
+      E::template store<8>(to + HALF * E::kBytes, y);
+    }
+  }
+}
+
+// K and V as above, K turned on the way, then the rows of q.
+template <bool BF16, int D>
+__global__ __launch_bounds__(kThreads) void cache_rope_store_kernel(const StoreLaunch p, const RopeLaunch rope) {
+  __shared__ Shared sh;
+  __shared__ Angles<D> angles;
+  const int q0 = p.units * p.c.hkv * 2;
+  if ((int)blockIdx.x >= q0) turn_q<BF16, D>(p, rope, angles, blockIdx.x - q0);
+  else store_job<BF16, D, true, true>(p, sh, &rope, &angles);
+}
+
 }  // namespace
+
+hipError_t launch_cache_rope_store(bool bf16, const StoreLaunch &p, const RopeLaunch &rope, hipStream_t st) {
+  const unsigned grid = (unsigned)p.units * p.c.hkv * 2 + (rope.q ? rope_jobs(p.cu[p.n_req], p.c.d) : 0);
+  auto go = [&](auto kern) { kern<<<grid, kThreads, 0, st>>>(p, rope); };
+  if (p.c.d == 128) bf16 ? go(cache_rope_store_kernel<true, 128>) : go(cache_rope_store_kernel<false, 128>);
+  else bf16 ? go(cache_rope_store_kernel<true, 64>) : go(cache_rope_store_kernel<false, 64>);
+  return hipGetLastError();
+}
 
 hipError_t launch_cache_store(bool write, bool bf16, const StoreLaunch &p, hipStream_t st) {
   const unsigned grid = (unsigned)p.units * p.c.hkv * (p.k && p.v ? 2 : 1);
