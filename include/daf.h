@@ -544,6 +544,38 @@ daf_status_t daf_cache_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *cache,
                             int32_t max_len, const void *q, void *o, float *lse,
                             void *workspace, size_t ws_bytes, hipStream_t stream);
 
+/* Requests of a call in groups whose sequences begin with the same pages, as
+ * daf_pages_fork leaves them: beams of one prompt, requests over one document set. cu
+ * (HOST, [n + 1] prefix sums from 0) has the requests of each group, one after the other,
+ * cu[n] = rows->n; shared (HOST [n]) the tokens that a group's sequences have in common,
+ * of which full pages count (0: none). Read during the call only. */
+typedef struct {
+  int32_t n;
+  const int32_t *cu;
+  const int32_t *shared;
+} daf_cache_groups_t;
+
+/* Bytes of workspace daf_cache_attn_shared needs (0 on bad input or none needed). It grows
+ * with the rows: at most 8 (D + 1) bytes per row and query head of 256 requests, 512 (D + 1)
+ * per group and K/V head of them, and 280 MB. */
+size_t daf_cache_attn_shared_workspace_size(const daf_attn_cfg_t *cfg,
+                                            const daf_cache_t *cache,
+                                            const daf_cache_rows_t *rows,
+                                            const daf_cache_groups_t *groups,
+                                            int32_t max_len);
+
+/* daf_cache_attn, with the pages that a group's sequences have in common read once for all
+ * of its rows. Arguments and results as there. The first shared / 64 entries of the tables
+ * of a group's sequences must be the same, which is not checked: where they are not, rows see
+ * the keys of another sequence of their group there, as far as their own len goes. A group of
+ * more than 256 requests may read its pages once for each 256. Made for groups whose own
+ * tokens are few beside the shared ones: those are taken 16 (row, head) pairs at a time. */
+daf_status_t daf_cache_attn_shared(const daf_attn_cfg_t *cfg, const daf_cache_t *cache,
+                                   int32_t layer, const daf_cache_rows_t *rows,
+                                   const daf_cache_groups_t *groups, int32_t max_len,
+                                   const void *q, void *o, float *lse, void *workspace,
+                                   size_t ws_bytes, hipStream_t stream);
+
 /* Page calls. They work on all layers, take sequence and page lists in DEVICE
  * memory and never wait for the device. Those that take pages take the free ones
  * (refs 0) of the lowest ids, in the order of the requests and of their pages, and

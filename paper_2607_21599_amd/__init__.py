@@ -21,8 +21,9 @@ __all__ = [
     "daf_layer_attn_noalloc", "daf_check_indices", "daf_select_important",
     "daf_linear", "daf_linear_swiglu", "daf_linear_mx_workspace_size", "daf_linear_mx", "daf_rmsnorm", "daf_add_rmsnorm", "daf_rope", "daf_silu_mul", "daf_decoder_layer_workspace_size",
     "daf_decoder_layer", "LayerWeights", "DAF_LAYER_DAF", "DAF_LAYER_FULL",
-    "DAF_PAGE_TOKENS", "Cache", "CacheRows",
+    "DAF_PAGE_TOKENS", "Cache", "CacheRows", "CacheGroups",
     "daf_cache_write", "daf_cache_write_rope", "daf_cache_read", "daf_cache_attn_workspace_size", "daf_cache_attn",
+    "daf_cache_attn_shared_workspace_size", "daf_cache_attn_shared",
     "daf_pages_workspace_size", "daf_pages_extend", "daf_pages_fork", "daf_pages_unshare", "daf_pages_free",
     "daf_pages_copy", "daf_pages_compact",
     "daf_status_string", "daf_last_error", "daf_version", "EXPORTED",
@@ -44,6 +45,7 @@ EXPORTED = [
     "daf_linear", "daf_linear_swiglu", "daf_linear_mx_workspace_size", "daf_linear_mx", "daf_rmsnorm", "daf_add_rmsnorm", "daf_rope", "daf_silu_mul", "daf_decoder_layer_workspace_size",
     "daf_decoder_layer",
     "daf_cache_write", "daf_cache_write_rope", "daf_cache_read", "daf_cache_attn_workspace_size", "daf_cache_attn",
+    "daf_cache_attn_shared_workspace_size", "daf_cache_attn_shared",
     "daf_pages_workspace_size", "daf_pages_extend", "daf_pages_fork", "daf_pages_unshare", "daf_pages_free",
     "daf_pages_copy", "daf_pages_compact",
     "daf_status_string", "daf_last_error", "daf_version",
@@ -152,6 +154,21 @@ class CacheRows(ctypes.Structure):
                          _list(pos, "pos", int(self._cu[-1]) if n >= 0 else 0))
 
 
+class CacheGroups(ctypes.Structure):
+    """daf_cache_groups_t: the requests of a call in groups whose sequences begin with the
+    same pages. ``cu`` are the host prefix sums of the requests per group, ``shared`` the
+    tokens that each group's sequences have in common."""
+    _fields_ = [("n", ctypes.c_int32), ("cu", ctypes.POINTER(ctypes.c_int32)), ("shared", ctypes.POINTER(ctypes.c_int32))]
+
+    def __init__(self, cu, shared):
+        self._cu = np.ascontiguousarray(cu, dtype=np.int32)
+        self._shared = np.ascontiguousarray(shared, dtype=np.int32)
+        if len(self._shared) != len(self._cu) - 1:
+            raise ValueError(f"{len(self._shared)} lengths for {len(self._cu) - 1} groups")
+        p = ctypes.POINTER(ctypes.c_int32)
+        super().__init__(len(self._shared), self._cu.ctypes.data_as(p), self._shared.ctypes.data_as(p))
+
+
 _lib = None
 
 
@@ -164,7 +181,7 @@ def lib() -> ctypes.CDLL:
                                "`python -c 'import __graft_entry__ as g; g.build()'`")
         L = ctypes.CDLL(library_path)
         cfgp, bp = ctypes.POINTER(AttnCfg), ctypes.POINTER(_BatchC)
-        cp, rp = ctypes.POINTER(Cache), ctypes.POINTER(CacheRows)
+        cp, rp, gp = ctypes.POINTER(Cache), ctypes.POINTER(CacheRows), ctypes.POINTER(CacheGroups)
         i32, i64, u32, sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_size_t
         sig = {
             "daf_gather_important": (i32, [bp, i32, _vp, i64, _vp, _vp, _vp]),
@@ -196,6 +213,8 @@ def lib() -> ctypes.CDLL:
             "daf_cache_read": (i32, [cfgp, cp, i32, rp, _vp, _vp, _vp]),
             "daf_cache_attn_workspace_size": (sz, [cfgp, cp, rp, i32]),
             "daf_cache_attn": (i32, [cfgp, cp, i32, rp, i32, _vp, _vp, _vp, _vp, sz, _vp]),
+            "daf_cache_attn_shared_workspace_size": (sz, [cfgp, cp, rp, gp, i32]),
+            "daf_cache_attn_shared": (i32, [cfgp, cp, i32, rp, gp, i32, _vp, _vp, _vp, _vp, sz, _vp]),
             "daf_pages_workspace_size": (sz, [cp]),
             "daf_pages_extend": (i32, [cp, i32, _vp, _vp, _vp, _vp]),
             "daf_pages_fork": (i32, [cp, i32, _vp, _vp, _vp, _vp, sz, _vp]),
@@ -430,6 +449,17 @@ def daf_cache_attn(cfg: AttnCfg, cache: Cache, layer: int, rows: CacheRows, max_
                    ws_bytes: int, stream=None):
     _check(lib().daf_cache_attn(_cfgp(cfg), cache, layer, rows, max_len, _ptr(q), _ptr(o), _ptr(lse),
                                 _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def daf_cache_attn_shared_workspace_size(cfg: AttnCfg, cache: Cache, rows: CacheRows, groups: CacheGroups,
+                                         max_len: int) -> int:
+    return int(lib().daf_cache_attn_shared_workspace_size(_cfgp(cfg), cache, rows, groups, max_len))
+
+
+def daf_cache_attn_shared(cfg: AttnCfg, cache: Cache, layer: int, rows: CacheRows, groups: CacheGroups, max_len: int, q,
+                          o, lse, workspace, ws_bytes: int, stream=None):
+    _check(lib().daf_cache_attn_shared(_cfgp(cfg), cache, layer, rows, groups, max_len, _ptr(q), _ptr(o), _ptr(lse),
+                                       _ptr(workspace), ws_bytes, _stream(stream)))
 
 
 def daf_pages_workspace_size(cache: Cache) -> int:

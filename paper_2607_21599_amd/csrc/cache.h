@@ -12,6 +12,7 @@ constexpr int kPage = DAF_PAGE_TOKENS;  // tokens of a page
 constexpr int kMaxCacheReqs = 256;      // requests per launch (their prefix sums are a kernel argument)
 constexpr int kMaxPageSeqs = 4096;      // sequences per page call (one workgroup plans it)
 constexpr int kMaxFree = 1 << 23;       // sequences per call that frees them (a workgroup each)
+constexpr int kXcdCount = 8;            // workgroups go to the XCDs in turn
 constexpr int kStoreThreads = 256, kCacheAttnThreads = 256;  // of the workgroups
 
 // What the kernels need of a cache; k/v and the scales start at the launch's layer.
@@ -56,6 +57,8 @@ constexpr int kStoreRows = 8;  // rows at positions: rows per unit
 hipError_t launch_cache_store(bool write, bool bf16, const StoreLaunch &p, hipStream_t st);
 
 // Attention over the cache.
+// (row, head) pairs of a row block: few rows, many rows in bf16 and in fp32
+constexpr int kCacheAttnRows = 16, kCacheWideRows = 128, kCacheWideRowsF32 = 64;
 struct CacheAttnLaunch {
   CacheView c;
   const int32_t *seq, *pos;
@@ -79,10 +82,19 @@ struct CacheAttnLaunch {
   int32_t per_req;                // row blocks of every request where they are equal, else 0
   int32_t cu[kMaxCacheReqs + 1];
   int32_t blk0[kMaxCacheReqs + 1];
+  // few rows' line: all pages of a request for each of its row blocks
+  __device__ __forceinline__ int line_blocks(int b) const { return blk0[b + 1] - blk0[b]; }
+  __device__ __forceinline__ int line_pages(int, int L) const { return max(1, (L + kPage - 1) / kPage); }
+  __device__ __forceinline__ int line_page(int, int i) const { return i; }
+  __device__ __forceinline__ int least_piece() const;
+  // where results go of a row block that is whole in a workgroup (the output), or in part
+  template <typename R>
+  __device__ __forceinline__ int whole_place(const R &, int) const { return -1; }
+  __device__ __forceinline__ int edge_place(int h, int k, int second) const {
+    return ((h * n_splits + k) * 2 + second) * kCacheAttnRows;
+  }
 };
 static_assert(sizeof(CacheAttnLaunch) < 4096, "kernel arguments must fit 4 KiB");
-// (row, head) pairs of a row block: few rows, many rows in bf16 and in fp32
-constexpr int kCacheAttnRows = 16, kCacheWideRows = 128, kCacheWideRowsF32 = 64;
 // Many rows: pages of a split, at least 6 (us a call: fp32 questions over up to 7000 keys
 // 15.4, 16.5 with 3, 19.7 with 12; 18 rows of 7 heads over 8000 keys 20.0, 20.9, 25.9).
 constexpr int kMinSplitPages = 6;
@@ -91,7 +103,60 @@ constexpr size_t kLineBytes = (2 * kMaxCacheReqs + 64) * sizeof(int32_t);
 // keys 11.1 with 4, 13.4 with 8, 17.2 with 16; of 16000 keys 12.0, 13.7, 17.9; with four
 // K/V heads pieces grow longer by themselves past 16384 keys).
 constexpr int kMinPiece = 4;
+__device__ __forceinline__ int CacheAttnLaunch::least_piece() const { return kMinPiece; }
 hipError_t launch_cache_attn(bool bf16, const CacheAttnLaunch &p, hipStream_t st);
+
+// Attention of groups of requests whose first pages are the same (cache_shared.hip).
+constexpr int kSharedMaxGroups = kMaxCacheReqs;
+struct SharedLaunch {
+  CacheView c;
+  const int32_t *seq, *pos;
+  const void *q;
+  void *o;
+  float *lse;
+  // partial outputs and their LSE, per (row, head) pair: [first_wgs][block_rows] of the
+  // groups' pages, then [hkv][rows * group] of row blocks whose rest of the line is in one
+  // workgroup, then [hkv][n_splits][2][16] of the others
+  float *part_o, *part_lse;
+  int32_t *line;       // the requests' first units in the line, their units, a piece's
+  int32_t lse_stride;
+  int32_t hq, group;
+  int32_t max_len;
+  int32_t rows;        // of the launch
+  int32_t n_groups;
+  int32_t block_rows;  // pairs of a row block of a group
+  int32_t split_pages; // pages per split of a group's pages
+  int32_t first_wgs;   // workgroups of the groups' pages
+  int32_t n_splits;    // workgroups per head of the line
+  int32_t whole;       // a row block's rest of the line is one unit
+  int32_t n_req;
+  float scale_log2;
+  int32_t cu[kMaxCacheReqs + 1];
+  int32_t pages[kMaxCacheReqs];           // of each request that are its group's
+  int32_t wg0[kSharedMaxGroups + 1];      // first workgroup of each group
+  unsigned char first[kSharedMaxGroups];  // first request of each group
+  __device__ __forceinline__ int line_blocks(int b) const {
+    return ((cu[b + 1] - cu[b]) * group + kCacheAttnRows - 1) / kCacheAttnRows;
+  }
+  __device__ __forceinline__ int line_pages(int b, int L) const {
+    return whole ? 1 : max(1, (L + kPage - 1) / kPage - pages[b]);
+  }
+  __device__ __forceinline__ int line_page(int b, int i) const {
+    return whole && i > 0 ? INT32_MAX : pages[b] + i;  // the end of a whole line: the sequence's
+  }
+  __device__ __forceinline__ int least_piece() const;
+  __device__ __forceinline__ int whole_pair(int h) const { return first_wgs * block_rows + h * rows * group; }
+  template <typename R>
+  __device__ __forceinline__ int whole_place(const R &r, int h) const {
+    return whole_pair(h) + r.row0 * group + r.block * kCacheAttnRows;
+  }
+  __device__ __forceinline__ int edge_place(int h, int k, int second) const {
+    return whole_pair(c.hkv) + ((h * n_splits + k) * 2 + second) * kCacheAttnRows;
+  }
+};
+__device__ __forceinline__ int SharedLaunch::least_piece() const { return whole ? 1 : kMinPiece; }
+static_assert(sizeof(SharedLaunch) < 4096, "kernel arguments must fit 4 KiB");
+hipError_t launch_cache_shared(bool bf16, const SharedLaunch &p, hipStream_t st);
 
 // Page calls.
 struct PoolView {

@@ -336,6 +336,193 @@ daf_status_t attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, int32_t layer
   return ok();
 }
 
+// ---- attention of groups ---------------------------------------------------------
+// The calls' launches take kMaxCacheReqs requests each; a group that two launches share is
+// one of each.
+int64_t shared_chunks(const daf_cache_rows_t *rows) { return (rows->n + kMaxCacheReqs - 1) / kMaxCacheReqs; }
+
+daf_status_t check_groups(const daf_cache_rows_t *rows, const daf_cache_groups_t *g) {
+  if (!g) return fail(DAF_ERR_INVALID_ARG, "groups is NULL");
+  if (g->n < 0) return fail(DAF_ERR_INVALID_ARG, "groups.n=%d must be >= 0", g->n);
+  if (!g->cu) return fail(DAF_ERR_INVALID_ARG, "groups.cu must be a non-NULL host array");
+  if (g->cu[0] != 0) return fail(DAF_ERR_INVALID_ARG, "groups.cu must start at 0");
+  for (int i = 0; i < g->n; ++i)
+    if (g->cu[i + 1] < g->cu[i]) return fail(DAF_ERR_INVALID_ARG, "group %d: groups.cu must be non-decreasing", i);
+  if (g->cu[g->n] != rows->n)
+    return fail(DAF_ERR_INVALID_ARG, "groups have %d requests, rows %d", g->cu[g->n], rows->n);
+  if (g->n > 0 && !g->shared) return fail(DAF_ERR_INVALID_ARG, "groups.shared must be a non-NULL host array");
+  for (int i = 0; i < g->n; ++i)
+    if (g->shared[i] < 0) return fail(DAF_ERR_INVALID_ARG, "group %d: shared=%d must be >= 0", i, g->shared[i]);
+  return DAF_OK;
+}
+
+// Pages that requests b0 .. b1 of a group take together; none for one request of few rows,
+// whose line is as good.
+int group_pages(const daf_attn_cfg_t *cfg, const daf_cache_rows_t *rows, int b0, int b1, int32_t shared, int32_t max_len) {
+  const int64_t pairs = (int64_t)(rows->cu[b1] - rows->cu[b0]) * (cfg->n_q_heads / cfg->n_kv_heads);
+  return b1 - b0 > 1 || pairs > 4 * kCacheAttnRows ? std::min(shared, max_len) / kPage : 0;
+}
+
+bool any_shared(const daf_attn_cfg_t *cfg, const daf_cache_rows_t *rows, const daf_cache_groups_t *g, int32_t max_len) {
+  for (int i = 0; i < g->n; ++i)
+    if (group_pages(cfg, rows, g->cu[i], g->cu[i + 1], g->shared[i], max_len) > 0) return true;
+  return false;
+}
+
+// The launch of the requests from b0 on, without its pointers. Pairs of its partial results,
+// 0 for no rows, -1: too many.
+int64_t plan_shared(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_cache_rows_t *rows,
+                    const daf_cache_groups_t *g, int32_t max_len, int b0, SharedLaunch &p) {
+  p.n_req = std::min(kMaxCacheReqs, rows->n - b0);
+  p.hq = cfg->n_q_heads;
+  p.group = cfg->n_q_heads / cfg->n_kv_heads;
+  p.max_len = max_len;
+  p.n_groups = 0;
+  for (int i = 0; i <= p.n_req; ++i) p.cu[i] = rows->cu[b0 + i] - rows->cu[b0];
+  p.rows = p.cu[p.n_req];
+  if (p.rows == 0) return 0;
+  int64_t most = 0, blocks = 0;
+  for (int i = 0; i < g->n; ++i) {
+    const int lo = std::max(g->cu[i], b0), hi = std::min(g->cu[i + 1], b0 + p.n_req);
+    if (lo >= hi) continue;
+    p.first[p.n_groups++] = (unsigned char)(lo - b0);
+    const int pages = group_pages(cfg, rows, lo, hi, g->shared[i], max_len);
+    for (int b = lo; b < hi; ++b) p.pages[b - b0] = pages;
+    if (pages > 0) most = std::max(most, (int64_t)(rows->cu[hi] - rows->cu[lo]) * p.group);
+  }
+  const bool bf16 = cfg->dtype == DAF_BF16;
+  p.block_rows = bf16 && most > kCacheWideRowsF32 ? kCacheWideRows : kCacheWideRowsF32;
+
+  // the line of what is not the groups': as in plan_attn
+  int64_t tail_pages = 1;
+  for (int b = 0; b < p.n_req; ++b) {
+    const int64_t n = row_blocks(cfg, p.cu[b + 1] - p.cu[b], kCacheAttnRows);
+    blocks += n;
+    if (n > 0) tail_pages = std::max(tail_pages, ((int64_t)max_len + kPage - 1) / kPage - p.pages[b]);
+  }
+  const int64_t jobs = blocks * c->n_kv_heads;
+  p.whole = tail_pages <= std::clamp<int64_t>(jobs / 3, 16, 64);
+  int64_t n_splits = blocks;
+  if (!p.whole) {
+    const bool two = p.n_req > 1 && (bf16 || cfg->head_dim == 64);
+    const int64_t wgs = (two ? 512 : 256) / c->n_kv_heads, line = blocks * tail_pages;
+    if (line > INT32_MAX / 2) return -1;
+    n_splits = std::max<int64_t>(2, std::min<int64_t>(wgs, (line + kMinPiece - 1) / kMinPiece));
+  }
+  if (jobs > INT32_MAX / 2) return -1;
+  p.n_splits = (int)n_splits;
+
+  // the groups' pages: two workgroups per CU in all, where there is work for them
+  auto group_blocks = [&](int i) {
+    const int lo = p.first[i], hi = i + 1 < p.n_groups ? p.first[i + 1] : p.n_req;
+    return ((int64_t)(p.cu[hi] - p.cu[lo]) * p.group + p.block_rows - 1) / p.block_rows;
+  };
+  auto workgroups = [&](int split_pages) {
+    int64_t n = 0;
+    for (int i = 0; i < p.n_groups; ++i) {
+      const int pages = p.pages[p.first[i]];
+      n += (pages + split_pages - 1) / split_pages * c->n_kv_heads * group_blocks(i);
+    }
+    return n;
+  };
+  int longest = 1;
+  for (int b = 0; b < p.n_req; ++b) longest = std::max(longest, p.pages[b]);
+  auto least_split = [&](int lo, int64_t wgs) {  // smallest of at least lo pages with at most wgs workgroups
+    int hi = std::max(lo, longest);
+    while (lo < hi) {
+      const int mid = lo + (hi - lo) / 2;
+      if (workgroups(mid) <= wgs) hi = mid;
+      else lo = mid + 1;
+    }
+    return lo;
+  };
+  const int64_t target = std::max<int64_t>(256, 512 - n_splits * c->n_kv_heads);
+  p.split_pages = least_split(std::min(kMinSplitPages, longest), target);
+  if (workgroups(p.split_pages) > target || p.split_pages > 64) p.split_pages = least_split(std::min(64, longest), 4096);
+  int64_t wg = 0;
+  for (int i = 0; i < p.n_groups; ++i) {
+    p.wg0[i] = (int)wg;
+    const int64_t units = (int64_t)((p.pages[p.first[i]] + p.split_pages - 1) / p.split_pages) * c->n_kv_heads;
+    wg += units * group_blocks(i);
+    if (wg > INT32_MAX / kCacheWideRows / 4) return -1;
+  }
+  p.wg0[p.n_groups] = (int)wg;
+  p.first_wgs = (int)wg;
+  const int64_t edges = p.whole ? 0 : n_splits * c->n_kv_heads * 2 * kCacheAttnRows;
+  const int64_t pairs = wg * p.block_rows + (int64_t)p.rows * p.hq + edges;
+  if (pairs > INT32_MAX || !fits(wg + n_splits * c->n_kv_heads, kCacheAttnThreads) ||
+      !fits((int64_t)p.rows * p.hq, kCacheAttnThreads))
+    return -1;
+  return pairs;
+}
+
+size_t shared_lse_bytes(int64_t pairs) { return (pairs * sizeof(float) + 255) / 256 * 256 + kLineBytes; }
+
+// Bytes of workspace; rows that are too many for one call are refused.
+daf_status_t shared_bytes(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_cache_rows_t *rows,
+                          const daf_cache_groups_t *g, int32_t max_len, size_t &bytes) {
+  bytes = 0;
+  for (int64_t i = 0; i < shared_chunks(rows); ++i) {
+    SharedLaunch p;
+    const int64_t pairs = plan_shared(cfg, c, rows, g, max_len, (int)i * kMaxCacheReqs, p);
+    if (pairs < 0)
+      return fail(DAF_ERR_UNSUPPORTED, "%d rows over %d keys are too many for one call", rows->cu[rows->n], max_len);
+    if (pairs > 0) bytes = std::max(bytes, shared_lse_bytes(pairs) + (size_t)pairs * c->head_dim * sizeof(float));
+  }
+  return DAF_OK;
+}
+
+daf_status_t attn_shared(const daf_attn_cfg_t *cfg, const daf_cache_t *c, int32_t layer, const daf_cache_rows_t *rows,
+                         const daf_cache_groups_t *g, int32_t max_len, const void *q, void *o, float *lse,
+                         void *workspace, size_t ws_bytes, hipStream_t stream) {
+  CHECK(check_attn(cfg, c, rows, max_len));
+  CHECK(check_layer(c, layer));
+  CHECK(check_groups(rows, g));
+  const int total = rows->cu[rows->n];
+  if (total == 0) return ok();
+  if (!any_shared(cfg, rows, g, max_len))
+    return attn(cfg, c, layer, rows, max_len, q, o, lse, workspace, ws_bytes, stream);
+  CHECK(need_ptr(q, "q"));
+  CHECK(need_ptr(o, "o"));
+  CHECK(aligned(lse, "lse"));
+  size_t need;
+  CHECK(shared_bytes(cfg, c, rows, g, max_len, need));
+  if (!workspace || ws_bytes < need)
+    return fail(DAF_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace ? ws_bytes : 0);
+  CHECK(aligned(workspace, "workspace"));
+  const bool bf16 = cfg->dtype == DAF_BF16;
+  const size_t row_bytes = (size_t)cfg->n_q_heads * cfg->head_dim * (bf16 ? 2 : 4);
+  const float scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale : 1.f / sqrtf((float)cfg->head_dim);
+  for (int64_t i = 0; i < shared_chunks(rows); ++i) {
+    const int b0 = (int)i * kMaxCacheReqs;
+    SharedLaunch p;
+    const int64_t pairs = plan_shared(cfg, c, rows, g, max_len, b0, p);
+    if (pairs <= 0) continue;
+    const int64_t row0 = rows->cu[b0];
+    p.c = view(c, layer);
+    p.seq = rows->seq ? rows->seq + b0 : nullptr;
+    if (!rows->seq) {
+      if (b0 >= c->n_seqs) p.c.n_seqs = 0;
+      else p.c.n_seqs -= b0, p.c.table += (int64_t)b0 * c->max_seq_pages, p.c.len += b0;
+    }
+    p.pos = rows->pos ? rows->pos + row0 : nullptr;
+    p.q = rows_at(q, row0, row_bytes);
+    p.o = const_cast<char *>(rows_at(o, row0, row_bytes));
+    p.lse = lse ? lse + row0 : nullptr;
+    p.lse_stride = total;
+    // each launch's join is done with the places before the next one's kernel
+    char *ws = static_cast<char *>(workspace);
+    const size_t lse_bytes = shared_lse_bytes(pairs);
+    p.part_lse = reinterpret_cast<float *>(ws);
+    p.line = reinterpret_cast<int32_t *>(ws + lse_bytes - kLineBytes);
+    p.part_o = reinterpret_cast<float *>(ws + lse_bytes);
+    p.scale_log2 = scale * 1.4426950408889634f;
+    const hipError_t e = launch_cache_shared(bf16, p, stream);
+    if (e != hipSuccess) return launched(e, "shared cache attention launch");
+  }
+  return ok();
+}
+
 // ---- page calls -------------------------------------------------------------------
 size_t page_list_bytes(const daf_cache_t *c) { return ((size_t)c->n_pages * sizeof(int32_t) + 255) / 256 * 256; }
 size_t page_ws_bytes(const daf_cache_t *c) { return kPageWorkHead + 4 * page_list_bytes(c); }
@@ -420,6 +607,23 @@ daf_status_t daf_cache_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *cache,
                             const daf_cache_rows_t *rows, int32_t max_len, const void *q, void *o, float *lse,
                             void *workspace, size_t ws_bytes, hipStream_t stream) {
   return attn(cfg, cache, layer, rows, max_len, q, o, lse, workspace, ws_bytes, stream);
+}
+
+size_t daf_cache_attn_shared_workspace_size(const daf_attn_cfg_t *cfg, const daf_cache_t *cache,
+                                            const daf_cache_rows_t *rows, const daf_cache_groups_t *groups,
+                                            int32_t max_len) {
+  if (check_attn(cfg, cache, rows, max_len) != DAF_OK || check_groups(rows, groups) != DAF_OK || rows->cu[rows->n] == 0)
+    return 0;
+  if (!any_shared(cfg, rows, groups, max_len)) return plan_attn(cfg, cache, rows, max_len).total;
+  size_t bytes;
+  return shared_bytes(cfg, cache, rows, groups, max_len, bytes) == DAF_OK ? bytes : 0;
+}
+
+daf_status_t daf_cache_attn_shared(const daf_attn_cfg_t *cfg, const daf_cache_t *cache, int32_t layer,
+                                   const daf_cache_rows_t *rows, const daf_cache_groups_t *groups, int32_t max_len,
+                                   const void *q, void *o, float *lse, void *workspace, size_t ws_bytes,
+                                   hipStream_t stream) {
+  return attn_shared(cfg, cache, layer, rows, groups, max_len, q, o, lse, workspace, ws_bytes, stream);
 }
 
 size_t daf_pages_workspace_size(const daf_cache_t *cache) {

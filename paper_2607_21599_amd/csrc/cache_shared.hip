@@ -1,0 +1,215 @@
+// Attention over the paged 8-bit K/V cache for groups of requests whose sequences begin
+// with the same pages (daf_cache_attn_shared).
+//
+// exp(s - m) sums over disjoint sets of keys join by their maxima, so a row's keys fall in
+// two: the pages that are its group's, which every row of the group takes together from one
+// copy of them in LDS, and the rest of its own sequence. One launch has both kinds of work:
+//  * of a group's pages: row blocks of all its requests' (row, head) pairs by the kernel for
+//    many rows of daf_cache_attn, split over the pages;
+//  * of the rest: the line of daf_cache_attn's few rows, from the first page that is not
+//    the group's on.
+// A second launch joins a row's partial results.
+#include "cache_attn.h"
+
+namespace daf {
+namespace {
+
+// The rows of a group over its first pages. A row's limit follows from its own sequence's
+// length; rows at the end of sequences past those pages, as a decode step has them, see all.
+template <int MT>
+struct GroupRows {
+  static constexpr bool kKnown = true;
+  const SharedLaunch &p;
+  int b0, n_req;   // the group's requests
+  int row0;        // its first row
+  int pages;       // its pages
+  int *cu, *len;   // LDS: of its requests, first rows from row0 on and tokens
+  __device__ __forceinline__ bool empty() const { return false; }
+  __device__ __forceinline__ int seen() const { return pages; }
+  __device__ __forceinline__ void prepare() {
+    for (int i = threadIdx.x; i < n_req; i += kThreads) {
+      const int seq = p.seq ? p.seq[b0 + i] : b0 + i;
+      cu[i] = p.cu[b0 + i] - row0;
+      len[i] = min(seq_len(p.c.len, p.c.n_seqs, p.c.max_seq_pages, seq), p.max_len);
+    }
+    if (threadIdx.x == 0) cu[n_req] = p.cu[b0 + n_req] - row0;
+    __syncthreads();
+  }
+  __device__ __forceinline__ int limit(int row) const {
+    int b = 0;
+    for (int step = kMaxCacheReqs / 2; step; step >>= 1)
+      if (b + step < n_req && cu[b + step] <= row) b += step;
+    const int L = len[b], at = p.pos ? min(p.pos[row0 + row], L - 1) : L - cu[b + 1] + row;
+    return max(-1, min(at, pages * kPage - 1));
+  }
+};
+
+// The workgroups of a group's units, (split, head) pairs, and of their row blocks. The row
+// blocks of a unit read the same pages: neighbours on one XCD, the units on the XCDs in
+// turn; the last units, fewer than XCDs, on all of them.
+struct UnitBlock {
+  int unit, block;
+};
+__device__ __forceinline__ UnitBlock unit_block(int wg, int units, int blocks) {
+  const int even = units / kXcdCount * kXcdCount, at = wg / kXcdCount;
+  if (wg < even * blocks) return {at / blocks * kXcdCount + wg % kXcdCount, at % blocks};
+  return {wg / blocks, wg % blocks};
+}
+__device__ __forceinline__ int workgroup_of(UnitBlock u, int units, int blocks) {
+  const int even = units / kXcdCount * kXcdCount;
+  if (u.unit < even) return (u.unit / kXcdCount * blocks + u.block) * kXcdCount + u.unit % kXcdCount;
+  return u.unit * blocks + u.block;
+}
+
+template <bool BF16, int D, int MT>
+union SharedMemory {
+  struct {
+    unsigned char lds[kStages * Wide<BF16, D, MT>::PAGE_BYTES];
+    int cu[kMaxCacheReqs + 1], len[kMaxCacheReqs];
+  } wide;
+  FewShared<D> few;
+};
+
+template <bool BF16, int D, int MT>
+__device__ __forceinline__ void group_job(const SharedLaunch &p, SharedMemory<BF16, D, MT> &sh) {
+  using W = Wide<BF16, D, MT>;
+  constexpr int PAIRS = kWaves * 16 * MT;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n16 = lane & 15, quad = lane >> 4;
+  const int g = find_in(p.wg0, p.n_groups, blockIdx.x);
+  const int b0 = p.first[g], b1 = g + 1 < p.n_groups ? p.first[g + 1] : p.n_req;
+  Request r;
+  r.b = b0;
+  r.row0 = p.cu[b0];
+  r.n = p.cu[b1] - r.row0;
+  r.L = 0;  // not used
+  const int total = r.n * p.group, blocks = (total + PAIRS - 1) / PAIRS, pages = p.pages[b0];
+  const UnitBlock ub = unit_block(blockIdx.x - p.wg0[g], (pages + p.split_pages - 1) / p.split_pages * p.c.hkv, blocks);
+  const int h = ub.unit % p.c.hkv, pg0 = ub.unit / p.c.hkv * p.split_pages;
+  r.block = ub.block;
+  // the pages are those of the group's first sequence
+  const int seq = p.seq ? p.seq[b0] : b0;
+  const bool there = (unsigned)seq < (unsigned)p.c.n_seqs;
+  r.pages = p.c.table + (int64_t)(there ? seq : 0) * p.c.max_seq_pages;
+  GroupRows<MT> rows{p, b0, b1 - b0, r.row0, there ? pages : 0, sh.wide.cu, sh.wide.len};
+  W w;
+  float unit;
+  wide_rows<BF16, D, MT>(p, sh.wide.lds, r, h, pg0, min(p.split_pages, pages - pg0), rows, w, unit);
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const float l = row_sum(w.l[mt]), inv = over(l);
+    const float lse = l == 0.f ? -INFINITY : (w.m[mt] + log2f(l)) * kLn2;
+    const size_t place = (size_t)blockIdx.x * PAIRS + (wave * MT + mt) * 16 + n16;
+    if (quad == 0) p.part_lse[place] = lse;
+#pragma unroll
+    for (int db = 0; db < W::DB; ++db)
+      *reinterpret_cast<f32x4 *>(p.part_o + place * D + db * 16 + quad * 4) = w.o[mt][db] * inv * unit;
+  }
+}
+
+template <bool BF16, int D, int MT>
+__global__ __launch_bounds__(kThreads, (BF16 || D == 64 ? 2 : 1)) void cache_shared_kernel(const SharedLaunch p) {
+  __shared__ __align__(16) SharedMemory<BF16, D, MT> sh;
+  if ((int)blockIdx.x < p.first_wgs) {
+    group_job<BF16, D, MT>(p, sh);
+  } else {
+    const int job = blockIdx.x - p.first_wgs;
+    line_job<BF16, D>(p, sh.few, job % p.c.hkv, job / p.c.hkv);
+  }
+}
+
+// Join a (row, head)'s partial results, o = sum_s e^(lse_s - lse) o_s: those of its group's
+// pages, then those of the line. Groups of D / 4 lanes take them in turn, four in flight,
+// and join their sums through LDS.
+template <bool BF16, int D>
+__global__ __launch_bounds__(kThreads) void cache_shared_join_kernel(const SharedLaunch p) {
+  constexpr int LP = D / 4, GROUPS = kThreads / LP;
+  __shared__ f32x4 sh_o[GROUPS][LP];
+  __shared__ float sh_m[GROUPS], sh_l[GROUPS];
+  const int t = threadIdx.x, g = t / LP, c = t % LP, lane = t & 63;
+  const int row = blockIdx.x / p.hq, head = blockIdx.x % p.hq;
+  const int piece = p.line[2 * kMaxCacheReqs];
+  const int b = find_in(p.cu, p.n_req, row);
+  int grp = -1;
+  for (int i = 0; i < p.n_groups; i += 64) grp += __builtin_popcountll(__ballot(i + lane < p.n_groups && p.first[i + lane] <= b));
+  const int h = head / p.group, in_head = head % p.group;
+  // the line: piece s of n_line, the first one's place is its workgroup's second
+  const int pair = (row - p.cu[b]) * p.group + in_head;
+  const int units = p.line[kMaxCacheReqs + b], from = p.line[b] + pair / kRows * units;
+  const int k0 = from / piece, k1 = (from + units - 1) / piece, n_line = k1 - k0 + 1;
+  // the group's pages
+  const int b0 = p.first[grp], b1 = grp + 1 < p.n_groups ? p.first[grp + 1] : p.n_req;
+  const int in_group = (row - p.cu[b0]) * p.group + in_head;
+  const int blocks = ((p.cu[b1] - p.cu[b0]) * p.group + p.block_rows - 1) / p.block_rows;
+  const int n_first = (p.pages[b0] + p.split_pages - 1) / p.split_pages, n = n_first + n_line;
+  auto at = [&](int s) {
+    if (s < n_first) {
+      const int wg = p.wg0[grp] + workgroup_of({s * p.c.hkv + h, in_group / p.block_rows}, n_first * p.c.hkv, blocks);
+      return wg * p.block_rows + in_group % p.block_rows;
+    }
+    s -= n_first;
+    return n_line == 1 ? p.whole_pair(h) + row * p.group + in_head : p.edge_place(h, k0 + s, s == 0) + pair % kRows;
+  };
+  float m = -INFINITY, l = 0.f;
+  f32x4 x = {};
+  for (int s0 = g; s0 < n; s0 += 4 * GROUPS) {
+    float lse[4];
+    f32x4 y[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int s = s0 + j * GROUPS;
+      const size_t place = s < n ? at(s) : 0;
+      lse[j] = s < n ? p.part_lse[place] : -INFINITY;
+      y[j] = s < n ? *reinterpret_cast<const f32x4 *>(p.part_o + place * D + c * 4) : f32x4{};
+    }
+    const float to = fmaxf(m, fmaxf(fmaxf(lse[0], lse[1]), fmaxf(lse[2], lse[3])));
+    const float ref = to == -INFINITY ? 0.f : to;  // a row that sees no key there, or NaN
+    const float a = __expf(m - ref);
+    m = to;
+    l *= a;
+    x *= a;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float w = __expf(lse[j] - ref);
+      l += w;
+      x += w * y[j];
+    }
+  }
+  sh_o[g][c] = x;
+  if (c == 0) sh_m[g] = m, sh_l[g] = l;
+  __syncthreads();
+  if (g) return;
+  for (int k = 1; k < GROUPS; ++k) m = fmaxf(m, sh_m[k]);
+  const float ref = m == -INFINITY ? 0.f : m;
+  l = 0.f;
+  x = f32x4{};
+  for (int k = 0; k < GROUPS; ++k) {
+    const float w = __expf(sh_m[k] - ref);
+    l += w * sh_l[k];
+    x += w * sh_o[k][c];
+  }
+  const float inv = over(l);
+  const float y[4] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
+  store_out<BF16>(p, row, head, c * 4, y, D);
+  if (c == 0 && p.lse) p.lse[(size_t)head * p.lse_stride + row] = l == 0.f ? -INFINITY : m + __logf(l);
+}
+
+template <bool BF16, int D, int MT>
+hipError_t launch(const SharedLaunch &p, hipStream_t st) {
+  cache_shared_kernel<BF16, D, MT><<<p.first_wgs + p.n_splits * p.c.hkv, kThreads, 0, st>>>(p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  cache_shared_join_kernel<BF16, D><<<p.rows * p.hq, kThreads, 0, st>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_cache_shared(bool bf16, const SharedLaunch &p, hipStream_t st) {
+  const bool two = p.block_rows == 128;
+  if (p.c.d == 128)
+    return !bf16 ? launch<false, 128, 1>(p, st) : two ? launch<true, 128, 2>(p, st) : launch<true, 128, 1>(p, st);
+  return !bf16 ? launch<false, 64, 1>(p, st) : two ? launch<true, 64, 2>(p, st) : launch<true, 64, 1>(p, st);
+}
+
+}  // namespace daf
