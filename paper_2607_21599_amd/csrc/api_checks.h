@@ -7,9 +7,11 @@
 #include <stdio.h>
 
 #include "daf.h"
-#include "daf_internal.h"
 
 namespace daf {
+
+// Error text of the calling thread (api.hip).
+daf_status_t set_error(daf_status_t st, const char *text);
 
 inline daf_status_t fail(daf_status_t st, const char *fmt, ...) {
   char text[512];

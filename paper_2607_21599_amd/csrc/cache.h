@@ -15,6 +15,9 @@ constexpr int kMaxFree = 1 << 23;       // sequences per call that frees them (a
 constexpr int kXcdCount = 8;            // workgroups go to the XCDs in turn
 constexpr int kStoreThreads = 256, kCacheAttnThreads = 256;  // of the workgroups
 
+// Error text of the calling thread (api.hip).
+daf_status_t set_error(daf_status_t st, const char *text);
+
 // What the kernels need of a cache; k/v and the scales start at the launch's layer.
 struct CacheView {
   unsigned char *k, *v;

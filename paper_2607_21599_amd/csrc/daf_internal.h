@@ -7,12 +7,7 @@
 
 #include "block_rule.h"
 
-#include "daf.h"
-
 namespace daf {
-
-// Error text of the calling thread (api.hip).
-daf_status_t set_error(daf_status_t st, const char *text);
 
 constexpr int kXcds = 8;          // MI355X: 8 XCDs, workgroups dispatched round-robin
 constexpr int kAttnThreads = 256; // 4 waves, 32 query rows each

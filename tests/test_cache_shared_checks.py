@@ -69,7 +69,7 @@ def test_workspace_bound(hq, hkv, d, dtype):
         r = daf.CacheRows([rows * i for i in range(n_req + 1)])
         for groups in {1, min(2, n_req // 2), n_req // 2}:  # of two requests or more
             cu = [n_req * i // groups for i in range(groups + 1)]
-            for shared, max_len in ((64, 128), (4096, 5000), (131072, 140000), (1 << 18, 1 << 19), (64, 1 << 19)):
+            for shared, max_len in ((64, 128), (4096, 5000), (131072, 140000), (1 << 17, 1 << 18), (64, 1 << 18)):
                 g = daf.CacheGroups(cu, [shared] * groups)
                 size = daf.daf_cache_attn_shared_workspace_size(cfg, c, r, g, max_len)
                 most = min(n_req, 256) * rows
