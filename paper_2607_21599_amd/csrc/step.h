@@ -33,16 +33,17 @@ struct MxLaunch {
   float *part;                    // splits > 1: [splits][M][N]
   int64_t m;
   int32_t n, k;
-  int32_t splits;
+  // A workgroup has one of `row_blocks` blocks of 16 mt rows of A, one of `splits` ranges of K
+  // and one of `groups` ranges of 16-row tiles of W; of its kMxWaves waves 2^kwaves_log2
+  // have a part of the range of K each, at most `steps` times kMxStep.
+  int32_t row_blocks, groups, splits, kwaves_log2;
+  int32_t mt, steps;
+  int32_t part_steps, longer_parts;    // steps of a wave's part: one more in the first longer_parts
+  int32_t group_tiles, longer_groups;  // the same of tiles
 };
-// Which kernel, and how K is split over workgroups.
-struct MxPlan {
-  int mt, nt;  // 16-row tiles of A and of W per wave
-  int splits;
-};
-constexpr int kMxUnit = 256;  // k per turn of a wave: 128 bytes of a row of W
-constexpr int kMxWaves = 8;
-MxPlan plan_linear_mx(int64_t m, int32_t n, int32_t k);
-hipError_t launch_linear_mx(const MxPlan &plan, const MxLaunch &p, hipStream_t st);
+constexpr int kMxStep = 128;  // k of a step: a lane has 32 of them, 16 bytes of W
+constexpr int kMxWavesLog2 = 3, kMxWaves = 1 << kMxWavesLog2;
+void plan_linear_mx(MxLaunch &p);  // from m, n and k
+hipError_t launch_linear_mx(const MxLaunch &p, hipStream_t st);
 
 }  // namespace daf

@@ -16,14 +16,22 @@ daf_status_t check_linear(int64_t M, int32_t N, int32_t K) {
   if (K <= 0 || K % kBlockValues != 0)
     return fail(DAF_ERR_UNSUPPORTED, "K=%d is not a positive multiple of %d", K, kBlockValues);
   // the grids of the kernel and of the join
-  if (M > INT32_MAX / 16 || !fits((M + 15) / 16 * (((int64_t)N + 15) / 16), 64 * kMxWaves) || M * N > UINT32_MAX / 2)
-    return fail(DAF_ERR_UNSUPPORTED, "M=%lld rows by N=%d are too many for one call", (long long)M, N);
+  if (N > INT32_MAX - 16 || K > 1 << 24 || M > INT32_MAX || M * N > UINT32_MAX / 2 ||
+      (M + 31) / 32 > 65535)
+    return fail(DAF_ERR_UNSUPPORTED, "M=%lld rows by N=%d, K=%d are too many for one call", (long long)M, N, K);
   return DAF_OK;
 }
 
-size_t linear_bytes(const MxPlan &a, int64_t M, int32_t N) {
-  return a.splits > 1 ? (size_t)a.splits * M * N * sizeof(float) : 0;
+MxLaunch planned(int64_t M, int32_t N, int32_t K) {
+  MxLaunch p{};
+  p.m = M;
+  p.n = N;
+  p.k = K;
+  plan_linear_mx(p);
+  return p;
 }
+
+size_t linear_bytes(const MxLaunch &p) { return p.splits > 1 ? (size_t)p.splits * p.m * p.n * sizeof(float) : 0; }
 
 }  // namespace
 
@@ -57,7 +65,7 @@ daf_status_t daf_add_rmsnorm(int32_t dtype, int64_t rows, int32_t width, const v
 
 size_t daf_linear_mx_workspace_size(int64_t M, int32_t N, int32_t K) {
   if (check_linear(M, N, K) != DAF_OK || M == 0) return 0;
-  return linear_bytes(plan_linear_mx(M, N, K), M, N);
+  return linear_bytes(planned(M, N, K));
 }
 
 daf_status_t daf_linear_mx(int64_t M, int32_t N, int32_t K, const void *A, const uint8_t *a_scales, const void *W,
@@ -71,16 +79,22 @@ daf_status_t daf_linear_mx(int64_t M, int32_t N, int32_t K, const void *A, const
   CHECK(aligned(bias, "bias"));
   CHECK(aligned(residual, "residual"));
   CHECK(need_ptr(C, "C"));
-  const MxPlan plan = plan_linear_mx(M, N, K);
-  const size_t need = linear_bytes(plan, M, N);
+  MxLaunch p = planned(M, N, K);
+  const size_t need = linear_bytes(p);
   if (need > 0) {
     if (!workspace || ws_bytes < need)
       return fail(DAF_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace ? ws_bytes : 0);
     CHECK(aligned(workspace, "workspace"));
   }
-  const MxLaunch p{static_cast<const unsigned char *>(A), a_scales, static_cast<const unsigned char *>(W), w_scales,
-                   bias, residual, C, static_cast<float *>(workspace), M, N, K, plan.splits};
-  return launched(launch_linear_mx(plan, p, stream), "linear_mx launch");
+  p.a = static_cast<const unsigned char *>(A);
+  p.a_scales = a_scales;
+  p.w = static_cast<const unsigned char *>(W);
+  p.w_scales = w_scales;
+  p.bias = bias;
+  p.residual = residual;
+  p.c = C;
+  p.part = static_cast<float *>(workspace);
+  return launched(launch_linear_mx(p, stream), "linear_mx launch");
 }
 
 }  // extern "C"
