@@ -352,15 +352,25 @@ __global__ __launch_bounds__(64 * kMxWaves, 2) void linear_mx_kernel(const MxLau
   wait_copies<0>();  // none may arrive after the workgroup's end
 }
 
-// The sum of the splits, in their order.
+// The sum of the splits, in their order: VEC features of a row per thread.
+template <int VEC>
 __global__ __launch_bounds__(256) void linear_mx_join_kernel(const MxLaunch p) {
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, total = p.m * p.n;
-  if (at >= total) return;
-  float x = p.part[at];
-  for (int s = 1; s < p.splits; ++s) x += p.part[s * total + at];
-  if (p.bias) x += (float)static_cast<const __bf16 *>(p.bias)[at % p.n];
-  if (p.residual) x += (float)static_cast<const __bf16 *>(p.residual)[at];
-  static_cast<__bf16 *>(p.c)[at] = (__bf16)x;
+  typedef float fv __attribute__((ext_vector_type(VEC)));
+  typedef __bf16 bv __attribute__((ext_vector_type(VEC)));
+  const int n = (blockIdx.y * 256 + threadIdx.x) * VEC;
+  if (n >= p.n) return;
+  const size_t at = (size_t)blockIdx.x * p.n + n, total = (size_t)p.m * p.n;
+  fv x = *reinterpret_cast<const fv *>(p.part + at);
+  for (int s = 1; s < p.splits; ++s) x += *reinterpret_cast<const fv *>(p.part + s * total + at);
+  auto add = [&](const void *rows, size_t from) {
+    const bv v = *reinterpret_cast<const bv *>(static_cast<const __bf16 *>(rows) + from);
+    for (int i = 0; i < VEC; ++i) x[i] += (float)v[i];
+  };
+  if (p.bias) add(p.bias, n);
+  if (p.residual) add(p.residual, at);
+  bv y;
+  for (int i = 0; i < VEC; ++i) y[i] = (__bf16)x[i];
+  *reinterpret_cast<bv *>(static_cast<__bf16 *>(p.c) + at) = y;
 }
 
 template <bool MX>
@@ -394,7 +404,10 @@ hipError_t launch_linear_mx(const MxLaunch &p, hipStream_t st) {
   p.a_scales ? launch<true>(p, st) : launch<false>(p, st);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
-  linear_mx_join_kernel<<<(unsigned)((p.m * p.n + 255) / 256), 256, 0, st>>>(p);
+  const int vec = p.n % 4 == 0 ? 4 : 1;
+  const dim3 grid((unsigned)p.m, (p.n + 256 * vec - 1) / (256 * vec));
+  if (vec == 4) linear_mx_join_kernel<4><<<grid, 256, 0, st>>>(p);
+  else linear_mx_join_kernel<1><<<grid, 256, 0, st>>>(p);
   return hipGetLastError();
 }
 

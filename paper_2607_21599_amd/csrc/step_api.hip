@@ -15,9 +15,8 @@ daf_status_t check_linear(int64_t M, int32_t N, int32_t K) {
   if (N <= 0) return fail(DAF_ERR_INVALID_ARG, "N=%d must be positive", N);
   if (K <= 0 || K % kBlockValues != 0)
     return fail(DAF_ERR_UNSUPPORTED, "K=%d is not a positive multiple of %d", K, kBlockValues);
-  // the grids of the kernel and of the join
-  if (N > INT32_MAX - 16 || K > 1 << 24 || M > INT32_MAX || M * N > UINT32_MAX / 2 ||
-      (M + 31) / 32 > 65535)
+  // the grids of the kernel and of the join, and offsets in a tile
+  if (M > 32 * 65535 || N > 256 * 65535 || K > 1 << 24 || !fits(M * ((N + 255) / 256), 256))
     return fail(DAF_ERR_UNSUPPORTED, "M=%lld rows by N=%d, K=%d are too many for one call", (long long)M, N, K);
   return DAF_OK;
 }
