@@ -86,6 +86,7 @@ struct CacheAttnLaunch {
   int32_t cu[kMaxCacheReqs + 1];
   int32_t blk0[kMaxCacheReqs + 1];
   // few rows' line: all pages of a request for each of its row blocks
+  __device__ __forceinline__ int row_of(int b) const { return cu[b]; }
   __device__ __forceinline__ int line_blocks(int b) const { return blk0[b + 1] - blk0[b]; }
   __device__ __forceinline__ int line_pages(int, int L) const { return max(1, (L + kPage - 1) / kPage); }
   __device__ __forceinline__ int line_page(int, int i) const { return i; }
@@ -111,6 +112,7 @@ hipError_t launch_cache_attn(bool bf16, const CacheAttnLaunch &p, hipStream_t st
 
 // Attention of groups of requests whose first pages are the same (cache_shared.hip).
 constexpr int kSharedMaxGroups = kMaxCacheReqs;
+constexpr int kMinSharedPages = 2;  // of a split of a group's pages
 struct SharedLaunch {
   CacheView c;
   const int32_t *seq, *pos;
@@ -138,14 +140,20 @@ struct SharedLaunch {
   int32_t pages[kMaxCacheReqs];           // of each request that are its group's
   int32_t wg0[kSharedMaxGroups + 1];      // first workgroup of each group
   unsigned char first[kSharedMaxGroups];  // first request of each group
+  // Most calls have as many rows of every request, or one group: what follows is then known
+  // without a load (0 and -1: it is not).
+  int32_t per_req;     // rows of every request
+  int32_t all_pages;   // of every request that are its group's
+  __device__ __forceinline__ int row_of(int b) const { return per_req ? b * per_req : cu[b]; }
+  __device__ __forceinline__ int first_page(int b) const { return all_pages >= 0 ? all_pages : pages[b]; }
   __device__ __forceinline__ int line_blocks(int b) const {
-    return ((cu[b + 1] - cu[b]) * group + kCacheAttnRows - 1) / kCacheAttnRows;
+    return ((row_of(b + 1) - row_of(b)) * group + kCacheAttnRows - 1) / kCacheAttnRows;
   }
   __device__ __forceinline__ int line_pages(int b, int L) const {
-    return whole ? 1 : max(1, (L + kPage - 1) / kPage - pages[b]);
+    return whole ? 1 : max(1, (L + kPage - 1) / kPage - first_page(b));
   }
   __device__ __forceinline__ int line_page(int b, int i) const {
-    return whole && i > 0 ? INT32_MAX : pages[b] + i;  // the end of a whole line: the sequence's
+    return whole && i > 0 ? INT32_MAX : first_page(b) + i;  // the end of a whole line: the sequence's
   }
   __device__ __forceinline__ int least_piece() const;
   __device__ __forceinline__ int whole_pair(int h) const { return first_wgs * block_rows + h * rows * group; }

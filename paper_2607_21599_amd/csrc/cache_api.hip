@@ -390,6 +390,12 @@ int64_t plan_shared(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_c
     for (int b = lo; b < hi; ++b) p.pages[b - b0] = pages;
     if (pages > 0) most = std::max(most, (int64_t)(rows->cu[hi] - rows->cu[lo]) * p.group);
   }
+  p.per_req = p.cu[1];
+  p.all_pages = p.pages[0];
+  for (int b = 0; b < p.n_req; ++b) {
+    if (p.cu[b + 1] - p.cu[b] != p.per_req) p.per_req = 0;
+    if (p.pages[b] != p.all_pages) p.all_pages = -1;
+  }
   const bool bf16 = cfg->dtype == DAF_BF16;
   p.block_rows = bf16 && most > kCacheWideRowsF32 ? kCacheWideRows : kCacheWideRowsF32;
 
@@ -436,9 +442,28 @@ int64_t plan_shared(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_c
     }
     return lo;
   };
-  const int64_t target = std::max<int64_t>(256, 512 - n_splits * c->n_kv_heads);
-  p.split_pages = least_split(std::min(kMinSplitPages, longest), target);
-  if (workgroups(p.split_pages) > target || p.split_pages > 64) p.split_pages = least_split(std::min(64, longest), 4096);
+  // Of splits that give up to 1, 2, .. 16 workgroups per CU the ones that take least, in us of
+  // bf16 and 128 features: 1.5 a page for a workgroup alone on its CU, 1.25 a page and
+  // workgroup for more, 0.2 ns a (row, head) and partial result written and read again, 1 for
+  // each 32 that a join reads one after the other. (32 decode rows over 512 pages, us a call:
+  // 256 workgroups 37.8, 376 43.5, 448 40.6, 512 46.8; 301 question rows: 476 217, 612 197, 748 174,
+  // 816 197, 1020 174; 80: 240 68.7, 380 69.8, 500 61.4, 620 72.5.) At least 2 pages, for short
+  // prefixes: 4 beams of 12 pages 11.5, in splits of 4 13.2, of 6 14.7.
+  // fp32 and blocks of 64 pairs take other times, here by their matrix instructions; fp32 of
+  // 128 features has one workgroup per CU.
+  const double unit = cfg->head_dim / 128. * (!bf16 ? 1.5 : p.block_rows == kCacheWideRows ? 1. : 0.7);
+  const bool alone = !bf16 && cfg->head_dim == 128;
+  double best = INFINITY;
+  for (int r = 1; r <= 16; ++r) {
+    const int sp = least_split(std::min(kMinSharedPages, longest), 256 * r);
+    const int64_t wgs = workgroups(sp), per_cu = (wgs + 255) / 256, splits = (longest + sp - 1) / sp;
+    const double page = alone ? 1.5 * (double)per_cu : per_cu <= 1 ? 1.5 : 1.25 * (double)per_cu;
+    const double us = sp * page * unit + 2e-4 * cfg->head_dim / 128 * (double)splits * p.rows * p.hq + (double)((splits + 31) / 32);
+    if (us < best) {
+      best = us;
+      p.split_pages = sp;
+    }
+  }
   int64_t wg = 0;
   for (int i = 0; i < p.n_groups; ++i) {
     p.wg0[i] = (int)wg;
@@ -514,7 +539,7 @@ daf_status_t attn_shared(const daf_attn_cfg_t *cfg, const daf_cache_t *c, int32_
     char *ws = static_cast<char *>(workspace);
     const size_t lse_bytes = shared_lse_bytes(pairs);
     p.part_lse = reinterpret_cast<float *>(ws);
-    p.line = reinterpret_cast<int32_t *>(ws + lse_bytes - kLineBytes);
+    p.line = p.whole ? nullptr : reinterpret_cast<int32_t *>(ws + lse_bytes - kLineBytes);
     p.part_o = reinterpret_cast<float *>(ws + lse_bytes);
     p.scale_log2 = scale * 1.4426950408889634f;
     const hipError_t e = launch_cache_shared(bf16, p, stream);

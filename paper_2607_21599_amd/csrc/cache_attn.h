@@ -422,7 +422,7 @@ template <bool BF16, int D, typename P>
 __device__ __forceinline__ void line_job(const P &p, FewShared<D> &sh, int h, int k) {
   const int lane = threadIdx.x & 63;
   const Line line = build_line(p);
-  if (h == 0 && k == 0 && threadIdx.x < 64) {  // for the join
+  if (h == 0 && k == 0 && threadIdx.x < 64 && p.line) {  // for the join
     int first = line.first;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -454,8 +454,8 @@ __device__ __forceinline__ void line_job(const P &p, FewShared<D> &sh, int h, in
     r.L = L;
     const int pages = p.line_pages(r.b, L), rest = at - first;
     r.block = rest / pages;
-    r.row0 = p.cu[r.b];
-    r.n = p.cu[r.b + 1] - r.row0;
+    r.row0 = p.row_of(r.b);
+    r.n = p.row_of(r.b + 1) - r.row0;
     r.pages = p.c.table + (int64_t)((unsigned)seq < (unsigned)p.c.n_seqs ? seq : 0) * p.c.max_seq_pages;
     const int pg0 = rest - r.block * pages, pg_end = min(pages, pg0 + to - at);
     const int place = pg0 == 0 && pg_end == pages ? p.whole_place(r, h) : p.edge_place(h, k, pg0 == 0);
@@ -737,23 +737,31 @@ __device__ __forceinline__ bool wide_rows(const P &p, unsigned char *lds, const 
     if (n > 0) fetch(0);
     if (n > 1) fetch(1);
   };
-  if constexpr (Rows::kKnown) {  // the pages are known: their copies go out before the rows' limits are
+  w.scale_log2 = p.scale_log2;
+  w.lane = lane;
+  int lim_hi = INT32_MIN, lim_lo = INT32_MAX;
+  auto row_at = [&](int mt) {  // past the end: the last pair
+    return min((r.block * kWaves + wave) * 16 * MT + mt * 16 + n16, total - 1);
+  };
+  auto load_rows = [&](int mt) {
+    const int idx = row_at(mt), row = idx / p.group, head = h * p.group + idx % p.group;
+    const size_t q_at = ((size_t)(r.row0 + row) * p.hq + head) * D;
+    load_q<BF16, D>(p, q_at, quad, [&](int j, int ds, const bf16x8 &x) { w.q[j][mt][ds] = x; });
+  };
+  if constexpr (Rows::kKnown) {
+    // the pages are known: their copies go out before the rows' limits are, and q before them
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) load_rows(mt);
     settle(0);
     begin();
     rows.prepare();
   }
-  w.scale_log2 = p.scale_log2;
-  w.lane = lane;
-  int lim_hi = INT32_MIN, lim_lo = INT32_MAX;
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
-    const int idx = min((r.block * kWaves + wave) * 16 * MT + mt * 16 + n16, total - 1);  // past the end: the last pair
-    const int row = idx / p.group, head = h * p.group + idx % p.group;
-    w.limit[mt] = rows.limit(row);
+    w.limit[mt] = rows.limit(row_at(mt) / p.group);
     lim_hi = max(lim_hi, w.limit[mt]);
     lim_lo = min(lim_lo, w.limit[mt]);
-    const size_t q_at = ((size_t)(r.row0 + row) * p.hq + head) * D;
-    load_q<BF16, D>(p, q_at, quad, [&](int j, int ds, const bf16x8 &x) { w.q[j][mt][ds] = x; });
+    if constexpr (!Rows::kKnown) load_rows(mt);
     w.m[mt] = kNoReference;
     w.top[mt] = kNoReference / p.scale_log2;
     w.l[mt] = 0.f;

@@ -9,6 +9,8 @@
 //  * of the rest: the line of daf_cache_attn's few rows, from the first page that is not
 //    the group's on.
 // A second launch joins a row's partial results.
+#include <algorithm>
+
 #include "cache_attn.h"
 
 namespace daf {
@@ -20,29 +22,65 @@ template <int MT>
 struct GroupRows {
   static constexpr bool kKnown = true;
   const SharedLaunch &p;
-  int b0, n_req;   // the group's requests
-  int row0;        // its first row
-  int pages;       // its pages
-  int *cu, *len;   // LDS: of its requests, first rows from row0 on and tokens
-  __device__ __forceinline__ bool empty() const { return false; }
-  __device__ __forceinline__ int seen() const { return pages; }
-  __device__ __forceinline__ void prepare() {
-    for (int i = threadIdx.x; i < n_req; i += kThreads) {
-      const int seq = p.seq ? p.seq[b0 + i] : b0 + i;
-      cu[i] = p.cu[b0 + i] - row0;
-      len[i] = min(seq_len(p.c.len, p.c.n_seqs, p.c.max_seq_pages, seq), p.max_len);
+  int b0, n_req;  // the group's requests
+  int row0;       // its first row
+  int pages;      // its pages
+  int *cu, *len;  // LDS, for requests of different rows: first rows from row0 on and tokens
+  int mine[4];    // else tokens of its requests: of lane, 64 + lane, ..; or of thread
+  __device__ __forceinline__ int tokens(int i) const {
+    const int seq = p.seq ? p.seq[b0 + i] : b0 + i;
+    return min(seq_len(p.c.len, p.c.n_seqs, p.c.max_seq_pages, seq), p.max_len);
+  }
+  // loads, and what waits for them
+  __device__ __forceinline__ void start() {
+    if (!p.per_req) {
+      mine[0] = (int)threadIdx.x < n_req ? tokens(threadIdx.x) : 0;
+      return;
     }
-    if (threadIdx.x == 0) cu[n_req] = p.cu[b0 + n_req] - row0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j * 64 < n_req) mine[j] = tokens(min(j * 64 + (int)(threadIdx.x & 63), n_req - 1));
+  }
+  __device__ __forceinline__ void prepare() {
+    if (p.per_req) return;
+    const int i = threadIdx.x;
+    if (i < n_req) cu[i] = p.cu[b0 + i] - row0, len[i] = mine[0];
+    if (i == 0) cu[n_req] = p.cu[b0 + n_req] - row0;
     __syncthreads();
   }
+  __device__ __forceinline__ bool empty() const { return false; }
+  __device__ __forceinline__ int seen() const { return pages; }
   __device__ __forceinline__ int limit(int row) const {
-    int b = 0;
-    for (int step = kMaxCacheReqs / 2; step; step >>= 1)
-      if (b + step < n_req && cu[b + step] <= row) b += step;
-    const int L = len[b], at = p.pos ? min(p.pos[row0 + row], L - 1) : L - cu[b + 1] + row;
+    int L, next;  // tokens of the row's sequence, and the row after its request's last
+    if (p.per_req) {
+      const int b = row / p.per_req;
+      next = (b + 1) * p.per_req;
+      L = __shfl(mine[0], b & 63);
+#pragma unroll
+      for (int j = 1; j < 4; ++j)
+        if (j * 64 < n_req) {
+          const int y = __shfl(mine[j], b & 63);
+          L = b >> 6 == j ? y : L;
+        }
+    } else {
+      int b = 0;
+      for (int step = kMaxCacheReqs / 2; step; step >>= 1)
+        if (b + step < n_req && cu[b + step] <= row) b += step;
+      L = len[b];
+      next = cu[b + 1];
+    }
+    const int at = p.pos ? min(p.pos[row0 + row], L - 1) : L - next + row;
     return max(-1, min(at, pages * kPage - 1));
   }
 };
+
+// The group of a workgroup or request, and its requests
+struct Group {
+  int g, b0, b1;
+};
+__device__ __forceinline__ Group group_at(const SharedLaunch &p, int g) {
+  return {g, p.first[g], g + 1 < p.n_groups ? p.first[g + 1] : p.n_req};
+}
 
 // The workgroups of a group's units, (split, head) pairs, and of their row blocks. The row
 // blocks of a unit read the same pages: neighbours on one XCD, the units on the XCDs in
@@ -76,22 +114,22 @@ __device__ __forceinline__ void group_job(const SharedLaunch &p, SharedMemory<BF
   constexpr int PAIRS = kWaves * 16 * MT;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n16 = lane & 15, quad = lane >> 4;
-  const int g = find_in(p.wg0, p.n_groups, blockIdx.x);
-  const int b0 = p.first[g], b1 = g + 1 < p.n_groups ? p.first[g + 1] : p.n_req;
+  const Group gr = p.n_groups == 1 ? Group{0, 0, p.n_req} : group_at(p, find_in(p.wg0, p.n_groups, blockIdx.x));
   Request r;
-  r.b = b0;
-  r.row0 = p.cu[b0];
-  r.n = p.cu[b1] - r.row0;
+  r.b = gr.b0;
+  r.row0 = p.row_of(gr.b0);
+  r.n = p.row_of(gr.b1) - r.row0;
   r.L = 0;  // not used
-  const int total = r.n * p.group, blocks = (total + PAIRS - 1) / PAIRS, pages = p.pages[b0];
-  const UnitBlock ub = unit_block(blockIdx.x - p.wg0[g], (pages + p.split_pages - 1) / p.split_pages * p.c.hkv, blocks);
+  const int total = r.n * p.group, blocks = (total + PAIRS - 1) / PAIRS, pages = p.first_page(gr.b0);
+  const UnitBlock ub = unit_block(blockIdx.x - (p.n_groups == 1 ? 0 : p.wg0[gr.g]), (pages + p.split_pages - 1) / p.split_pages * p.c.hkv, blocks);
   const int h = ub.unit % p.c.hkv, pg0 = ub.unit / p.c.hkv * p.split_pages;
   r.block = ub.block;
   // the pages are those of the group's first sequence
-  const int seq = p.seq ? p.seq[b0] : b0;
+  const int seq = p.seq ? p.seq[gr.b0] : gr.b0;
   const bool there = (unsigned)seq < (unsigned)p.c.n_seqs;
   r.pages = p.c.table + (int64_t)(there ? seq : 0) * p.c.max_seq_pages;
-  GroupRows<MT> rows{p, b0, b1 - b0, r.row0, there ? pages : 0, sh.wide.cu, sh.wide.len};
+  GroupRows<MT> rows{p, gr.b0, gr.b1 - gr.b0, r.row0, there ? pages : 0, sh.wide.cu, sh.wide.len, {}};
+  rows.start();
   W w;
   float unit;
   wide_rows<BF16, D, MT>(p, sh.wide.lds, r, h, pg0, min(p.split_pages, pages - pg0), rows, w, unit);
@@ -119,32 +157,50 @@ __global__ __launch_bounds__(kThreads, (BF16 || D == 64 ? 2 : 1)) void cache_sha
 }
 
 // Join a (row, head)'s partial results, o = sum_s e^(lse_s - lse) o_s: those of its group's
-// pages, then those of the line. Groups of D / 4 lanes take them in turn, four in flight,
-// and join their sums through LDS.
-template <bool BF16, int D>
+// pages, then those of the line. A workgroup's groups of D / 4 lanes take a pair each, or
+// TEAM of them one: its results in turn, FLIGHT at a time, their sums joined through LDS.
+template <bool BF16, int D, int TEAM>
 __global__ __launch_bounds__(kThreads) void cache_shared_join_kernel(const SharedLaunch p) {
-  constexpr int LP = D / 4, GROUPS = kThreads / LP;
+  constexpr int LP = D / 4, GROUPS = kThreads / LP, FLIGHT = 4;
   __shared__ f32x4 sh_o[GROUPS][LP];
   __shared__ float sh_m[GROUPS], sh_l[GROUPS];
-  const int t = threadIdx.x, g = t / LP, c = t % LP, lane = t & 63;
-  const int row = blockIdx.x / p.hq, head = blockIdx.x % p.hq;
-  const int piece = p.line[2 * kMaxCacheReqs];
-  const int b = find_in(p.cu, p.n_req, row);
-  int grp = -1;
-  for (int i = 0; i < p.n_groups; i += 64) grp += __builtin_popcountll(__ballot(i + lane < p.n_groups && p.first[i + lane] <= b));
+  const int t = threadIdx.x, lanes = t / LP, g = lanes % TEAM, c = t % LP, lane = t & 63;
+  const int64_t job = (int64_t)blockIdx.x * (GROUPS / TEAM) + lanes / TEAM;
+  const bool mine = job < (int64_t)p.rows * p.hq;
+  const int row = mine ? (int)(job / p.hq) : p.rows - 1, head = mine ? (int)(job % p.hq) : 0;
+  // the wave's pairs one after the other: searches by all lanes
+  int b = p.per_req ? row / p.per_req : 0;
+  Group gr{0, 0, p.n_req};
+  if (!p.per_req || p.n_groups > 1) {
+#pragma unroll
+    for (int k = 0; k < 64; k += TEAM == GROUPS ? 64 : LP) {
+      const int r = __builtin_amdgcn_readlane(row, k), at = p.per_req ? r / p.per_req : find_in(p.cu, p.n_req, r);
+      int g = p.n_groups > 1 ? -1 : 0;
+      if (p.n_groups > 1)
+        for (int i = 0; i < p.n_groups; i += 64)
+          g += __builtin_popcountll(__ballot(i + lane < p.n_groups && p.first[i + lane] <= at));
+      if (TEAM == GROUPS || lane / LP == k / LP) b = at, gr.g = g;
+    }
+    gr = group_at(p, gr.g);
+  }
   const int h = head / p.group, in_head = head % p.group;
   // the line: piece s of n_line, the first one's place is its workgroup's second
-  const int pair = (row - p.cu[b]) * p.group + in_head;
-  const int units = p.line[kMaxCacheReqs + b], from = p.line[b] + pair / kRows * units;
-  const int k0 = from / piece, k1 = (from + units - 1) / piece, n_line = k1 - k0 + 1;
+  const int pair = (row - p.row_of(b)) * p.group + in_head;
+  int k0 = 0, n_line = 1;
+  if (!p.whole) {
+    const int piece = p.line[2 * kMaxCacheReqs], units = p.line[kMaxCacheReqs + b];
+    const int from = p.line[b] + pair / kRows * units;
+    k0 = from / piece;
+    n_line = (from + units - 1) / piece - k0 + 1;
+  }
   // the group's pages
-  const int b0 = p.first[grp], b1 = grp + 1 < p.n_groups ? p.first[grp + 1] : p.n_req;
-  const int in_group = (row - p.cu[b0]) * p.group + in_head;
-  const int blocks = ((p.cu[b1] - p.cu[b0]) * p.group + p.block_rows - 1) / p.block_rows;
-  const int n_first = (p.pages[b0] + p.split_pages - 1) / p.split_pages, n = n_first + n_line;
+  const int row0 = p.row_of(gr.b0), wg0 = p.n_groups == 1 ? 0 : p.wg0[gr.g];
+  const int in_group = (row - row0) * p.group + in_head;
+  const int blocks = ((p.row_of(gr.b1) - row0) * p.group + p.block_rows - 1) / p.block_rows;
+  const int n_first = (p.first_page(gr.b0) + p.split_pages - 1) / p.split_pages, n = n_first + n_line;
   auto at = [&](int s) {
     if (s < n_first) {
-      const int wg = p.wg0[grp] + workgroup_of({s * p.c.hkv + h, in_group / p.block_rows}, n_first * p.c.hkv, blocks);
+      const int wg = wg0 + workgroup_of({s * p.c.hkv + h, in_group / p.block_rows}, n_first * p.c.hkv, blocks);
       return wg * p.block_rows + in_group % p.block_rows;
     }
     s -= n_first;
@@ -152,54 +208,77 @@ __global__ __launch_bounds__(kThreads) void cache_shared_join_kernel(const Share
   };
   float m = -INFINITY, l = 0.f;
   f32x4 x = {};
-  for (int s0 = g; s0 < n; s0 += 4 * GROUPS) {
-    float lse[4];
-    f32x4 y[4];
+  for (int s0 = g; s0 < n; s0 += FLIGHT * TEAM) {
+    float lse[FLIGHT];
+    f32x4 y[FLIGHT];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int s = s0 + j * GROUPS;
-      const size_t place = s < n ? at(s) : 0;
+    for (int j = 0; j < FLIGHT; ++j) {
+      const int s = s0 + j * TEAM;
+      const size_t place = at(min(s, n - 1));
       lse[j] = s < n ? p.part_lse[place] : -INFINITY;
       y[j] = s < n ? *reinterpret_cast<const f32x4 *>(p.part_o + place * D + c * 4) : f32x4{};
     }
-    const float to = fmaxf(m, fmaxf(fmaxf(lse[0], lse[1]), fmaxf(lse[2], lse[3])));
+    float to = m;
+#pragma unroll
+    for (int j = 0; j < FLIGHT; ++j) to = fmaxf(to, lse[j]);
     const float ref = to == -INFINITY ? 0.f : to;  // a row that sees no key there, or NaN
     const float a = __expf(m - ref);
     m = to;
     l *= a;
     x *= a;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < FLIGHT; ++j) {
       const float w = __expf(lse[j] - ref);
       l += w;
       x += w * y[j];
     }
   }
-  sh_o[g][c] = x;
-  if (c == 0) sh_m[g] = m, sh_l[g] = l;
-  __syncthreads();
-  if (g) return;
-  for (int k = 1; k < GROUPS; ++k) m = fmaxf(m, sh_m[k]);
-  const float ref = m == -INFINITY ? 0.f : m;
-  l = 0.f;
-  x = f32x4{};
-  for (int k = 0; k < GROUPS; ++k) {
-    const float w = __expf(sh_m[k] - ref);
-    l += w * sh_l[k];
-    x += w * sh_o[k][c];
+  if constexpr (TEAM > 1) {
+    sh_o[lanes][c] = x;
+    if (c == 0) sh_m[lanes] = m, sh_l[lanes] = l;
+    __syncthreads();
+    if (g) return;
+    for (int k = 1; k < TEAM; ++k) m = fmaxf(m, sh_m[lanes + k]);
+    const float ref = m == -INFINITY ? 0.f : m;
+    l = 0.f;
+    x = f32x4{};
+    for (int k = 0; k < TEAM; ++k) {
+      const float w = __expf(sh_m[lanes + k] - ref);
+      l += w * sh_l[lanes + k];
+      x += w * sh_o[lanes + k][c];
+    }
   }
+  if (!mine) return;
   const float inv = over(l);
   const float y[4] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
   store_out<BF16>(p, row, head, c * 4, y, D);
   if (c == 0 && p.lse) p.lse[(size_t)head * p.lse_stride + row] = l == 0.f ? -INFINITY : m + __logf(l);
 }
 
+// A join of few pairs gives each a workgroup; one of many, which fill the device by
+// themselves, helps a group of lanes where it would have more than 8 results to take (301
+// question rows of 28 heads of 128, 12 results each, us of the join: teams of 2 13.9, of 8 19.0;
+// 4 rows, 7 each: of 1 4.5, of 8 4.0).
+constexpr int kJoinTurns = 8, kJoinPairs = 4096;
+
 template <bool BF16, int D, int MT>
 hipError_t launch(const SharedLaunch &p, hipStream_t st) {
   cache_shared_kernel<BF16, D, MT><<<p.first_wgs + p.n_splits * p.c.hkv, kThreads, 0, st>>>(p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  cache_shared_join_kernel<BF16, D><<<p.rows * p.hq, kThreads, 0, st>>>(p);
+  int most = 1;  // partial results of a row
+  for (int g = 0; g < p.n_groups; ++g) most = std::max(most, (p.pages[p.first[g]] + p.split_pages - 1) / p.split_pages + 1);
+  if (!p.whole) most += p.n_splits / 4;  // of the line's workgroups few have a part of one row
+  const int64_t pairs = (int64_t)p.rows * p.hq;
+  auto join = [&](auto kern, int team) {
+    const int per_wg = kThreads / (D / 4) / team;
+    kern<<<(unsigned)((pairs + per_wg - 1) / per_wg), kThreads, 0, st>>>(p);
+  };
+  constexpr int ALL = kThreads / (D / 4);
+  if (pairs < kJoinPairs || most > 4 * kJoinTurns) join(cache_shared_join_kernel<BF16, D, ALL>, ALL);
+  else if (most > 2 * kJoinTurns) join(cache_shared_join_kernel<BF16, D, 4>, 4);
+  else if (most > kJoinTurns) join(cache_shared_join_kernel<BF16, D, 2>, 2);
+  else join(cache_shared_join_kernel<BF16, D, 1>, 1);
   return hipGetLastError();
 }
 
