@@ -50,6 +50,7 @@ struct RopeLaunch {
   void *q_out;
   int64_t q_pitch, kv_pitch;  // bytes from row to row of q, and of k and v
   int32_t hq;
+  int32_t per_req;  // rows of every request where they are equal, else 0
   double turn[64];  // of pair i of a head's features, per position: theta^(-2i/D) / (2 pi)
 };
 static_assert(sizeof(StoreLaunch) + sizeof(RopeLaunch) < 4096, "kernel arguments must fit 4 KiB");

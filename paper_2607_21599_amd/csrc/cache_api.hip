@@ -161,6 +161,9 @@ daf_status_t store(bool write, const daf_attn_cfg_t *cfg, const daf_cache_t *c, 
       p.v = rows_at(v, row0, row_bytes);
       if (rope) {
         RopeLaunch r = *rope;
+        r.per_req = p.cu[1];
+        for (int b = 1; b < p.n_req; ++b)
+          if (p.cu[b + 1] - p.cu[b] != r.per_req) r.per_req = 0;
         r.q = rows_at(rope->q, row0, rope->q_pitch);
         r.q_out = const_cast<char *>(rows_at(rope->q_out, row0, (size_t)cfg->n_q_heads * c->head_dim * (bf16 ? 2 : 4)));
         const hipError_t e = launch_cache_rope_store(bf16, p, r, stream);

@@ -175,26 +175,39 @@ __device__ __forceinline__ void put(const X &x, Old &old, unsigned char *codes, 
 
 // ---- the rotary embedding -----------------------------------------------------------
 // Features i and i + D/2 of a head turn by the angle pos * theta^(-2i/D). The angle is taken
-// in turns (2 pi), in fp64, where the whole turns of far positions fall away exactly;
-// what is left, within an eighth of a turn of a multiple of a quarter, goes into the Taylor
-// series of sine and cosine up to x^15 and x^14 (off by less than 2^-44), also in fp64:
-// the values are those of fp32, rounded once.
+// in turns (2 pi), in fp64, where the whole and quarter turns of far positions fall away
+// exactly; what is left, at most an eighth of a turn, goes in fp32 into the Taylor series of
+// sine and cosine up to x^9 and x^10 (the next terms are below 2^-25): off by less than
+// 1.5 2^-24. (All of it in fp64, rounded once: 3 us more for 16384 rows of 4 heads.)
 __device__ __forceinline__ void sine_cosine(double turns, float &sine, float &cosine) {
   const double r = turns - rint(turns), q = rint(4 * r);
-  const double x = (r - 0.25 * q) * 6.283185307179586476925, y = x * x;
-  auto f = [&](double next, double den) { return 1 - y * next * (1 / den); };
-  const double s = x * f(f(f(f(f(f(f(1, 14. * 15), 12. * 13), 10. * 11), 8. * 9), 6. * 7), 4. * 5), 2. * 3);
-  const double c = f(f(f(f(f(f(f(1, 13. * 14), 11. * 12), 9. * 10), 7. * 8), 5. * 6), 3. * 4), 1. * 2);
+  const float x = (float)((r - 0.25 * q) * 6.283185307179586476925), y = x * x;
+  auto next = [&](float a, float b) { return __builtin_fmaf(a, y, b); };
+  const float s = __builtin_fmaf(x * y, next(next(next(1.f / 362880, -1.f / 5040), 1.f / 120), -1.f / 6), x);
+  const float c = next(next(next(next(next(-1.f / 3628800, 1.f / 40320), -1.f / 720), 1.f / 24), -0.5f), 1.f);
   const int k = (int)q & 3;  // quarters of a turn
-  const float a = (float)(k & 1 ? c : s), b = (float)(k & 1 ? s : c);
+  const float a = k & 1 ? c : s, b = k & 1 ? s : c;
   sine = k & 2 ? -a : a;
   cosine = k == 1 || k == 2 ? -b : b;
 }
 
-// Sines and cosines of a page's slots (or of some rows), [slot][pair of features]
+// The place of the n-th set bit, from 0, of which there are more than n.
+__device__ __forceinline__ int nth_bit(unsigned long long m, int n) {
+  int at = 0;
+#pragma unroll
+  for (int w = 32; w; w >>= 1) {
+    const int below = __builtin_popcountll((m >> at) & ((1ull << w) - 1));
+    if (n >= below) n -= below, at += w;
+  }
+  return at;
+}
+
+// Sines and cosines of as many slots as a pass over a page has, or of rows of q: [slot][pair
+// of features]
 template <int D>
 struct Angles {
-  float cosine[kPage][D / 2], sine[kPage][D / 2];
+  static constexpr int SLOTS = kThreads / (D / 8);
+  float cosine[SLOTS][D / 2], sine[SLOTS][D / 2];
 };
 
 // K (IS_V false) or V of one page of one head: the rows in sh.row (set, and a
@@ -244,24 +257,51 @@ __device__ __forceinline__ void do_page(const StoreLaunch &p, Shared &sh, const 
     if (!go) return;  // uniform in the workgroup
     unsigned x[PASSES][X::words(N)];
     if constexpr (TURN) {
-      constexpr int HALF = D / 2;
-      const double turn = rope->turn[t % HALF];
+      // Angles are made by all threads, whatever rows there are: of few rows all at once, in
+      // the order of their slots, else a pass at a time, into a place that the pass before
+      // does not read.
+      constexpr int HALF = D / 2, SLOTS = Angles<D>::SLOTS;
+      const double turn = rope->turn[t % HALF], base = pg * (double)kPage;
+      const bool high = d0 >= HALF, few = __builtin_popcountll(go) <= 2 * SLOTS;
+      auto angle = [&](int place, int s) {
+        sine_cosine((base + s) * turn, angles[place / SLOTS].sine[place % SLOTS][t % HALF],
+                    angles[place / SLOTS].cosine[place % SLOTS][t % HALF]);
+      };
+      if (few) {
+        const int n = __builtin_popcountll(go);
 #pragma unroll 1
-      for (int s = t / HALF; s < kPage; s += kThreads / HALF)
-        if ((go >> s) & 1) sine_cosine((pg * (double)kPage + s) * turn, angles->sine[s][t % HALF], angles->cosine[s][t % HALF]);
-      __syncthreads();
-      const bool high = d0 >= HALF;
+        for (int r = t / HALF; r < n; r += kThreads / HALF) angle(r, nth_bit(go, r));
+        __syncthreads();
+      }
+      int half = 0;  // of the angles' places
 #pragma unroll
       for (int i = 0; i < PASSES; ++i) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[i][j] = 0u;  // other slots
+        const unsigned rows_here = (unsigned)(go >> i * SPP) & (unsigned)((1ull << SPP) - 1);
+        if (!rows_here) continue;
+        int place;  // of this lane's slot
+        if (few) {
+          place = __builtin_popcountll(go & ((1ull << slot(i)) - 1));
+        } else {
+#pragma unroll 1
+          for (int s = t / HALF; s < SPP; s += kThreads / HALF)
+            if ((rows_here >> s) & 1) angle(half + s, i * SPP + s);
+          __syncthreads();
+          place = half + slot0;
+          half ^= SLOTS;
+        }
         unsigned other[E::words(N)];  // the half of the pairs that is another lane's
 #pragma unroll
         for (int j = 0; j < E::words(N); ++j) other[j] = __shfl_xor((int)given[i][j], CH / 2);
-        const float *c = &angles->cosine[slot(i)][d0 % HALF], *s = &angles->sine[slot(i)][d0 % HALF];
+        if ((mine >> i) & 1) {
+          const float *c = &angles[place / SLOTS].cosine[place % SLOTS][d0 % HALF];
+          const float *s = &angles[place / SLOTS].sine[place % SLOTS][d0 % HALF];
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-          const float b = E::template get<false>(other, j) * s[j];
-          const float y = __builtin_fmaf(E::template get<false>(given[i], j), c[j], high ? b : -b);
-          x[i][j] = (mine >> i) & 1 ? __builtin_bit_cast(unsigned, y) : 0u;  // other slots have no angles
+          for (int j = 0; j < N; ++j) {
+            const float b = E::template get<false>(other, j) * s[j];
+            x[i][j] = __builtin_bit_cast(unsigned, __builtin_fmaf(E::template get<false>(given[i], j), c[j], high ? b : -b));
+          }
         }
       }
     } else {
@@ -426,22 +466,26 @@ __global__ __launch_bounds__(kThreads) void cache_store_kernel(const StoreLaunch
 template <bool BF16, int D>
 __device__ __forceinline__ void turn_q(const StoreLaunch &p, const RopeLaunch &rope, Angles<D> &angles, int job) {
   using E = Elem<BF16>;
-  constexpr int HALF = D / 2, ROWS = kThreads / HALF, PIECES = HALF / 8, FLIGHT = 4;
+  constexpr int HALF = D / 2, ROWS = kThreads / HALF, PIECES = HALF / 8, FLIGHT = BF16 ? 4 : 2;
+  constexpr int HEADS = kThreads / PIECES;  // at once
   const int t = threadIdx.x, row0 = job * ROWS, n = min(ROWS, p.cu[p.n_req] - row0);
-  const int items = n * rope.hq * PIECES;  // a piece: 8 features of the one half and 8 of the other
-  const unsigned char *q = static_cast<const unsigned char *>(rope.q);
-  unsigned char *out = static_cast<unsigned char *>(rope.q_out);
-  auto feature = [&](int w) { return (w / PIECES % rope.hq * D + w % PIECES * 8) * E::kBytes; };  // byte in the row
-  auto row_of = [&](int w) { return w / (PIECES * rope.hq); };
+  // a thread has 8 features of the one half of a head and 8 of the other, of FLIGHT rows
+  const int piece = t % PIECES * 8;
+  const unsigned char *q = static_cast<const unsigned char *>(rope.q) + (int64_t)row0 * rope.q_pitch;
+  const int64_t out_pitch = (int64_t)rope.hq * (D * E::kBytes);
+  unsigned char *out = static_cast<unsigned char *>(rope.q_out) + row0 * out_pitch;
   unsigned a[FLIGHT][E::words(8)], b[FLIGHT][E::words(8)];
-  auto load = [&](int i, int w) {
-    const unsigned char *at = q + (int64_t)(row0 + row_of(w)) * rope.q_pitch + feature(w);
-    E::template load<8>(at, a[i]);
-    E::template load<8>(at + HALF * E::kBytes, b[i]);
-  };
+  auto load = [&](int r0, int head) {
+    if (head >= rope.hq) return;
 #pragma unroll
-  for (int i = 0; i < FLIGHT; ++i)
-    if (t + i * kThreads < items) load(i, t + i * kThreads);
+    for (int i = 0; i < FLIGHT; ++i)
+      if (r0 + i < n) {
+        const unsigned char *at = q + (r0 + i) * rope.q_pitch + (head * D + piece) * E::kBytes;
+        E::template load<8>(at, a[i]);
+        E::template load<8>(at + HALF * E::kBytes, b[i]);
+      }
+  };
+  load(0, t / PIECES);
   // the lanes of HALF have one row: its request, its position, its angles
   const int r = t / HALF, row = row0 + min(r, n - 1);
   int64_t at;
@@ -449,44 +493,53 @@ __device__ __forceinline__ void turn_q(const StoreLaunch &p, const RopeLaunch &r
     at = p.pos[row];
   } else {
     int b = 0;
-    for (int step = kMaxCacheReqs / 2; step; step >>= 1)
-      if (b + step < p.n_req && p.cu[b + step] <= row) b += step;
+    if (rope.per_req) {
+      b = row / rope.per_req;
+    } else {  // every lane looks at one request of each 64, for each of the wave's rows
+#pragma unroll
+      for (int k = 0; k < 64; k += HALF) {
+        const int at_row = __builtin_amdgcn_readlane(row, k), lane = t & 63;
+        int n_before = 0;
+        for (int i = 0; i < p.n_req; i += 64)
+          n_before += __builtin_popcountll(__ballot(i + lane < p.n_req && p.cu[i + lane + 1] <= at_row));
+        if (lane / HALF == k / HALF) b = n_before;
+      }
+    }
     const int seq = p.seq ? p.seq[b] : b;
     at = (int64_t)seq_len(p.c.len, p.c.n_seqs, p.c.max_seq_pages, seq) - p.cu[b + 1] + row;
   }
   sine_cosine((double)at * rope.turn[t % HALF], angles.sine[r][t % HALF], angles.cosine[r][t % HALF]);
   __syncthreads();
-  for (int w0 = t; w0 < items; w0 += FLIGHT * kThreads) {
+  for (int head = t / PIECES; head < rope.hq; head += HEADS)
+    for (int r0 = 0; r0 < n; r0 += FLIGHT) {
+      if (r0 > 0 || head >= HEADS) load(r0, head);
 #pragma unroll
-    for (int i = 0; i < FLIGHT; ++i) {
-      const int w = w0 + i * kThreads;
-      if (w >= items) break;
-      if (w0 != t) load(i, w);
-      const int k = row_of(w), c = w % PIECES * 8;
-      float x[8], y[8];
+      for (int i = 0; i < FLIGHT; ++i) {
+        if (r0 + i >= n) break;
+        const float *co = &angles.cosine[r0 + i][piece], *si = &angles.sine[r0 + i][piece];
+        float x[8], y[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float u = E::template get<false>(a[i], j), v = E::template get<false>(b[i], j);
-        const float co = angles.cosine[k][c + j], si = angles.sine[k][c + j];
-        x[j] = __builtin_fmaf(u, co, -(v * si));
-        y[j] = __builtin_fmaf(v, co, u * si);
-        if constexpr (BF16) x[j] = (float)(__bf16)x[j], y[j] = (float)(__bf16)y[j];
+        for (int j = 0; j < 8; ++j) {
+          const float u = E::template get<false>(a[i], j), v = E::template get<false>(b[i], j);
+          x[j] = __builtin_fmaf(u, co[j], -(v * si[j]));
+          y[j] = __builtin_fmaf(v, co[j], u * si[j]);
+          if constexpr (BF16) x[j] = (float)(__bf16)x[j], y[j] = (float)(__bf16)y[j];
+        }
+        unsigned char *to = out + (r0 + i) * out_pitch + (head * D + piece) * E::kBytes;
+        E::template store<8>(to, x);
+        E::template store<8>(to + HALF * E::kBytes, y);
       }
-      unsigned char *to = out + (int64_t)(row0 + k) * rope.hq * (D * E::kBytes) + feature(w);
-      E::template store<8>(to, x);
-      E::template store<8>(to + HALF * E::kBytes, y);
     }
-  }
 }
 
 // K and V as above, K turned on the way, then the rows of q.
 template <bool BF16, int D>
-__global__ __launch_bounds__(kThreads) void cache_rope_store_kernel(const StoreLaunch p, const RopeLaunch rope) {
+__global__ __launch_bounds__(kThreads, BF16 ? 5 : 4) void cache_rope_store_kernel(const StoreLaunch p, const RopeLaunch rope) {
   __shared__ Shared sh;
-  __shared__ Angles<D> angles;
+  __shared__ Angles<D> angles[2];
   const int q0 = p.units * p.c.hkv * 2;
-  if ((int)blockIdx.x >= q0) turn_q<BF16, D>(p, rope, angles, blockIdx.x - q0);
-  else store_job<BF16, D, true, true>(p, sh, &rope, &angles);
+  if ((int)blockIdx.x >= q0) turn_q<BF16, D>(p, rope, angles[0], blockIdx.x - q0);
+  else store_job<BF16, D, true, true>(p, sh, &rope, angles);
 }
 
 }  // namespace

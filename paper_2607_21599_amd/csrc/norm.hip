@@ -5,10 +5,11 @@
 // at most 448), or both. fp32 arithmetic; the codes are rounded once, from the fp32
 // value.
 //
-// A row stays in registers between the sum of squares and its use, so that every
-// input is read once; 8 values per thread and piece, 4 neighbouring lanes have the 32
-// values of a scale. Sums go in a fixed order: a call's result depends on its inputs
-// alone.
+// A row of up to 16384 values stays in registers between the sum of squares and its use, so
+// that every input is read once; 8 values per thread and piece, 4 neighbouring lanes have
+// the 32 values of a scale. Sums go in a fixed order: a call's result depends on its inputs
+// alone. Bound by HBM: 5043 rows of 3584 with all outputs (163 MB) in 32 us, the rate of a
+// large copy; one row in 2.0 us, of which most is the launch.
 #include "e4m3.h"
 #include "step.h"
 
@@ -132,26 +133,30 @@ __global__ __launch_bounds__(kNormThreads) void add_rmsnorm_kernel(const NormLau
   }
 }
 
-template <bool BF16, int WAVES>
+template <bool BF16>
 hipError_t launch(const NormLaunch &p, hipStream_t st) {
-  constexpr int ROWS = kNormThreads / 64 / WAVES;
-  const unsigned grid = (unsigned)((p.rows + ROWS - 1) / ROWS);
-  const int pieces = (p.width / 8 + 64 * WAVES - 1) / (64 * WAVES);
-  auto go = [&](auto kern) { kern<<<grid, kNormThreads, 0, st>>>(p); };
-  if (pieces <= 1) go(add_rmsnorm_kernel<BF16, WAVES, 1>);
-  else if (pieces <= 2) go(add_rmsnorm_kernel<BF16, WAVES, 2>);
-  else if (pieces <= 4) go(add_rmsnorm_kernel<BF16, WAVES, 4>);
-  else if (pieces <= 8) go(add_rmsnorm_kernel<BF16, WAVES, 8>);
-  else go(add_rmsnorm_kernel<BF16, WAVES, 0>);
+  auto go = [&](auto kern, int waves) {
+    const int rows = kNormThreads / 64 / waves;
+    kern<<<(unsigned)((p.rows + rows - 1) / rows), kNormThreads, 0, st>>>(p);
+  };
+  // As many waves per row as give every thread one piece: rows of all sums and outputs, us by
+  // 1, 2, 4 and 8 waves: 40000 of 256 21.6, 26.5, 36.0, 52.2; 16000 of 1024 32.3, 29.6, 29.6,
+  // 34.8; 5043 of 3584 45.8, 39.6, 35.2, 32.4; 2000 of 8192 47.6, 40.4, 34.8, 32.9.
+  const int pieces = (p.width / 8 + 63) / 64;  // of a lane of one wave
+  if (pieces <= 1) go(add_rmsnorm_kernel<BF16, 1, 1>, 1);
+  else if (pieces <= 2) go(add_rmsnorm_kernel<BF16, 2, 1>, 2);
+  else if (pieces <= 4) go(add_rmsnorm_kernel<BF16, 4, 1>, 4);
+  else if (pieces <= 8) go(add_rmsnorm_kernel<BF16, 8, 1>, 8);
+  else if (pieces <= 16) go(add_rmsnorm_kernel<BF16, 8, 2>, 8);
+  else if (pieces <= 32) go(add_rmsnorm_kernel<BF16, 8, 4>, 8);
+  else go(add_rmsnorm_kernel<BF16, 8, 0>, 8);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_add_rmsnorm(bool bf16, const NormLaunch &p, hipStream_t st) {
-  const bool wave_per_row = p.rows >= 1024 && p.width <= 64 * 8 * 8;
-  if (wave_per_row) return bf16 ? launch<true, 1>(p, st) : launch<false, 1>(p, st);
-  return bf16 ? launch<true, kNormThreads / 64>(p, st) : launch<false, kNormThreads / 64>(p, st);
+  return bf16 ? launch<true>(p, st) : launch<false>(p, st);
 }
 
 }  // namespace daf
