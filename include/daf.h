@@ -319,9 +319,9 @@ daf_status_t daf_linear_swiglu(int64_t M, int32_t I, int32_t K, const void *A,
  *   255 is NaN; NaN codes of A are NaN. Products are exact, sums fp32; bias and residual are
  *   added in fp32 before the single rounding to bf16. residual may be C itself.
  * N below 2^24, K a positive multiple of 32 up to 2^24, M below 2^21 (DAF_ERR_UNSUPPORTED
- * otherwise), made for M up to
- * 32: more rows read the weights again for each 32. Scales need no alignment, all else 16
- * bytes. M = 0 is a no-op. workspace: at least daf_linear_mx_workspace_size bytes (0: none
+ * otherwise). Made for M up to 32: more rows read the weights again for each 32. Scales
+ * need no alignment and are read in whole aligned words of 4 bytes, all else 16 bytes. M = 0
+ * is a no-op. workspace (K above 4096): at least daf_linear_mx_workspace_size bytes (0: none
  * needed, or bad input), contents undefined after the call; calls that may run at the same
  * time, captured ones included, need one each. */
 size_t daf_linear_mx_workspace_size(int64_t M, int32_t N, int32_t K);

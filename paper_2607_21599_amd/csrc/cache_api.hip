@@ -421,29 +421,26 @@ int64_t plan_shared(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_c
   if (jobs > INT32_MAX / 2) return -1;
   p.n_splits = (int)n_splits;
 
-  // the groups' pages: two workgroups per CU in all, where there is work for them
+  // the groups' pages: row blocks and pages of each group that has any
+  int64_t jobs_of[kSharedMaxGroups];  // row blocks of all heads
+  int pages_of[kSharedMaxGroups], n_shared = 0, longest = 1;
+  int64_t work = 0;
   auto group_blocks = [&](int i) {
     const int lo = p.first[i], hi = i + 1 < p.n_groups ? p.first[i + 1] : p.n_req;
     return ((int64_t)(p.cu[hi] - p.cu[lo]) * p.group + p.block_rows - 1) / p.block_rows;
   };
-  auto workgroups = [&](int split_pages) {
+  for (int i = 0; i < p.n_groups; ++i) {
+    const int pages = p.pages[p.first[i]];
+    if (pages == 0) continue;
+    pages_of[n_shared] = pages;
+    jobs_of[n_shared] = group_blocks(i) * c->n_kv_heads;
+    work += pages * jobs_of[n_shared++];
+    longest = std::max(longest, pages);
+  }
+  auto workgroups = [&](int64_t split_pages) {
     int64_t n = 0;
-    for (int i = 0; i < p.n_groups; ++i) {
-      const int pages = p.pages[p.first[i]];
-      n += (pages + split_pages - 1) / split_pages * c->n_kv_heads * group_blocks(i);
-    }
+    for (int i = 0; i < n_shared; ++i) n += (pages_of[i] + split_pages - 1) / split_pages * jobs_of[i];
     return n;
-  };
-  int longest = 1;
-  for (int b = 0; b < p.n_req; ++b) longest = std::max(longest, p.pages[b]);
-  auto least_split = [&](int lo, int64_t wgs) {  // smallest of at least lo pages with at most wgs workgroups
-    int hi = std::max(lo, longest);
-    while (lo < hi) {
-      const int mid = lo + (hi - lo) / 2;
-      if (workgroups(mid) <= wgs) hi = mid;
-      else lo = mid + 1;
-    }
-    return lo;
   };
   // Of splits that give up to 1, 2, .. 16 workgroups per CU the ones that take least, in us of
   // bf16 and 128 features: 1.5 a page for a workgroup alone on its CU, 1.25 a page and
@@ -451,20 +448,24 @@ int64_t plan_shared(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_c
   // each 32 that a join reads one after the other. (32 decode rows over 512 pages, us a call:
   // 256 workgroups 37.8, 376 43.5, 448 40.6, 512 46.8; 301 question rows: 476 217, 612 197, 748 174,
   // 816 197, 1020 174; 80: 240 68.7, 380 69.8, 500 61.4, 620 72.5.) At least 2 pages, for short
-  // prefixes: 4 beams of 12 pages 11.5, in splits of 4 13.2, of 6 14.7.
-  // fp32 and blocks of 64 pairs take other times, here by their matrix instructions; fp32 of
-  // 128 features has one workgroup per CU.
+  // prefixes: 4 beams of 12 pages 11.5, in splits of 4 13.2, of 6 14.7. fp32 and blocks of 64
+  // pairs take other times, here by their matrix instructions; fp32 of 128 features has one
+  // workgroup per CU.
   const double unit = cfg->head_dim / 128. * (!bf16 ? 1.5 : p.block_rows == kCacheWideRows ? 1. : 0.7);
   const bool alone = !bf16 && cfg->head_dim == 128;
   double best = INFINITY;
-  for (int r = 1; r <= 16; ++r) {
-    const int sp = least_split(std::min(kMinSharedPages, longest), 256 * r);
+  for (int r : {1, 2, 3, 4, 6, 8, 12, 16}) {
+    // the smallest number of pages with at most 256 r workgroups, from the one below which there are more
+    int64_t sp = std::clamp<int64_t>(work / (256 * r), std::min(kMinSharedPages, longest), longest);
+    while (sp < longest && workgroups(sp) > 256 * r) sp += std::max<int64_t>(1, sp / 64);
+    sp = std::min<int64_t>(sp, longest);
     const int64_t wgs = workgroups(sp), per_cu = (wgs + 255) / 256, splits = (longest + sp - 1) / sp;
     const double page = alone ? 1.5 * (double)per_cu : per_cu <= 1 ? 1.5 : 1.25 * (double)per_cu;
-    const double us = sp * page * unit + 2e-4 * cfg->head_dim / 128 * (double)splits * p.rows * p.hq + (double)((splits + 31) / 32);
+    const double us = (double)sp * page * unit + 2e-4 * cfg->head_dim / 128 * (double)splits * p.rows * p.hq +
+                      (double)((splits + 31) / 32);
     if (us < best) {
       best = us;
-      p.split_pages = sp;
+      p.split_pages = (int)sp;
     }
   }
   int64_t wg = 0;
@@ -487,12 +488,12 @@ int64_t plan_shared(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_c
 size_t shared_lse_bytes(int64_t pairs) { return (pairs * sizeof(float) + 255) / 256 * 256 + kLineBytes; }
 
 // Bytes of workspace; rows that are too many for one call are refused.
+// p and pairs: the last launch's plan.
 daf_status_t shared_bytes(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_cache_rows_t *rows,
-                          const daf_cache_groups_t *g, int32_t max_len, size_t &bytes) {
+                          const daf_cache_groups_t *g, int32_t max_len, size_t &bytes, SharedLaunch &p, int64_t &pairs) {
   bytes = 0;
   for (int64_t i = 0; i < shared_chunks(rows); ++i) {
-    SharedLaunch p;
-    const int64_t pairs = plan_shared(cfg, c, rows, g, max_len, (int)i * kMaxCacheReqs, p);
+    pairs = plan_shared(cfg, c, rows, g, max_len, (int)i * kMaxCacheReqs, p);
     if (pairs < 0)
       return fail(DAF_ERR_UNSUPPORTED, "%d rows over %d keys are too many for one call", rows->cu[rows->n], max_len);
     if (pairs > 0) bytes = std::max(bytes, shared_lse_bytes(pairs) + (size_t)pairs * c->head_dim * sizeof(float));
@@ -514,7 +515,9 @@ daf_status_t attn_shared(const daf_attn_cfg_t *cfg, const daf_cache_t *c, int32_
   CHECK(need_ptr(o, "o"));
   CHECK(aligned(lse, "lse"));
   size_t need;
-  CHECK(shared_bytes(cfg, c, rows, g, max_len, need));
+  SharedLaunch p;
+  int64_t pairs;
+  CHECK(shared_bytes(cfg, c, rows, g, max_len, need, p, pairs));
   if (!workspace || ws_bytes < need)
     return fail(DAF_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace ? ws_bytes : 0);
   CHECK(aligned(workspace, "workspace"));
@@ -523,8 +526,7 @@ daf_status_t attn_shared(const daf_attn_cfg_t *cfg, const daf_cache_t *c, int32_
   const float scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale : 1.f / sqrtf((float)cfg->head_dim);
   for (int64_t i = 0; i < shared_chunks(rows); ++i) {
     const int b0 = (int)i * kMaxCacheReqs;
-    SharedLaunch p;
-    const int64_t pairs = plan_shared(cfg, c, rows, g, max_len, b0, p);
+    if (shared_chunks(rows) > 1) pairs = plan_shared(cfg, c, rows, g, max_len, b0, p);  // else it is planned already
     if (pairs <= 0) continue;
     const int64_t row0 = rows->cu[b0];
     p.c = view(c, layer);
@@ -644,7 +646,9 @@ size_t daf_cache_attn_shared_workspace_size(const daf_attn_cfg_t *cfg, const daf
     return 0;
   if (!any_shared(cfg, rows, groups, max_len)) return plan_attn(cfg, cache, rows, max_len).total;
   size_t bytes;
-  return shared_bytes(cfg, cache, rows, groups, max_len, bytes) == DAF_OK ? bytes : 0;
+  SharedLaunch p;
+  int64_t pairs;
+  return shared_bytes(cfg, cache, rows, groups, max_len, bytes, p, pairs) == DAF_OK ? bytes : 0;
 }
 
 daf_status_t daf_cache_attn_shared(const daf_attn_cfg_t *cfg, const daf_cache_t *cache, int32_t layer,

@@ -142,3 +142,23 @@ def cache_tensors(n_layers: int, n_pages: int, n_kv_heads: int, head_dim: int, n
             "table": torch.full((n_seqs, max_seq_pages), -1, dtype=torch.int32, device=device),
             "len": torch.zeros(n_seqs, dtype=torch.int32, device=device),
             "refs": torch.zeros(n_pages, dtype=torch.int32, device=device)}
+
+
+def mx_weights(w: torch.Tensor) -> tuple[torch.Tensor, torch.Tensor]:
+    """A weight matrix [N][K] as daf_linear_mx takes it: codes uint8 [N][K / 2] and
+    scales uint8 [N][K / 32]. Per 32 values of a row the scale is the smallest power of two
+    in [2^-100, 2^120] under which the largest magnitude is at most 6; codes are nearest,
+    ties to the even one. Done once, when a model is loaded; finite weights."""
+    n, k = w.shape
+    if k % 32:
+        raise ValueError(f"rows of {k} values are not whole blocks of 32")
+    x = w.double().view(n, k // 32, 32)
+    top = x.abs().amax(2)
+    m, e = torch.frexp(top)  # top = m 2^e, m in [0.5, 1): at most 6 2^s where m 2^(e - s) <= 0.75 2^3
+    e = torch.where(top > 0, (e - 3 + (m > 0.75).int()).clamp(-100, 120), -100)
+    y = (x.abs() * torch.exp2(-e.double())[..., None]).clamp(max=6)
+    step = torch.where(y < 2, 0.5, torch.where(y < 4, 1.0, 2.0))
+    y = torch.round(y / step) * step
+    code = torch.where(y <= 2, 2 * y, torch.where(y <= 4, 2 + y, 4 + y / 2)).to(torch.uint8)
+    code = (code | (x < 0).to(torch.uint8) << 3).view(n, k)
+    return code[:, 0::2] | code[:, 1::2] << 4, (e + 127).to(torch.uint8)
