@@ -558,7 +558,7 @@ typedef struct {
 
 /* Bytes of workspace daf_cache_attn_shared needs (0 on bad input or none needed). It grows
  * with the rows: at most 8 (D + 1) bytes per row and query head of 256 requests, 512 (D + 1)
- * per group and K/V head of them, and 280 MB. */
+ * per group and K/V head of them, and 544 MB. */
 size_t daf_cache_attn_shared_workspace_size(const daf_attn_cfg_t *cfg,
                                             const daf_cache_t *cache,
                                             const daf_cache_rows_t *rows,
@@ -570,7 +570,8 @@ size_t daf_cache_attn_shared_workspace_size(const daf_attn_cfg_t *cfg,
  * of a group's sequences must be the same, which is not checked: where they are not, rows see
  * the keys of another sequence of their group there, as far as their own len goes. A group of
  * more than 256 requests may read its pages once for each 256. Made for groups whose own
- * tokens are few beside the shared ones: those are taken 16 (row, head) pairs at a time. */
+ * tokens are few beside the shared ones: those are taken 16 (row, head) pairs at a time. Where
+ * the shared pages are few, daf_cache_attn's way through the whole sequences is taken. */
 daf_status_t daf_cache_attn_shared(const daf_attn_cfg_t *cfg, const daf_cache_t *cache,
                                    int32_t layer, const daf_cache_rows_t *rows,
                                    const daf_cache_groups_t *groups, int32_t max_len,
