@@ -50,13 +50,14 @@ struct RopeLaunch {
   void *q_out;
   int64_t q_pitch, kv_pitch;  // bytes from row to row of q, and of k and v
   int32_t hq;
-  int32_t per_req;  // rows of every request where they are equal, else 0
+  int32_t per_req;   // rows of every request where they are equal, else 0
+  uint32_t q_share;  // q's share of the workgroups, times 2^32
   double turn[64];  // of pair i of a head's features, per position: theta^(-2i/D) / (2 pi)
 };
 static_assert(sizeof(StoreLaunch) + sizeof(RopeLaunch) < 4096, "kernel arguments must fit 4 KiB");
 // workgroups of q's rows
 inline int64_t rope_jobs(int64_t rows, int d) { return (rows * (d / 2) + kStoreThreads - 1) / kStoreThreads; }
-hipError_t launch_cache_rope_store(bool bf16, const StoreLaunch &p, const RopeLaunch &rope, hipStream_t st);
+hipError_t launch_cache_rope_store(bool bf16, const StoreLaunch &p, RopeLaunch rope, hipStream_t st);
 constexpr int kStoreRows = 8;  // rows at positions: rows per unit
 hipError_t launch_cache_store(bool write, bool bf16, const StoreLaunch &p, hipStream_t st);
 

@@ -395,11 +395,12 @@ __device__ __forceinline__ void do_page(const StoreLaunch &p, Shared &sh, const 
 // is its page's first takes the page; else one page each of those that its n last
 // rows can touch.
 template <bool BF16, int D, bool WRITE, bool ROPE>
-__device__ __forceinline__ void store_job(const StoreLaunch &p, Shared &sh, const RopeLaunch *rope, Angles<D> *angles) {
+__device__ __forceinline__ void store_job(const StoreLaunch &p, Shared &sh, const RopeLaunch *rope, Angles<D> *angles,
+                                          int wg) {
   const int t = threadIdx.x;
   const int half = p.units * p.c.hkv;  // workgroups of K, then those of V
-  const bool is_v = (int)blockIdx.x >= half || !p.k;
-  const int job = (int)blockIdx.x >= half ? blockIdx.x - half : blockIdx.x;
+  const bool is_v = wg >= half || !p.k;
+  const int job = wg >= half ? wg - half : wg;
   const int h = job % p.c.hkv, unit = job / p.c.hkv;
   int b = 0;
   if (p.per_req) {
@@ -458,7 +459,7 @@ __device__ __forceinline__ void store_job(const StoreLaunch &p, Shared &sh, cons
 template <bool BF16, int D, bool WRITE>
 __global__ __launch_bounds__(kThreads) void cache_store_kernel(const StoreLaunch p) {
   __shared__ Shared sh;
-  store_job<BF16, D, WRITE, false>(p, sh, nullptr, nullptr);
+  store_job<BF16, D, WRITE, false>(p, sh, nullptr, nullptr, blockIdx.x);
 }
 
 // Rows of q, turned: a workgroup has kThreads / (D / 2) rows, whose angles its threads make
@@ -532,21 +533,25 @@ __device__ __forceinline__ void turn_q(const StoreLaunch &p, const RopeLaunch &r
     }
 }
 
-// K and V as above, K turned on the way, then the rows of q.
+// K and V as above, K turned on the way, and the rows of q, whose workgroups lie evenly
+// among theirs: these wait for chains of loads, those of q for memory (us a call, and with q
+// last: 16384 rows 55 and 63.6, 4915 rows at positions 39.6 and 38.6).
 template <bool BF16, int D>
 __global__ __launch_bounds__(kThreads, BF16 ? 5 : 4) void cache_rope_store_kernel(const StoreLaunch p, const RopeLaunch rope) {
   __shared__ Shared sh;
   __shared__ Angles<D> angles[2];
-  const int q0 = p.units * p.c.hkv * 2;
-  if ((int)blockIdx.x >= q0) turn_q<BF16, D>(p, rope, angles[0], blockIdx.x - q0);
-  else store_job<BF16, D, true, true>(p, sh, &rope, angles);
+  const unsigned q = (unsigned)((uint64_t)blockIdx.x * rope.q_share >> 32);  // of q's before this one
+  if ((unsigned)(((uint64_t)blockIdx.x + 1) * rope.q_share >> 32) > q) turn_q<BF16, D>(p, rope, angles[0], q);
+  else store_job<BF16, D, true, true>(p, sh, &rope, angles, blockIdx.x - q);
 }
 
 }  // namespace
 
-hipError_t launch_cache_rope_store(bool bf16, const StoreLaunch &p, const RopeLaunch &rope, hipStream_t st) {
-  const unsigned grid = (unsigned)p.units * p.c.hkv * 2 + (rope.q ? rope_jobs(p.cu[p.n_req], p.c.d) : 0);
-  auto go = [&](auto kern) { kern<<<grid, kThreads, 0, st>>>(p, rope); };
+hipError_t launch_cache_rope_store(bool bf16, const StoreLaunch &p, RopeLaunch rope, hipStream_t st) {
+  const uint64_t jobs = rope.q ? rope_jobs(p.cu[p.n_req], p.c.d) : 0, grid = (uint64_t)p.units * p.c.hkv * 2 + jobs;
+  // of grid workgroups exactly `jobs`: grid * share = jobs 2^32 and at most grid more
+  rope.q_share = jobs ? (uint32_t)((jobs << 32) / grid + 1) : 0;
+  auto go = [&](auto kern) { kern<<<(unsigned)grid, kThreads, 0, st>>>(p, rope); };
   if (p.c.d == 128) bf16 ? go(cache_rope_store_kernel<true, 128>) : go(cache_rope_store_kernel<false, 128>);
   else bf16 ? go(cache_rope_store_kernel<true, 64>) : go(cache_rope_store_kernel<false, 64>);
   return hipGetLastError();
