@@ -9,6 +9,16 @@
 //  * of the rest: the line of daf_cache_attn's few rows, from the first page that is not
 //    the group's on.
 // A second launch joins a row's partial results.
+//
+// Bound by the issue of the many rows' kernel (its comment) where the shared pages have more
+// than a few rows, and by the two launches' chains where they do not: 32 decode rows of 28 heads
+// on 4 of 128 over 32768 shared keys and up to 700 of their own 31.8 + 6.3 us (one copy of the
+// pages, 33.5 MB, is 7 us of HBM; by daf_cache_attn, a copy for each from the caches, 111), 301
+// question rows 157 + 13.9 (141 GFLOP, 0.90 PFLOP/s; by daf_cache_attn 190). A page takes a
+// workgroup alone on its CU 1.5 us, one of two 2.5; ahead of its pages are 6 us of launch, page
+// ids, scales and first copies. Row blocks of 256 pairs (64 rows a wave, one workgroup per CU)
+// take 2.15 us a page for two of 128 pairs on a CU 2.5, but leave no place for the tails and
+// split into twice as many partial results: 48 for 36 us.
 #include <algorithm>
 
 #include "cache_attn.h"
@@ -74,12 +84,30 @@ struct GroupRows {
   }
 };
 
-// The group of a workgroup or request, and its requests
+// A group, its requests and its first workgroup
 struct Group {
-  int g, b0, b1;
+  int b0, b1, wg0;
 };
-__device__ __forceinline__ Group group_at(const SharedLaunch &p, int g) {
-  return {g, p.first[g], g + 1 < p.n_groups ? p.first[g + 1] : p.n_req};
+// The last group whose `from` is at most x, one x for each STEP lanes. All that is asked of the
+// groups comes in one trip to the arguments, 64 groups at a time.
+template <int STEP, typename F>
+__device__ __forceinline__ Group find_group(const SharedLaunch &p, int x, F from) {
+  Group gr{0, p.n_req, 0};
+  const int lane = threadIdx.x & 63;
+  for (int i = 0; i < p.n_groups; i += 64) {
+    const int g = min(i + lane, p.n_groups - 1);
+    const int b0 = p.first[g], b1 = g + 1 < p.n_groups ? p.first[g + 1] : p.n_req, wg0 = p.wg0[g];
+    const int at = from(b0, wg0);
+    int n = 0;  // groups of these that begin by x
+#pragma unroll
+    for (int k = 0; k < 64; k += STEP) {
+      const int y = __builtin_popcountll(__ballot(i + lane < p.n_groups && at <= __builtin_amdgcn_readlane(x, k)));
+      if (lane / STEP == k / STEP) n = y;
+    }
+    const Group y{__shfl(b0, max(n - 1, 0)), __shfl(b1, max(n - 1, 0)), __shfl(wg0, max(n - 1, 0))};
+    if (n > 0) gr = y;
+  }
+  return gr;
 }
 
 // The workgroups of a group's units, (split, head) pairs, and of their row blocks. The row
@@ -114,14 +142,19 @@ __device__ __forceinline__ void group_job(const SharedLaunch &p, SharedMemory<BF
   constexpr int PAIRS = kWaves * 16 * MT;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n16 = lane & 15, quad = lane >> 4;
-  const Group gr = p.n_groups == 1 ? Group{0, 0, p.n_req} : group_at(p, find_in(p.wg0, p.n_groups, blockIdx.x));
+  Group gr{0, p.n_req, 0};
+  if (p.n_groups > 1) {
+    gr = find_group<64>(p, blockIdx.x, [](int, int wg0) { return wg0; });
+    gr = {__builtin_amdgcn_readfirstlane(gr.b0), __builtin_amdgcn_readfirstlane(gr.b1),
+          __builtin_amdgcn_readfirstlane(gr.wg0)};
+  }
   Request r;
   r.b = gr.b0;
   r.row0 = p.row_of(gr.b0);
   r.n = p.row_of(gr.b1) - r.row0;
   r.L = 0;  // not used
   const int total = r.n * p.group, blocks = (total + PAIRS - 1) / PAIRS, pages = p.first_page(gr.b0);
-  const UnitBlock ub = unit_block(blockIdx.x - (p.n_groups == 1 ? 0 : p.wg0[gr.g]), (pages + p.split_pages - 1) / p.split_pages * p.c.hkv, blocks);
+  const UnitBlock ub = unit_block(blockIdx.x - gr.wg0, (pages + p.split_pages - 1) / p.split_pages * p.c.hkv, blocks);
   const int h = ub.unit % p.c.hkv, pg0 = ub.unit / p.c.hkv * p.split_pages;
   r.block = ub.block;
   // the pages are those of the group's first sequence
@@ -170,19 +203,16 @@ __global__ __launch_bounds__(kThreads) void cache_shared_join_kernel(const Share
   const int row = mine ? (int)(job / p.hq) : p.rows - 1, head = mine ? (int)(job % p.hq) : 0;
   // the wave's pairs one after the other: searches by all lanes
   int b = p.per_req ? row / p.per_req : 0;
-  Group gr{0, 0, p.n_req};
-  if (!p.per_req || p.n_groups > 1) {
+  constexpr int STEP = TEAM == GROUPS ? 64 : LP;  // lanes of one pair
+  if (!p.per_req) {
 #pragma unroll
-    for (int k = 0; k < 64; k += TEAM == GROUPS ? 64 : LP) {
-      const int r = __builtin_amdgcn_readlane(row, k), at = p.per_req ? r / p.per_req : find_in(p.cu, p.n_req, r);
-      int g = p.n_groups > 1 ? -1 : 0;
-      if (p.n_groups > 1)
-        for (int i = 0; i < p.n_groups; i += 64)
-          g += __builtin_popcountll(__ballot(i + lane < p.n_groups && p.first[i + lane] <= at));
-      if (TEAM == GROUPS || lane / LP == k / LP) b = at, gr.g = g;
+    for (int k = 0; k < 64; k += STEP) {
+      const int at = find_in(p.cu, p.n_req, __builtin_amdgcn_readlane(row, k));
+      if (lane / STEP == k / STEP) b = at;
     }
-    gr = group_at(p, gr.g);
   }
+  Group gr{0, p.n_req, 0};
+  if (p.n_groups > 1) gr = find_group<STEP>(p, b, [](int b0, int) { return b0; });
   const int h = head / p.group, in_head = head % p.group;
   // the line: piece s of n_line, the first one's place is its workgroup's second
   const int pair = (row - p.row_of(b)) * p.group + in_head;
@@ -194,13 +224,13 @@ __global__ __launch_bounds__(kThreads) void cache_shared_join_kernel(const Share
     n_line = (from + units - 1) / piece - k0 + 1;
   }
   // the group's pages
-  const int row0 = p.row_of(gr.b0), wg0 = p.n_groups == 1 ? 0 : p.wg0[gr.g];
+  const int row0 = p.row_of(gr.b0);
   const int in_group = (row - row0) * p.group + in_head;
   const int blocks = ((p.row_of(gr.b1) - row0) * p.group + p.block_rows - 1) / p.block_rows;
   const int n_first = (p.first_page(gr.b0) + p.split_pages - 1) / p.split_pages, n = n_first + n_line;
   auto at = [&](int s) {
     if (s < n_first) {
-      const int wg = wg0 + workgroup_of({s * p.c.hkv + h, in_group / p.block_rows}, n_first * p.c.hkv, blocks);
+      const int wg = gr.wg0 + workgroup_of({s * p.c.hkv + h, in_group / p.block_rows}, n_first * p.c.hkv, blocks);
       return wg * p.block_rows + in_group % p.block_rows;
     }
     s -= n_first;

@@ -18,7 +18,7 @@ pytestmark = pytest.mark.gpu
 
 BF16 = torch.bfloat16
 HIDDEN, INTER, HQ, HKV, D, LAYERS, THETA, EPS = 384, 640, 8, 2, 64, 2, 1e4, 1e-6
-GROUPS, SHARED, TAILS = [5, 1, 3], [1344, 64, 130], [3, 61, 64, 1, 127, 30, 2, 5, 62]
+GROUPS, SHARED, TAILS = [5, 1, 3], [2144, 64, 130], [3, 61, 64, 1, 127, 30, 2, 5, 62]
 N = len(TAILS)
 QKV = (HQ + 2 * HKV) * D
 
