@@ -21,7 +21,7 @@
 // included). Rings beside registers: loads of W to registers in operand layout keep the
 // address unit 64 cycles for 1 KiB, a copy of whole pieces of rows 16; with those, and A
 // read again for each tile, 26 to 42 us. 1 row by 4608 x 3584 6.0 us, most of it launch and
-// one chain of loads; 12 rows by 3584 x 18944 12.8 + 3.9 us in 5 splits.
+// one chain of loads; 12 rows by 3584 x 18944 13.5 us in 5 splits, of which the join is 3.9.
 #include <algorithm>
 
 #include "step.h"
@@ -137,8 +137,10 @@ struct Slot {
   }
 };
 constexpr int kSlotBytes = 4096 + 512;  // a copy of words writes one for each of 64 lanes
-template <int MT>
-constexpr int kSlots = MT == 1 ? 4 : 3;  // of a wave's ring: with the sums, what LDS holds
+// Of a wave's ring: two tiles are on their way beside the one that is read. (us: 1 row by 37888 x
+// 3584 14.7, with 2 slots 17.0, with 4 15.9; 12 rows by 3584 x 18944 13.5, 13.3 and 14.8; 32 rows,
+// for which 4 do not fit LDS, by 37888 x 3584 19.5 and 21.1.)
+constexpr int kSlots = 3;
 
 // The words of 16 rows' scales, `blocks` bytes a row, from block b0 of each on
 struct ScaleWords {
@@ -165,7 +167,7 @@ template <bool MX, int MT, int STEPS>
 __global__ __launch_bounds__(64 * kMxWaves, 2) void linear_mx_kernel(const MxLaunch p) {
   using S = Slot<4 * STEPS>;
   using SA = Slot<16>;  // of A 256 bytes a row: a step of bf16, two of codes
-  constexpr int SLOTS = kSlots<MT>, APIECE = MX ? 2 : 1, ITEMS = (STEPS + APIECE - 1) / APIECE * MT;
+  constexpr int SLOTS = kSlots, APIECE = MX ? 2 : 1, ITEMS = (STEPS + APIECE - 1) / APIECE * MT;
   __shared__ f32x4 sums[2][kMxWaves][MT][64];
   __shared__ __align__(16) unsigned char rings[kMxWaves][SLOTS][kSlotBytes];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -221,7 +223,7 @@ __global__ __launch_bounds__(64 * kMxWaves, 2) void linear_mx_kernel(const MxLau
   };
   auto fetch_item = [&](int slot, int item) { item < ITEMS ? fetch_a(slot, item) : fetch(slot, item - ITEMS); };
 #pragma unroll
-  for (int i = 0; i < SLOTS - 1; ++i) fetch_item(i, i);
+  for (int i = 0; i < SLOTS; ++i) fetch_item(i, i);
 
   int slot = 0;
   auto turn = [&] { slot = slot == SLOTS - 1 ? 0 : slot + 1; };
@@ -236,7 +238,7 @@ __global__ __launch_bounds__(64 * kMxWaves, 2) void linear_mx_kernel(const MxLau
 #pragma unroll
   for (int item = 0; item < ITEMS; ++item) {
     // fewer steps than 4: a tile has fewer copies than a part of A
-    wait_copies<STEPS == 4 ? (SLOTS - 2) * 6 : 0>();
+    wait_copies<STEPS == 4 ? (SLOTS - 1) * 6 : 0>();
     const unsigned char *at = rings[wave][slot];
     const int e = item % MT, s = item / MT * APIECE;
     u32x4 x[4];
@@ -253,7 +255,7 @@ __global__ __launch_bounds__(64 * kMxWaves, 2) void linear_mx_kernel(const MxLau
       for (int i = 0; i < 4; ++i) x[i] = SA::read(at, n16, g * 4 + i);
     }
     slot_is_read();
-    fetch_item(before(), item + SLOTS - 1);
+    if (item < ITEMS - 1) fetch_item(slot, item + SLOTS);
     turn();
     if constexpr (MX) {
 #pragma unroll
@@ -370,6 +372,9 @@ __global__ __launch_bounds__(256) void linear_mx_join_kernel(const MxLaunch p) {
   const size_t at = (size_t)blockIdx.x * p.n + n, total = (size_t)p.m * p.n;
   constexpr int FLIGHT = 8;
   fv x = {};
+  bv bias = {}, residual = {};
+  if (p.bias) bias = *reinterpret_cast<const bv *>(static_cast<const __bf16 *>(p.bias) + n);
+  if (p.residual) residual = *reinterpret_cast<const bv *>(static_cast<const __bf16 *>(p.residual) + at);
   for (int s0 = 0; s0 < p.splits; s0 += FLIGHT) {
     fv y[FLIGHT];
 #pragma unroll
@@ -378,12 +383,10 @@ __global__ __launch_bounds__(256) void linear_mx_join_kernel(const MxLaunch p) {
     for (int i = 0; i < FLIGHT; ++i)
       if (s0 + i < p.splits) x += y[i];
   }
-  auto add = [&](const void *rows, size_t from) {
-    const bv v = *reinterpret_cast<const bv *>(static_cast<const __bf16 *>(rows) + from);
-    for (int i = 0; i < VEC; ++i) x[i] += (float)v[i];
-  };
-  if (p.bias) add(p.bias, n);
-  if (p.residual) add(p.residual, at);
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) x[i] += (float)bias[i];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) x[i] += (float)residual[i];
   bv y;
   for (int i = 0; i < VEC; ++i) y[i] = (__bf16)x[i];
   *reinterpret_cast<bv *>(static_cast<__bf16 *>(p.c) + at) = y;
