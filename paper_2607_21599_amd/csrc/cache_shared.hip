@@ -16,9 +16,8 @@
 // pages, 33.5 MB, is 7 us of HBM; by daf_cache_attn, a copy for each from the caches, 111), 301
 // question rows 157 + 13.9 (141 GFLOP, 0.90 PFLOP/s; by daf_cache_attn 190). A page takes a
 // workgroup alone on its CU 1.5 us, one of two 2.5; ahead of its pages are 6 us of launch, page
-// ids, scales and first copies. Row blocks of 256 pairs (64 rows a wave, one workgroup per CU)
-// take 2.15 us a page for two of 128 pairs on a CU 2.5, but leave no place for the tails and
-// split into twice as many partial results: 48 for 36 us.
+// ids, scales and first copies. Row blocks of 256 pairs (64 rows a wave, 502 registers, one
+// workgroup per CU) at their best splits took 48 us for 36 and 254 for 167.
 #include <algorithm>
 
 #include "cache_attn.h"
