@@ -318,8 +318,8 @@ daf_status_t daf_linear_swiglu(int64_t M, int32_t I, int32_t K, const void *A,
  *   A scale's byte counts as 27 where it is less and 247 where it is more (2^-100 .. 2^120),
  *   255 is NaN; NaN codes of A are NaN. Products are exact, sums fp32; bias and residual are
  *   added in fp32 before the single rounding to bf16. residual may be C itself.
- * N below 2^24, K a positive multiple of 32 up to 2^24, M below 2^21 (DAF_ERR_UNSUPPORTED
- * otherwise). Made for M up to 32: more rows read the weights again for each 32. Scales
+ * N up to 65535 * 256, K a positive multiple of 32 up to 2^24, M up to 65535 * 32
+ * (DAF_ERR_UNSUPPORTED otherwise). Made for M up to 32: more rows read the weights again for each 32. Scales
  * need no alignment and are read in whole aligned words of 4 bytes, all else 16 bytes. M = 0
  * is a no-op. workspace (K above 4096): at least daf_linear_mx_workspace_size bytes (0: none
  * needed, or bad input), contents undefined after the call; calls that may run at the same
@@ -349,7 +349,8 @@ daf_status_t daf_rmsnorm(int64_t rows, int32_t width, const void *x,
  *   values. Infinities count as the largest finite value, NaN stays NaN and does not
  *   count for the scale.
  * At least one of y and codes. fp32 arithmetic. width must be a positive multiple of 8,
- * with codes of 32; other pointers 16-byte aligned; rows = 0 is a no-op. */
+ * with codes of 32, rows below 2^23 (DAF_ERR_UNSUPPORTED otherwise); other pointers 16-byte
+ * aligned; rows = 0 is a no-op. */
 daf_status_t daf_add_rmsnorm(int32_t dtype, int64_t rows, int32_t width, const void *x,
                              const void *delta, const void *w, float eps, void *sum,
                              void *y, void *codes, uint8_t *scales, hipStream_t stream);
@@ -568,10 +569,11 @@ size_t daf_cache_attn_shared_workspace_size(const daf_attn_cfg_t *cfg,
 /* daf_cache_attn, with the pages that a group's sequences have in common read once for all
  * of its rows. Arguments and results as there. The first shared / 64 entries of the tables
  * of a group's sequences must be the same, which is not checked: where they are not, rows see
- * the keys of another sequence of their group there, as far as their own len goes. A group of
- * more than 256 requests may read its pages once for each 256. Made for groups whose own
- * tokens are few beside the shared ones: those are taken 16 (row, head) pairs at a time. Where
- * the shared pages are few, daf_cache_attn's way through the whole sequences is taken. */
+ * the keys of another sequence of their group there, as far as their own len goes. Sequences
+ * out of range, as a padded batch has them, are left out. A group of more than 256 requests
+ * may read its pages once for each 256. Made for groups whose own tokens are few beside the
+ * shared ones: those are taken 16 (row, head) pairs at a time. Where the shared pages are few,
+ * daf_cache_attn's way through the whole sequences is taken. */
 daf_status_t daf_cache_attn_shared(const daf_attn_cfg_t *cfg, const daf_cache_t *cache,
                                    int32_t layer, const daf_cache_rows_t *rows,
                                    const daf_cache_groups_t *groups, int32_t max_len,

@@ -156,10 +156,16 @@ __device__ __forceinline__ void group_job(const SharedLaunch &p, SharedMemory<BF
   const UnitBlock ub = unit_block(blockIdx.x - gr.wg0, (pages + p.split_pages - 1) / p.split_pages * p.c.hkv, blocks);
   const int h = ub.unit % p.c.hkv, pg0 = ub.unit / p.c.hkv * p.split_pages;
   r.block = ub.block;
-  // the pages are those of the group's first sequence
-  const int seq = p.seq ? p.seq[gr.b0] : gr.b0;
-  const bool there = (unsigned)seq < (unsigned)p.c.n_seqs;
-  r.pages = p.c.table + (int64_t)(there ? seq : 0) * p.c.max_seq_pages;
+  // the pages are those of the group's first sequence that is in range: batches are padded
+  int seq = 0;
+  bool there = false;
+  for (int b = gr.b0; b < gr.b1 && !there; b += 64) {
+    const int at = min(b + lane, gr.b1 - 1), mine = p.seq ? p.seq[at] : at;
+    const unsigned long long in = __ballot((unsigned)mine < (unsigned)p.c.n_seqs);
+    there = in != 0;
+    if (there) seq = __builtin_amdgcn_readlane(mine, __builtin_ctzll(in));
+  }
+  r.pages = p.c.table + (int64_t)seq * p.c.max_seq_pages;
   GroupRows<MT> rows{p, gr.b0, gr.b1 - gr.b0, r.row0, there ? pages : 0, sh.wide.cu, sh.wide.len, {}};
   rows.start();
   W w;

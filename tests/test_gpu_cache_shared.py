@@ -183,6 +183,29 @@ def test_sequences_and_pages_that_are_not_there():
     assert o.isfinite().all() and not lse.isnan().any()
 
 
+@pytest.mark.parametrize("n", [5, 70])
+def test_padded_groups(n):
+    """Requests whose sequence is out of range, with and without rows, at a group's head: the others read the
+    group's pages as if it were not there."""
+    p, _, seq, _ = _forked([n], [2300], [1 + i % 70 for i in range(n)], 4, 2, 64, BF16, seed=16)
+    q = torch.randn(n, 4, 64, generator=torch.Generator().manual_seed(6)).to(BF16).cuda()
+    cu = list(range(n + 1))
+    good, good_lse = _attn(p, 0, cu, seq, q, [n], [2300])
+    for gone in ([0], [0, 1], list(range(n - 1))):
+        bad = [(-1 if i % 2 else 1 << 30) if i in gone else x for i, x in enumerate(seq)]
+        o, lse = _attn(p, 0, cu, bad, q, [n], [2300])
+        assert (o[:len(gone)] == 0).all() and (lse[:, :len(gone)] == -torch.inf).all()
+        assert torch.equal(o[len(gone):], good[len(gone):]) and torch.equal(lse[:, len(gone):], good_lse[:, len(gone):])
+    # the first has no rows either
+    nq = [0] + [1] * (n - 1)
+    want, want_lse = _attn(p, 0, _cu(nq), seq, q[1:].contiguous(), [n], [2300])
+    o, lse = _attn(p, 0, _cu(nq), [-1] + seq[1:], q[1:].contiguous(), [n], [2300])
+    assert torch.equal(o, want) and torch.equal(lse, want_lse)
+    # none is there
+    o, lse = _attn(p, 0, cu, [-1] * n, q, [n], [2300])
+    assert (o == 0).all() and (lse == -torch.inf).all()
+
+
 def test_empty_sequences_and_rows_without_keys():
     p = _pair(pages=8, heads=1, hq=4, d=64, n_seqs=4, max_seq_pages=60)
     q = torch.randn(9, 4, 64, generator=torch.Generator().manual_seed(2)).to(BF16).cuda()
