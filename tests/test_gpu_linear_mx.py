@@ -149,6 +149,25 @@ def test_nan_and_infinity_stay_in_their_rows():
     assert clean.isfinite().all()
 
 
+@pytest.mark.parametrize("m,n,k", [(5, 37, 416), (20, 33, 4128), (3, 16, 32)])
+def test_scales_of_any_alignment(m, n, k):
+    """Scales from every byte of a word on, to the last byte of their allocation, between bytes of other scales."""
+    t = _inputs(m, n, k, True, 21)
+    want = _run(t)
+    for off in (1, 2, 3):
+        u = dict(t)
+        for name in ("ws", "as"):
+            whole = torch.full((t[name].numel() + off,), 255, dtype=torch.uint8, device="cuda")  # NaN
+            whole[off:] = t[name].flatten()
+            u[name] = whole[off:].view(t[name].shape)
+            assert u[name].data_ptr() % 4 == off
+        assert torch.equal(_run(u), want)
+        between = torch.full((t["ws"].numel() + 8,), 255, dtype=torch.uint8, device="cuda")
+        between[off:off + t["ws"].numel()] = t["ws"].flatten()
+        u["ws"] = between[off:off + t["ws"].numel()].view(n, k // 32)
+        assert torch.equal(_run(u), want)
+
+
 @pytest.mark.parametrize("m,n,k", [(3, 65, 512), (12, 96, 18944)])
 def test_residual_in_place(m, n, k):
     t = _inputs(m, n, k, True, 8)
