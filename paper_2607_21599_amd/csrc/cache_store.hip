@@ -255,23 +255,23 @@ __device__ __forceinline__ void do_page(const StoreLaunch &p, Shared &sh, const 
 #pragma unroll
     for (int i = 0; i < PASSES; ++i)
       if ((rows_mine >> i) & 1) E::template load<N>(at(i), given[i]);
-    if (!go) return;  // uniform in the workgroup
+    if (!can) return;  // uniform in the workgroup, as `go`
     unsigned x[PASSES][X::words(N)];
     if constexpr (TURN) {
-      // Angles are made by all threads, whatever rows there are: of few rows all at once, in
+      // Angles, which do not wait for the page's id either, are made by all threads, whatever rows there are: of few rows all at once, in
       // the order of their slots, else a pass at a time, into a place that the pass before
       // does not read.
       constexpr int HALF = D / 2, SLOTS = Angles<D>::SLOTS;
       const double turn = rope->turn[t % HALF], base = pg * (double)kPage;
-      const bool high = d0 >= HALF, few = __builtin_popcountll(go) <= 2 * SLOTS;
+      const bool high = d0 >= HALF, few = __builtin_popcountll(can) <= 2 * SLOTS;
       auto angle = [&](int place, int s) {
         sine_cosine((base + s) * turn, angles[place / SLOTS].sine[place % SLOTS][t % HALF],
                     angles[place / SLOTS].cosine[place % SLOTS][t % HALF]);
       };
       if (few) {
-        const int n = __builtin_popcountll(go);
+        const int n = __builtin_popcountll(can);
 #pragma unroll 1
-        for (int r = t / HALF; r < n; r += kThreads / HALF) angle(r, nth_bit(go, r));
+        for (int r = t / HALF; r < n; r += kThreads / HALF) angle(r, nth_bit(can, r));
         __syncthreads();
       }
       int half = 0;  // of the angles' places
@@ -279,11 +279,11 @@ __device__ __forceinline__ void do_page(const StoreLaunch &p, Shared &sh, const 
       for (int i = 0; i < PASSES; ++i) {
 #pragma unroll
         for (int j = 0; j < N; ++j) x[i][j] = 0u;  // other slots
-        const unsigned rows_here = (unsigned)(go >> i * SPP) & (unsigned)((1ull << SPP) - 1);
+        const unsigned rows_here = (unsigned)(can >> i * SPP) & (unsigned)((1ull << SPP) - 1);
         if (!rows_here) continue;
         int place;  // of this lane's slot
         if (few) {
-          place = __builtin_popcountll(go & ((1ull << slot(i)) - 1));
+          place = __builtin_popcountll(can & ((1ull << slot(i)) - 1));
         } else {
 #pragma unroll 1
           for (int s = t / HALF; s < SPP; s += kThreads / HALF)
@@ -295,7 +295,7 @@ __device__ __forceinline__ void do_page(const StoreLaunch &p, Shared &sh, const 
         unsigned other[E::words(N)];  // the half of the pairs that is another lane's
 #pragma unroll
         for (int j = 0; j < E::words(N); ++j) other[j] = __shfl_xor((int)given[i][j], CH / 2);
-        if ((mine >> i) & 1) {
+        if ((rows_mine >> i) & 1) {
           const float *c = &angles[place / SLOTS].cosine[place % SLOTS][d0 % HALF];
           const float *s = &angles[place / SLOTS].sine[place % SLOTS][d0 % HALF];
 #pragma unroll
@@ -311,6 +311,7 @@ __device__ __forceinline__ void do_page(const StoreLaunch &p, Shared &sh, const 
 #pragma unroll
         for (int j = 0; j < E::words(N); ++j) x[i][j] = given[i][j];
     }
+    if (!go) return;
     float present = 0.f;
     if (t == 0) present = *scale;
     const bool kept = ((held >= 64 ? ~0ull : (1ull << held) - 1) & ~go) != 0;
