@@ -17,7 +17,7 @@
 // (4915 rows over 512 pages, 57 MB, 23 us: chains of dependent loads, a page's at a
 // time, of which more rows per unit or fewer took as long) and for a few (32 rows 4.9 and
 // 3.5 us). With the rotation of K, and q's rows of 28 heads beside them: 16384 rows 55 us (285
-// MB, the rate of a large copy), 4915 scattered ones 39 (28 without q), 32 ragged appends 5.7.
+// MB, the rate of a large copy), 4915 scattered ones 36 (26 without q), 32 ragged appends 5.5.
 #include "cache.h"
 #include "e4m3.h"
 
@@ -258,9 +258,10 @@ __device__ __forceinline__ void do_page(const StoreLaunch &p, Shared &sh, const 
     if (!can) return;  // uniform in the workgroup, as `go`
     unsigned x[PASSES][X::words(N)];
     if constexpr (TURN) {
-      // Angles, which do not wait for the page's id either, are made by all threads, whatever rows there are: of few rows all at once, in
+      // Angles are made by all threads, whatever rows there are: of few rows all at once, in
       // the order of their slots, else a pass at a time, into a place that the pass before
-      // does not read.
+      // does not read. They do not wait for the page's id either (4915 scattered rows 36.3 us,
+      // after its arrival 39.0, with the scale's load before them and the barrier 38.5).
       constexpr int HALF = D / 2, SLOTS = Angles<D>::SLOTS;
       const double turn = rope->turn[t % HALF], base = pg * (double)kPage;
       const bool high = d0 >= HALF, few = __builtin_popcountll(can) <= 2 * SLOTS;
