@@ -537,8 +537,10 @@ __device__ __forceinline__ void turn_q(const StoreLaunch &p, const RopeLaunch &r
 }
 
 // K and V as above, K turned on the way, and the rows of q, whose workgroups lie evenly
-// among theirs: these wait for chains of loads, those of q for memory (us a call, and with q
-// last: 16384 rows 55 and 63.6, 4915 rows at positions 39.6 and 38.6).
+// among theirs: these wait for chains of loads, those of q for memory (16384 rows 55 us, with
+// q's last 63.6; 4915 rows at positions as long either way). Registers leave room for 5
+// workgroups per CU: with 8, of builds for rows at positions and for others, 16384 rows took
+// 58.7, 15.4 for 16.8 without q, and 4915 as long.
 template <bool BF16, int D>
 __global__ __launch_bounds__(kThreads, BF16 ? 5 : 4) void cache_rope_store_kernel(const StoreLaunch p, const RopeLaunch rope) {
   __shared__ Shared sh;
