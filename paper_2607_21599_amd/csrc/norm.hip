@@ -56,10 +56,10 @@ __global__ __launch_bounds__(kNormThreads) void add_rmsnorm_kernel(const NormLau
   __shared__ float part[kNormThreads / 64];
   const int t = threadIdx.x % THREADS, wave = threadIdx.x >> 6;
   const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS;
-  const bool have = row < p.rows;  // one wave per row: none waits for another
-  if (WAVES == 1 && !have) return;
+  const bool have = row < p.rows;
+  if (WAVES == 1 && !have) return;  // one wave per row: none waits for another
   const int64_t row0 = row * p.width;
-  const int pieces = p.width / 8;
+  const int pieces = have ? p.width / 8 : 0;  // waves past the last row still reach the barrier
   constexpr int HELD = PIECES > 0 ? PIECES : 1;
   float s[HELD][8], ss = 0.f;
   auto sum = [&](int j, float (&v)[8], bool again) {  // of x and delta, in the rows' type

@@ -101,6 +101,28 @@ def test_rows_of_every_width(rows, width, dtype):
             _check(x, d, w, _ran(x, d, w, y=y, codes=codes))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("width", [512, 544, 1024, 1056, 2048, 2080, 4096, 4128, 8224, 16384, 16416])
+def test_nothing_is_written_past_the_last_row(width, dtype):
+    """Every number of waves per row, with every number of rows in the last workgroup: inputs, and eight rows
+    before and behind each output, stay."""
+    for rows in range(1, 10):
+        x, delta, w = _inputs(rows, width, dtype, rows)
+        kept = [v.clone() for v in (x, delta, w)]
+        whole = {}
+        for n, cols, t in (("sum", width, dtype), ("y", width, dtype), ("codes", width, torch.float8_e4m3fn), ("scales", width // 32, torch.uint8)):
+            whole[n] = torch.full((rows + 16, cols), 77.0, device="cuda").to(t)
+        out = {n: v[8:-8] for n, v in whole.items()}
+        daf.daf_add_rmsnorm(daf.DAF_BF16 if dtype == BF16 else daf.DAF_F32, rows, width, x, delta, w, EPS, out["sum"], out["y"],
+                            out["codes"], out["scales"])
+        torch.cuda.synchronize()
+        for n, v in whole.items():
+            ends = torch.cat([v[:8], v[-8:]]).float()
+            assert torch.equal(ends, torch.full_like(ends, 77.0).to(v.dtype).float()), (n, rows)
+        assert all(torch.equal(a, b) for a, b in zip(kept, (x, delta, w)))
+        _check(x, delta, w, out)
+
+
 def test_codes_are_those_of_the_rounding_of_y():
     """Both outputs of one call, and those of a call each, are the same bits."""
     x, delta, w = _inputs(40, 3584, BF16, 3)
