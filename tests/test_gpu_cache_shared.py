@@ -114,6 +114,19 @@ def test_questions(dtype, d, hq, heads, shared, nq):
     _check(p, 0, _cu(nq), seq, [5], [shared])
 
 
+@pytest.mark.parametrize("dtype,d,hq,heads,groups,shared,nq", [
+    (BF16, 128, 28, 4, [3], [2200], [60, 50, 64]),                       # a few partial results of each row
+    (F32, 128, 16, 16, [3, 2], [4416, 200], [60, 64, 40, 50, 51]),       # more of them
+    (BF16, 64, 16, 16, [2, 4], [3200, 100], [70, 60, 40, 30, 30, 31]),
+    (F32, 64, 16, 16, [2, 4], [6400, 100], [2, 2, 70, 64, 70, 64]),
+    (BF16, 128, 16, 16, [2, 4], [6400, 100], [2, 2, 70, 64, 70, 64])])
+def test_more_pairs_than_a_join_helps(dtype, d, hq, heads, groups, shared, nq):
+    """Rows and heads that fill the device by themselves: their joins by one, two or four teams of lanes."""
+    assert sum(nq) * hq >= 4096
+    p, _, seq, _ = _forked(groups, shared, [n + 5 for n in nq], hq, heads, d, dtype, seed=17)
+    _check(p, 0, _cu(nq), seq, groups, shared)
+
+
 @pytest.mark.parametrize("dtype,d,hq,heads", CFGS)
 def test_rows_at_positions(dtype, d, hq, heads):
     """Anywhere in their sequences, in no order, before the first token and past the last."""
