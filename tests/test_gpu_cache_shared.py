@@ -175,6 +175,17 @@ def test_more_requests_than_a_launch_takes():
     _check(p, 0, list(range(len(seq) + 1)), seq, groups, shared)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("varied", [False, True])
+def test_more_groups_than_lanes(dtype, varied):
+    """Over a hundred groups of one to three requests, long and short prefixes, with none among them."""
+    groups = [2, 1, 3] * 34
+    shared = [2200 + i if i in (0, 50, 63, 64, 65, 101) else 64 * (i % 4) + i % 5 for i in range(102)]
+    nq = [1 + (i % 3 if varied else 0) - (varied and i % 11 == 0) for i in range(sum(groups))]
+    p, _, seq, _ = _forked(groups, shared, [3 + i % 7 for i in range(sum(groups))], 6, 1, 64, dtype, seed=18)
+    _check(p, 0, _cu(nq), seq, groups, shared)
+
+
 def test_sequences_and_pages_that_are_not_there():
     """Sequences out of range see nothing; pages out of range hold no keys, for the whole group."""
     p, _, seq, _ = _forked([3], [2220], [30, 5, 64], 4, 2, 64, BF16, seed=8)
