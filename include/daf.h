@@ -567,7 +567,8 @@ size_t daf_cache_attn_shared_workspace_size(const daf_attn_cfg_t *cfg,
                                             int32_t max_len);
 
 /* daf_cache_attn, with the pages that a group's sequences have in common read once for all
- * of its rows. Arguments and results as there. The first shared / 64 entries of the tables
+ * of its rows. Arguments and results as there, with as many bits of a probability as that call
+ * gives it. The first shared / 64 entries of the tables
  * of a group's sequences must be the same, which is not checked: where they are not, rows see
  * the keys of another sequence of their group there, as far as their own len goes. Sequences
  * out of range, as a padded batch has them, are left out. A group of more than 256 requests

@@ -136,6 +136,7 @@ struct SharedLaunch {
   int32_t first_wgs;   // workgroups of the groups' pages
   int32_t n_splits;    // workgroups per head of the line
   int32_t whole;       // a row block's rest of the line is one unit
+  int32_t exact;       // the groups' weights in as many bits as the line's
   int32_t n_req;
   float scale_log2;
   int32_t cu[kMaxCacheReqs + 1];

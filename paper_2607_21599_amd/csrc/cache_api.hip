@@ -191,15 +191,20 @@ size_t wide_pairs(const daf_attn_cfg_t *cfg, int64_t blocks, int block_rows) {
   return (size_t)blocks * cfg->n_kv_heads * block_rows;
 }
 
+// Up to four of few rows' blocks read a page from the caches as often before the wide
+// kernel's larger tiles pay (7 heads on one, us a call, few rows and wide: 8000 keys, 9
+// rows 17.4 and 19.7, 18 rows 21.3 and 20.0; 131072 keys 58.0 and 56.9, 103 and 57.4).
+bool many_rows(const daf_attn_cfg_t *cfg, const daf_cache_rows_t *rows) {
+  int64_t most = 0;
+  for (int b = 0; b < rows->n; ++b) most = std::max<int64_t>(most, rows->cu[b + 1] - rows->cu[b]);
+  return most * (cfg->n_q_heads / cfg->n_kv_heads) > 4 * kCacheAttnRows;
+}
+
 // Kernel and its splits, from the sizes that the host knows.
 AttnPlan plan_attn(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_cache_rows_t *rows, int32_t max_len) {
   AttnPlan a{};
-  int64_t most = 0, blocks = 0, least = INT32_MAX;
-  for (int b = 0; b < rows->n; ++b) most = std::max<int64_t>(most, rows->cu[b + 1] - rows->cu[b]);
-  // Up to four of few rows' blocks read a page from the caches as often before the wide
-  // kernel's larger tiles pay (7 heads on one, us a call, few rows and wide: 8000 keys, 9
-  // rows 17.4 and 19.7, 18 rows 21.3 and 20.0; 131072 keys 58.0 and 56.9, 103 and 57.4).
-  a.wide = most * (cfg->n_q_heads / cfg->n_kv_heads) > 4 * kCacheAttnRows;
+  int64_t blocks = 0, least = INT32_MAX;
+  a.wide = many_rows(cfg, rows);
   a.block_rows = !a.wide ? kCacheAttnRows : cfg->dtype == DAF_BF16 ? kCacheWideRows : kCacheWideRowsF32;
   for (int b = 0; b < rows->n; ++b) {
     const int64_t n = row_blocks(cfg, rows->cu[b + 1] - rows->cu[b], a.block_rows);
@@ -390,6 +395,7 @@ int64_t plan_shared(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_c
   p.hq = cfg->n_q_heads;
   p.group = cfg->n_q_heads / cfg->n_kv_heads;
   p.max_len = max_len;
+  p.exact = !many_rows(cfg, rows);  // a row's weights as daf_cache_attn has them
   p.n_groups = 0;
   for (int i = 0; i <= p.n_req; ++i) p.cu[i] = rows->cu[b0 + i] - rows->cu[b0];
   p.rows = p.cu[p.n_req];

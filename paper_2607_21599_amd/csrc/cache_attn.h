@@ -675,7 +675,8 @@ struct Wide {
 
 // Row block r.block of r's rows over the pages pg0 .. pg0 + split_pages - 1, as far as a row
 // sees them, by the whole workgroup: sums in w, O in units of `unit`. False: no keys here.
-// rows: empty(), seen() and limit(row) of the block, the last with a row in r.
+// rows: empty(), seen() and limit(row) of the block, the last with a row in r; exact(): bf16's
+// weights as the few rows' kernel has them.
 template <bool BF16, int D, int MT, typename P, typename Rows>
 __device__ __forceinline__ bool wide_rows(const P &p, unsigned char *lds, const Request &r, int h, int pg0,
                                           int split_pages, Rows &rows, Wide<BF16, D, MT> &w, float &unit) {
@@ -857,7 +858,7 @@ __device__ __forceinline__ bool wide_rows(const P &p, unsigned char *lds, const 
     }
 #pragma unroll
     for (int m = 32; m; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
-    if (__ballot(odd || least * kHalfSpread < most) == 0) {
+    if (!rows.exact() && __ballot(odd || least * kHalfSpread < most) == 0) {
       unit = most;
       per_unit = most > 0.f ? 1.f / most : 0.f;
       run(HalfWeights{});

@@ -143,6 +143,7 @@ struct LenRows {
   const CacheAttnLaunch &p;
   const Request &r;
   int split, pg0;
+  __device__ __forceinline__ bool exact() const { return false; }
   __device__ __forceinline__ bool empty() const { return split > 0 && pg0 >= (r.L + kPage - 1) / kPage; }
   __device__ __forceinline__ int limit(int row) const { return row_limit(p, r, row); }
   __device__ __forceinline__ int seen() const {
