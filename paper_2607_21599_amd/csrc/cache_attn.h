@@ -777,10 +777,17 @@ __device__ __forceinline__ bool wide_rows(const P &p, unsigned char *lds, const 
   w.lim_hi = __builtin_amdgcn_readfirstlane(lim_hi);
   lim_lo = __builtin_amdgcn_readfirstlane(lim_lo);
 
+  // Pages that are known go through the products whether a row sees them or not: those that
+  // no row of the wave sees may hold anything, a scale of NaN too, by which codes of 0 would
+  // be NaN (their scores are masked). Their values get scale 0.
+  auto hide_unseen = [&] {
+    if constexpr (Rows::kKnown) vss = firsts <= w.lim_hi ? vss : 0.f;
+  };
   if constexpr (!Rows::kKnown) {
     settle(0);
     begin();
   }
+  hide_unseen();
   // The products of the n pages, with weights as P has them.
   auto pages_of_64 = [&](auto weights) {
     using Form = decltype(weights);
@@ -839,6 +846,7 @@ __device__ __forceinline__ bool wide_rows(const P &p, unsigned char *lds, const 
       if (i >= span) break;
       id = load_ids(i);
       settle(i);
+      hide_unseen();
       lds_barrier();  // every wave is done with the pages before
       begin();
     }
@@ -849,7 +857,8 @@ __device__ __forceinline__ bool wide_rows(const P &p, unsigned char *lds, const 
     bool odd = !(vss >= 0.f);
     for (int i = 64; i < span; i += 64) {
       const int next = load_ids(i);
-      if (i + lane < span && (unsigned)next < (unsigned)p.c.n_pages) {
+      const bool visible = !Rows::kKnown || (pg0 + i + lane) * kPage <= w.lim_hi;
+      if (visible && i + lane < span && (unsigned)next < (unsigned)p.c.n_pages) {
         const float vs = p.c.v_scale[(size_t)next * p.c.hkv + h];
         most = fmaxf(most, vs);
         least = vs > 0.f ? fminf(least, vs) : least;
