@@ -568,13 +568,14 @@ size_t daf_cache_attn_shared_workspace_size(const daf_attn_cfg_t *cfg,
 
 /* daf_cache_attn, with the pages that a group's sequences have in common read once for all
  * of its rows. Arguments and results as there, with as many bits of a probability as that call
- * gives it. The first shared / 64 entries of the tables
- * of a group's sequences must be the same, which is not checked: where they are not, rows see
- * the keys of another sequence of their group there, as far as their own len goes. Sequences
- * out of range, as a padded batch has them, are left out. A group of more than 256 requests
- * may read its pages once for each 256. Made for groups whose own tokens are few beside the
- * shared ones: those are taken 16 (row, head) pairs at a time. Where the shared pages are few,
- * daf_cache_attn's way through the whole sequences is taken. */
+ * gives it. As far as their len goes, the first shared / 64 entries of the tables of a group's
+ * sequences must be the same, which is not checked: where they are not, rows see the keys of
+ * another sequence of their group there, as far as their own len goes. Sequences out of range,
+ * as a padded batch has them, and sequences that end before the shared tokens do, as freed ones,
+ * change nothing for the others. A group of more than 256 requests may read its pages once for
+ * each 256. Made for groups whose own tokens are few beside the shared ones: those are taken 16
+ * (row, head) pairs at a time. Where the shared pages are few, daf_cache_attn's way through the
+ * whole sequences is taken. */
 daf_status_t daf_cache_attn_shared(const daf_attn_cfg_t *cfg, const daf_cache_t *cache,
                                    int32_t layer, const daf_cache_rows_t *rows,
                                    const daf_cache_groups_t *groups, int32_t max_len,

@@ -676,7 +676,7 @@ struct Wide {
 // Row block r.block of r's rows over the pages pg0 .. pg0 + split_pages - 1, as far as a row
 // sees them, by the whole workgroup: sums in w, O in units of `unit`. False: no keys here.
 // rows: empty(), seen() and limit(row) of the block, the last with a row in r; exact(): bf16's
-// weights as the few rows' kernel has them.
+// weights as the few rows' kernel has them; kKnown: other_pages(), whether r.pages have changed.
 template <bool BF16, int D, int MT, typename P, typename Rows>
 __device__ __forceinline__ bool wide_rows(const P &p, unsigned char *lds, const Request &r, int h, int pg0,
                                           int split_pages, Rows &rows, Wide<BF16, D, MT> &w, float &unit) {
@@ -690,6 +690,8 @@ __device__ __forceinline__ bool wide_rows(const P &p, unsigned char *lds, const 
     return i + lane < split_pages && pg0 + i + lane < p.c.max_seq_pages ? r.pages[pg0 + i + lane] : -1;
   };
   int id = load_ids(0);
+  if constexpr (Rows::kKnown)
+    if (rows.other_pages()) id = load_ids(0);
   if (rows.empty()) return false;
   const int total = r.n * p.group;
   const int seen = rows.seen();  // pages that a row of the block sees

@@ -34,14 +34,41 @@ template <int MT>
 struct GroupRows {
   static constexpr bool kKnown = true;
   const SharedLaunch &p;
+  Request &r;     // of all the group's rows
   int b0, n_req;  // the group's requests
-  int row0;       // its first row
   int pages;      // its pages
-  int *cu, *len;  // LDS, for requests of different rows: first rows from row0 on and tokens
+  int *cu, *len;  // LDS, for requests of different rows: first rows from the group's on and tokens
   int mine[4];    // else tokens of its requests: of lane, 64 + lane, ..; or of thread
-  __device__ __forceinline__ int tokens(int i) const {
-    const int seq = p.seq ? p.seq[b0 + i] : b0 + i;
+  __device__ __forceinline__ int sequence(int i) const { return p.seq ? p.seq[b0 + i] : b0 + i; }
+  __device__ __forceinline__ int tokens_of(int seq) const {
     return min(seq_len(p.c.len, p.c.n_seqs, p.c.max_seq_pages, seq), p.max_len);
+  }
+  __device__ __forceinline__ int tokens(int i) const { return tokens_of(sequence(i)); }
+  // The group's pages are in the tables of its sequences that reach their end. At first they
+  // are taken from the first sequence that is in range (batches are padded), which needs no
+  // length; where that one is shorter (as a freed slot of the batch), from the first that is not, or
+  // the longest.
+  __device__ __forceinline__ void take_pages(int seq) {
+    r.pages = p.c.table + (int64_t)seq * p.c.max_seq_pages;
+    r.L = tokens_of(seq);
+  }
+  __device__ __forceinline__ bool other_pages() {
+    if (r.L >= pages * kPage || n_req == 1) return false;
+    const int lane = threadIdx.x & 63;
+    int longest = -1, at = 0;
+    for (int i = 0; i < n_req && longest < pages * kPage; i += 64) {
+      const int seq = sequence(min(i + lane, n_req - 1)), n = min(tokens_of(seq), pages * kPage);
+      int top = n;
+#pragma unroll
+      for (int m = 32; m; m >>= 1) top = max(top, __shfl_xor(top, m));
+      if (top > longest) {
+        longest = __builtin_amdgcn_readfirstlane(top);
+        at = __builtin_amdgcn_readlane(seq, __builtin_ctzll(__ballot(n == top)));
+      }
+    }
+    if (longest <= r.L) return false;  // the first is the longest
+    take_pages(at);
+    return true;
   }
   // loads, and what waits for them
   __device__ __forceinline__ void start() {
@@ -56,8 +83,8 @@ struct GroupRows {
   __device__ __forceinline__ void prepare() {
     if (p.per_req) return;
     const int i = threadIdx.x;
-    if (i < n_req) cu[i] = p.cu[b0 + i] - row0, len[i] = mine[0];
-    if (i == 0) cu[n_req] = p.cu[b0 + n_req] - row0;
+    if (i < n_req) cu[i] = p.cu[b0 + i] - r.row0, len[i] = mine[0];
+    if (i == 0) cu[n_req] = p.cu[b0 + n_req] - r.row0;
     __syncthreads();
   }
   __device__ __forceinline__ bool exact() const { return p.exact; }
@@ -82,7 +109,7 @@ struct GroupRows {
       L = len[b];
       next = cu[b + 1];
     }
-    const int at = p.pos ? min(p.pos[row0 + row], L - 1) : L - next + row;
+    const int at = p.pos ? min(p.pos[r.row0 + row], L - 1) : L - next + row;
     return max(-1, min(at, pages * kPage - 1));
   }
 };
@@ -155,13 +182,11 @@ __device__ __forceinline__ void group_job(const SharedLaunch &p, SharedMemory<BF
   r.b = gr.b0;
   r.row0 = p.row_of(gr.b0);
   r.n = p.row_of(gr.b1) - r.row0;
-  r.L = 0;  // not used
   const int total = r.n * p.group, blocks = (total + PAIRS - 1) / PAIRS, pages = p.first_page(gr.b0);
   const UnitBlock ub = unit_block(blockIdx.x - gr.wg0, (pages + p.split_pages - 1) / p.split_pages * p.c.hkv, blocks);
   const int h = ub.unit % p.c.hkv, pg0 = ub.unit / p.c.hkv * p.split_pages;
   r.block = ub.block;
-  // the pages are those of the group's first sequence that is in range: batches are padded
-  int seq = 0;
+  int seq = 0;  // the first one in range
   bool there = false;
   for (int b = gr.b0; b < gr.b1 && !there; b += 64) {
     const int at = min(b + lane, gr.b1 - 1), mine = p.seq ? p.seq[at] : at;
@@ -169,8 +194,8 @@ __device__ __forceinline__ void group_job(const SharedLaunch &p, SharedMemory<BF
     there = in != 0;
     if (there) seq = __builtin_amdgcn_readlane(mine, __builtin_ctzll(in));
   }
-  r.pages = p.c.table + (int64_t)seq * p.c.max_seq_pages;
-  GroupRows<MT> rows{p, gr.b0, gr.b1 - gr.b0, r.row0, there ? pages : 0, sh.wide.cu, sh.wide.len, {}};
+  GroupRows<MT> rows{p, r, gr.b0, gr.b1 - gr.b0, there ? pages : 0, sh.wide.cu, sh.wide.len, {}};
+  rows.take_pages(seq);
   rows.start();
   W w;
   float unit;
