@@ -316,8 +316,10 @@ daf_status_t daf_linear_swiglu(int64_t M, int32_t I, int32_t K, const void *A,
  *   a_scales NULL: A [M][K] in bf16. Else A [M][K] are e4m3 codes and a_scales [M][K / 32]
  *   their scales, as daf_add_rmsnorm writes them.
  *   A scale's byte counts as 27 where it is less and 247 where it is more (2^-100 .. 2^120),
- *   255 is NaN; NaN codes of A are NaN. Products are exact, sums fp32; bias and residual are
- *   added in fp32 before the single rounding to bf16. residual may be C itself.
+ *   255 is NaN; NaN codes of A are NaN, and codes of 256 or more under 2^120 are infinite, as
+ *   bf16 has no 2^128. Products are exact where they are 0 or 2^-126 .. 2^128 in size (a smaller
+ *   one may count as 0, a larger one is infinite), sums fp32; bias and residual are added in
+ *   fp32 before the single rounding to bf16. residual may be C itself.
  * N up to 65535 * 256, K a positive multiple of 32 up to 2^24, M up to 65535 * 32
  * (DAF_ERR_UNSUPPORTED otherwise). Made for M up to 32: more rows read the weights again for each 32. Scales
  * need no alignment and are read in whole aligned words of 4 bytes, all else 16 bytes. M = 0
@@ -346,8 +348,8 @@ daf_status_t daf_rmsnorm(int64_t rows, int32_t width, const void *x,
  *   codes [rows][width] and per 32 values one byte b [rows][width / 32] (no alignment),
  *   for a value code * 2^(b - 127): the smallest power of two >= 2^-100 under which the 32
  *   magnitudes are at most 448. Codes are rounded once, to nearest even, from the fp32
- *   values. Infinities count as the largest finite value, NaN stays NaN and does not
- *   count for the scale.
+ *   values. Infinities count as the largest finite value, which rounds to 256 * 2^120 and is
+ *   infinite again in daf_linear_mx; NaN stays NaN and does not count for the scale.
  * At least one of y and codes. fp32 arithmetic. width must be a positive multiple of 8,
  * with codes of 32, rows below 2^23 (DAF_ERR_UNSUPPORTED otherwise); other pointers 16-byte
  * aligned; rows = 0 is a no-op. */

@@ -2,8 +2,9 @@
 // (+ residual), W as e2m1 codes with a power-of-two scale per 32 of a row, A in bf16 or
 // as e4m3 codes with such scales (daf_add_rmsnorm).
 //
-// Codes times their scale become bf16 by one conversion instruction per two values, exactly,
-// so the products of v_mfma_f32_16x16x32_bf16 are exact and sums are fp32. (The
+// Codes times their scale become bf16 by one conversion instruction per two values, exactly
+// below 2^128, so the products of v_mfma_f32_16x16x32_bf16 are exact within fp32's normal
+// range, and sums are fp32. (The
 // instruction that takes the codes and scales themselves keeps about 13 bits of a small
 // term beside a large one.)
 //
@@ -43,8 +44,9 @@ __device__ __forceinline__ f32x4 mfma(const bf16x8 &a, const bf16x8 &b, const f3
 #endif
 }
 
-// 2^(b - 127) of a scale's byte, which counts as one of 27 .. 247 (2^-100 .. 2^120) so that
-// no value of a code is lost or infinite; 255 is NaN
+// 2^(b - 127) of a scale's byte, which counts as one of 27 .. 247 (2^-100 .. 2^120), as rows in
+// 8 bits and weights have them: all values of codes are then normal bf16 values, but for e4m3
+// codes of 256 or more under 2^120, which are infinite; 255 is NaN
 __device__ __forceinline__ float scale_of(unsigned b) {
   const unsigned e = b == 255 ? 0x7fc00000u : min(max(b, 27u), 247u) << 23;
   return __builtin_bit_cast(float, e);
