@@ -373,11 +373,12 @@ int group_pages(const daf_attn_cfg_t *cfg, const daf_cache_rows_t *rows, int b0,
 
 // Whether pages are taken by groups: that is two launches, of which the first begins with more to
 // look up, against daf_cache_attn's one or two, where other requests' copies of a page come from
-// the caches. Both forms' times for 2600 draws of up to 32 requests in 1 to 6 groups, 1 to
-// 40 rows each, prefixes to 512 pages: with up to 32 pages in the longest of the groups'
-// prefixes groups take 1.5 times as long, with up to 64 as long, with more 0.86 (fp32 0.93).
-// Over all draws the chosen form takes 2.0% more than the better one, groups always 34%,
-// groups never 6%. (To count the pages that groups save too made it 1.7%.)
+// the caches. Both forms' times for 6000 draws of up to 32 requests in 1 to 6 groups, 1 to
+// 40 rows each, prefixes to 512 pages: with up to 16 pages in the longest of the groups'
+// prefixes groups take 1.7 times as long, with up to 32 1.1, with up to 64 as long, with more 0.89
+// (fp32 0.98). Over all draws the chosen form takes 2.5% more than the better one (by 64 for 32
+// pages 2.4%), groups always 36%, groups never 5%. (To count the pages that groups save too
+// makes it 1.8%.)
 constexpr int kLeastLongest = 32;
 bool takes_groups(const daf_attn_cfg_t *cfg, const daf_cache_rows_t *rows, const daf_cache_groups_t *g,
                   int32_t max_len) {
@@ -462,9 +463,10 @@ int64_t plan_shared(const daf_attn_cfg_t *cfg, const daf_cache_t *c, const daf_c
   // Of splits that give up to 1, 2, .. 16 workgroups per CU the ones that take least, in us of
   // bf16 and 128 features: 1.5 a page for a workgroup alone on its CU, 1.25 a page and
   // workgroup for more, 0.2 ns a (row, head) and partial result written and read again, 1 for
-  // each 32 that a join reads one after the other. (32 decode rows over 512 pages, us a call:
-  // 256 workgroups 37.8, 376 43.5, 448 40.6, 512 46.8; 301 question rows: 476 217, 612 197, 748 174,
-  // 816 197, 1020 174; 80: 240 68.7, 380 69.8, 500 61.4, 620 72.5.) At least 2 pages, for short
+  // each 32 that a join reads one after the other. (301 question rows over 512 pages, us a call:
+  // 476 workgroups 217, 612 197, 748 174, 816 197, 1020 174; 80: 240 68.7, 380 69.8, 500 61.4,
+  // 620 72.5.) Two bf16 terms take 2.0 for 1.5, by which none of 60 drawn calls is planned
+  // otherwise (32 decode rows: 256 workgroups 42.6, 376 49.7, 512 49.2). At least 2 pages, for short
   // prefixes: 4 beams of 12 pages 11.5, in splits of 4 13.2, of 6 14.7. fp32 and blocks of 64
   // pairs take other times, here by their matrix instructions; fp32 of 128 features has one
   // workgroup per CU.

@@ -13,14 +13,16 @@
 // decode rows over 32768 shared keys 42.5 us a call, with one fp16 term 36.1), else one fp16
 // term (8 requests' 301 question rows 167 us, with two bf16 terms 219; daf_cache_attn 188).
 //
-// Bound by the issue of the many rows' kernel (its comment) where the shared pages have more
-// than a few rows, and by the two launches' chains where they do not: 32 decode rows of 28 heads
-// on 4 of 128 over 32768 shared keys and up to 700 of their own 31.8 + 6.3 us (one copy of the
-// pages, 33.5 MB, is 7 us of HBM; by daf_cache_attn, a copy for each from the caches, 111), 301
-// question rows 157 + 13.9 (141 GFLOP, 0.90 PFLOP/s; by daf_cache_attn 190). A page takes a
-// workgroup alone on its CU 1.5 us, one of two 2.5; ahead of its pages are 6 us of launch, page
-// ids, scales and first copies. Row blocks of 256 pairs (64 rows a wave, 502 registers, one
-// workgroup per CU) at their best splits took 48 us for 36 and 254 for 167.
+// Question rows are bound by the issue of the many rows' kernel (its comment): 301 of 28 heads on
+// 4 of 128 over 32768 shared keys 157 + 13.4 us (141 GFLOP, 0.90 PFLOP/s; by daf_cache_attn 188;
+// fp32 473, by daf_cache_attn 412). Decode rows fill no device by themselves: 32 over 32768 shared
+// keys and up to 700 of their own 39.4 + 6.2 us (one copy of the pages, 33.5 MB, is 7 us of HBM;
+// by daf_cache_attn, a copy for each from the caches, 111; fp32 73 and 132), in 256 workgroups of
+// 16 pages and a wave per SIMD, whose matrix and vector instructions take 75% of its cycles: the
+// rest is waiting, for its own chain and at barriers. A page takes such a workgroup 2.0 us, with
+// one fp16 term 1.5, one of two on a CU 2.5; ahead of its pages are 6 us of launch, page ids, scales
+// and first copies. (Row blocks of 256 pairs, 64 rows a wave, 502 registers, one workgroup per CU,
+// at their best splits, all with one fp16 term: 48 us for 36 and 254 for 167.)
 #include <algorithm>
 
 #include "cache_attn.h"

@@ -16,13 +16,14 @@
 // four operands of 8 values; A is held in the same order of k. A tile's sums of the waves
 // meet in LDS, in a fixed order, one barrier per tile.
 //
-// 32 rows by 37888 x 3584 (72 MB of W) take 18.6 us, 4.0 TB/s, where reading as many bytes
-// takes 13; of the SIMDs' cycles matrix instructions are 21% and vector instructions 36%.
-// Without the joins it takes 16.6, without matrix instructions 17.0, of A alone 5.1 (launch
-// included). Rings beside registers: loads of W to registers in operand layout keep the
-// address unit 64 cycles for 1 KiB, a copy of whole pieces of rows 16; with those, and A
-// read again for each tile, 26 to 42 us. 1 row by 4608 x 3584 6.0 us, most of it launch and
-// one chain of loads; 12 rows by 3584 x 18944 13.5 us in 5 splits, of which the join is 3.9.
+// 32 rows by 37888 x 3584 (72 MB of W) take 18.6 to 19.4 us, 3.9 TB/s, where reading as many
+// bytes takes 13; of the SIMDs' cycles matrix instructions are 22% and vector instructions 36%.
+// In calls of 19.3, without the joins it takes 16.8, without matrix instructions 17.4, of A alone
+// 5.5 (launch included). Rings beside registers: loads of W to registers in operand layout keep
+// the address unit 64 cycles for 1 KiB, a copy of whole pieces of rows 16; the first version,
+// with those and A read again for each tile, took 26 to 42. 1 row by 4608 x 3584 5.7 us, most of
+// it launch and one chain of loads; 12 rows by 3584 x 18944 13.6 us in 5 splits, of which the
+// join is 3.9 and what A takes ahead of W, with launches and join, 8.4.
 #include <algorithm>
 
 #include "step.h"
@@ -140,8 +141,8 @@ struct Slot {
 };
 constexpr int kSlotBytes = 4096 + 512;  // a copy of words writes one for each of 64 lanes
 // Of a wave's ring: two tiles are on their way beside the one that is read. (us: 1 row by 37888 x
-// 3584 14.7, with 2 slots 17.0, with 4 15.9; 12 rows by 3584 x 18944 13.5, 13.3 and 14.8; 32 rows,
-// for which 4 do not fit LDS, by 37888 x 3584 19.5 and 21.1.)
+// 3584 14.8, with 2 slots 17.0, with 4 15.8; 12 rows by 3584 x 18944 13.6, 13.5 and 14.7; 32 rows,
+// for which 4 do not fit LDS, by 37888 x 3584 19.3 and 20.9.)
 constexpr int kSlots = 3;
 
 // The words of 16 rows' scales, `blocks` bytes a row, from block b0 of each on
@@ -405,8 +406,9 @@ void launch(const MxLaunch &p, hipStream_t st) {
 }  // namespace
 
 // Up to 4 steps of a wave, which with two tiles of A are 128 registers, by 8 waves: K above
-// 4096 is split over workgroups. One workgroup per CU (their rings fill its LDS; 512 for 256
-// took 27.2 us for 20.4 in the case of 37888 rows); short K leaves waves for more tiles at once.
+// 4096 is split over workgroups, and more than 32 rows pass W again (37888 x 3584 by 32 rows
+// 19.3 us, 64 28.5, 128 50.4). One workgroup per CU (their rings fill its LDS; 512 for 256 take
+// 23.4 us for 19.3 by 32 rows); short K leaves waves for more tiles at once.
 void plan_linear_mx(MxLaunch &p) {
   const int steps = (p.k + kMxStep - 1) / kMxStep;
   p.mt = p.m <= 16 ? 1 : 2;

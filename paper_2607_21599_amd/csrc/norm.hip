@@ -9,7 +9,7 @@
 // that every input is read once; 8 values per thread and piece, 4 neighbouring lanes have
 // the 32 values of a scale. Sums go in a fixed order: a call's result depends on its inputs
 // alone. Bound by HBM: 5043 rows of 3584 with all outputs (163 MB) in 32 us, the rate of a
-// large copy; one row in 2.0 us, of which most is the launch.
+// large copy (fp32: 308 MB in 59); one row in 2.0 us, of which most is the launch.
 #include "e4m3.h"
 #include "step.h"
 
